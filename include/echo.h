@@ -469,6 +469,131 @@ int echo_refcache_update(const echo_refcache_cfg* cfg, const echo_refcache_state
                          const int32_t* idx, const uint8_t* mask, int32_t n_sel,
                          const float* y_sel, void* xref, void* y, void* stream);
 
+/* ------------------------------------------------------- rows in 8 bits */
+/*
+ * Rows held as codes in [-127, 127] with one fp32 scale per row, for the linear
+ * layers below and for states kept in 8 bits.
+ *
+ * echo_quantize_rows: for i = 0 .. M-1, with a_i = x[r_i] (r_i = rows[i], or i
+ * where rows is NULL), or, where shift and scale are given (both or neither,
+ * fp32 [D]), a_i = LN(x[r_i]) * (1 + scale) + shift (LN as in
+ * echo_block_partial, in fp32, not rounded to 16 bits in between):
+ *   row_scale_i = fp32(max_j |a_ij| / 127)
+ *   codes_ij    = the real quotient 127 a_ij / max_j |a_ij| rounded to the
+ *                 nearest whole number, halves to the even one
+ * A row of zeros has scale 0 and codes 0.  A row with an infinity or NaN, or
+ * with r_i outside [0, x_rows), has scale NaN and codes 0.
+ * x: `dtype`, rows ldx >= D elements apart; codes (16-byte aligned): rows ldq
+ * bytes apart, ldq a multiple of 128 and at least echo_int8_pitch(D); the bytes
+ * between D and ldq are written as zeros.  x, rows and row_scale need the
+ * alignment of their element type only, shift and scale 16 bytes.
+ *
+ * echo_dequantize_rows: x_ij = cast(fp32(row_scale_i * codes_ij)), x being the
+ * output here; rows, shift and scale do not apply (x_rows is not read).
+ *
+ * Requires 1 <= D <= 65536, ldq <= 65536, 0 <= M; M = 0 is a no-op.
+ */
+typedef struct {
+  int32_t M;
+  int32_t D;
+  int32_t dtype;   /* of x */
+  int32_t x_rows;  /* rows of x that `rows` may name (>= M without `rows`) */
+  int64_t ldx;     /* elements between rows of x */
+  int64_t ldq;     /* bytes between rows of codes */
+  float ln_eps;
+} echo_quantize_cfg;
+
+/* D rounded up to a multiple of 128 (0 for D outside [1, 65536]). */
+int64_t echo_int8_pitch(int32_t D);
+int echo_quantize_rows(const echo_quantize_cfg* cfg, const void* x, const int32_t* rows, const float* shift,
+                       const float* scale, int8_t* codes, float* row_scale, void* stream);
+int echo_dequantize_rows(const echo_quantize_cfg* cfg, const int8_t* codes, const float* row_scale, void* x,
+                         void* stream);
+
+/*
+ * Linear layer on such rows: a holds M tokens, w N channels (the weight matrix
+ * [N][K] quantized by row), each with its scales:
+ *   y_mn = f( a_scale_m w_scale_n sum_k a_mk w_nk + bias_n )
+ * The sum is exact (32-bit integers).  epilogue: ECHO_LINEAR_NONE; GELU_TANH;
+ * or GATE_RESIDUAL: f(z) = residual[r_m]_n + gate_n z in fp32 (r_m =
+ * residual_rows[m], or m where that is NULL; a row outside [0,
+ * residual_nrows) gives NaN).  c is written in out_dtype, rounded once.
+ * a: rows lda bytes apart, w: rows ldw bytes apart, both as
+ * echo_quantize_rows writes them: multiples of 128, at least
+ * echo_int8_pitch(K), zeros behind K in one of the two at least.  bias [N] in
+ * bias_dtype or NULL; gate fp32 [N]; residual rows ldr elements apart in
+ * residual_dtype; c rows ldc elements apart.
+ * a, w: 16-byte aligned; every other pointer by its element type.
+ * Requires 1 <= N <= 2^22, 1 <= K <= 65536, M >= 0 (0: no-op), and fewer than
+ * 2^24 tiles of 64 x 64 outputs.
+ */
+typedef enum { ECHO_LINEAR_NONE = 0, ECHO_LINEAR_GELU_TANH = 1, ECHO_LINEAR_GATE_RESIDUAL = 2 } echo_linear_epilogue;
+
+typedef struct {
+  int32_t M;
+  int32_t N;
+  int32_t K;
+  int32_t epilogue;
+  int32_t out_dtype;
+  int32_t bias_dtype;
+  int32_t residual_dtype;
+  int32_t residual_nrows;
+  int64_t lda;
+  int64_t ldw;
+  int64_t ldc;
+  int64_t ldr;
+} echo_linear_int8_cfg;
+
+size_t echo_linear_int8_workspace(const echo_linear_int8_cfg* cfg);
+int echo_linear_int8(const echo_linear_int8_cfg* cfg, const int8_t* a, const float* a_scale, const int8_t* w,
+                     const float* w_scale, const void* bias, const float* gate, const void* residual,
+                     const int32_t* residual_rows, void* c, void* workspace, size_t workspace_bytes, void* stream);
+
+/* --------------------------------------------------------- cross attention */
+/*
+ * Attention of Lq queries to the Lk states of an encoder (of another length),
+ * for B elements, H query heads and Hkv state heads (Hkv divides H; query
+ * head h reads state head h / (H / Hkv)):
+ *   out[b,i,h] = sum_j softmax_j(scale q[b,i,h] . k[b,j,h']) v[b,j,h']
+ * over the states j < k_len[b] (device int32 [B], taken as 0 .. Lk; NULL: Lk)
+ * with key_mask[b][j] != 0 (device uint8 [B][Lk]; NULL: all).  A query with no
+ * such state, or whose scores are all -inf, gets zeros; what masked states
+ * hold has no effect.  Scores, softmax and sums in fp32 (the probabilities
+ * enter the second product in `dtype`).
+ * Every tensor has its strides, in elements, for the element, the row and the
+ * head; dh values are contiguous.  Strides are multiples of 16 bytes and not
+ * negative; those of q, k and v may be 0.
+ * Supported: ECHO_BF16 with dh 64 or 128; ECHO_F32 with dh % 4 == 0, dh <= 128;
+ * scale > 0 and finite; B * Hkv * ceil(Lq * (H / Hkv) / 128) below 2^24.
+ * B, Lq >= 0 (0: no-op), Lk >= 0 (0: every output is zero).
+ */
+typedef struct {
+  int64_t batch;
+  int64_t row;
+  int64_t head;
+} echo_strides;
+
+typedef struct {
+  int32_t B;
+  int32_t Lq;
+  int32_t Lk;
+  int32_t H;
+  int32_t Hkv;
+  int32_t dh;
+  int32_t dtype;
+  float scale;
+  echo_strides q;
+  echo_strides k;
+  echo_strides v;
+  echo_strides out;
+} echo_cross_attention_cfg;
+
+/* masked: whether key_mask will be given */
+size_t echo_cross_attention_workspace(const echo_cross_attention_cfg* cfg, int32_t masked);
+int echo_cross_attention(const echo_cross_attention_cfg* cfg, const void* q, const void* k, const void* v,
+                         const int32_t* k_len, const uint8_t* key_mask, void* out, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------ kernel timing */
 /*
  * Optional per-kernel timing with HIP events, for the calling thread.

@@ -19,6 +19,7 @@ ECHO_F32, ECHO_BF16 = 0, 1
 ECHO_BLOCK_BATCH_INVARIANT = 1
 ECHO_ANCHOR_TOPK, ECHO_ANCHOR_UNIFORM = 0, 1
 ECHO_CODEC_RESIDUAL_INT8, ECHO_CODEC_FULL, ECHO_CODEC_NAIVE_INT8 = 0, 1, 2
+ECHO_LINEAR_NONE, ECHO_LINEAR_GELU_TANH, ECHO_LINEAR_GATE_RESIDUAL = 0, 1, 2
 
 c_int32, c_int64, c_size_t, c_void_p, c_float, c_double = (
     ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_float,
@@ -81,6 +82,28 @@ class ScheduleState(ctypes.Structure):
     _fields_ = [("step", c_int32), ("delta_max", c_double), ("delta_acc", c_double)]
 
 
+class QuantizeCfg(ctypes.Structure):
+    _fields_ = [("M", c_int32), ("D", c_int32), ("dtype", c_int32), ("x_rows", c_int32),
+                ("ldx", c_int64), ("ldq", c_int64), ("ln_eps", c_float)]
+
+
+class LinearInt8Cfg(ctypes.Structure):
+    _fields_ = [("M", c_int32), ("N", c_int32), ("K", c_int32), ("epilogue", c_int32),
+                ("out_dtype", c_int32), ("bias_dtype", c_int32), ("residual_dtype", c_int32),
+                ("residual_nrows", c_int32), ("lda", c_int64), ("ldw", c_int64), ("ldc", c_int64),
+                ("ldr", c_int64)]
+
+
+class Strides(ctypes.Structure):
+    _fields_ = [("batch", c_int64), ("row", c_int64), ("head", c_int64)]
+
+
+class CrossAttentionCfg(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("Lq", c_int32), ("Lk", c_int32), ("H", c_int32), ("Hkv", c_int32),
+                ("dh", c_int32), ("dtype", c_int32), ("scale", c_float), ("q", Strides), ("k", Strides),
+                ("v", Strides), ("out", Strides)]
+
+
 class KernelTime(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char_p), ("launches", c_int64), ("total_ms", c_double)]
 
@@ -127,6 +150,18 @@ _SIGNATURES = {
     "echo_refcache_update": (ctypes.c_int, [_P(RefCacheCfg), _P(RefCacheState), c_void_p,
                                             c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
                                             c_void_p, c_void_p]),
+    "echo_int8_pitch": (c_int64, [c_int32]),
+    "echo_quantize_rows": (ctypes.c_int, [_P(QuantizeCfg), c_void_p, c_void_p, c_void_p, c_void_p,
+                                          c_void_p, c_void_p, c_void_p]),
+    "echo_dequantize_rows": (ctypes.c_int, [_P(QuantizeCfg), c_void_p, c_void_p, c_void_p, c_void_p]),
+    "echo_linear_int8_workspace": (c_size_t, [_P(LinearInt8Cfg)]),
+    "echo_linear_int8": (ctypes.c_int, [_P(LinearInt8Cfg), c_void_p, c_void_p, c_void_p, c_void_p,
+                                        c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                        c_size_t, c_void_p]),
+    "echo_cross_attention_workspace": (c_size_t, [_P(CrossAttentionCfg), c_int32]),
+    "echo_cross_attention": (ctypes.c_int, [_P(CrossAttentionCfg), c_void_p, c_void_p, c_void_p,
+                                            c_void_p, c_void_p, c_void_p, c_void_p, c_size_t,
+                                            c_void_p]),
     "echo_profile_enable": (ctypes.c_int, [ctypes.c_int]),
     "echo_profile_read": (ctypes.c_int, [_P(KernelTime), c_int32]),
     "echo_mfma_ceiling": (ctypes.c_int, [c_int32, c_int32, c_double, _P(c_double), c_void_p]),

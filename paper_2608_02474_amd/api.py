@@ -10,6 +10,12 @@ step of the path runs in the library's HIP kernels.
   block_partial(w, x, idx, n_sel, H)     DiT block on the selected tokens
   cache_update(x, idx, mask, n_sel, ...) int8 residual cache write + reuse
   CachedBlock                            the four calls composed, with its cache
+
+and the operators of a block served in 8 bits:
+
+  quantize_rows / dequantize_rows        rows as 8-bit codes with a scale each
+  linear_int8(a, w, bias, ...)           linear layer on such rows
+  cross_attention(q, k, v, ...)          attention to states of another length
 """
 from __future__ import annotations
 
@@ -19,8 +25,8 @@ import dataclasses
 import torch
 
 from . import _lib
-from ._lib import (BlockCfg, BlockWeights, CacheCfg, EnergyCfg, KernelTime, RefCacheCfg, WanBlockCfg,
-                   WanBlockWeights,
+from ._lib import (BlockCfg, BlockWeights, CacheCfg, CrossAttentionCfg, EnergyCfg, KernelTime, LinearInt8Cfg,
+                   QuantizeCfg, RefCacheCfg, Strides, WanBlockCfg, WanBlockWeights,
                    RefCacheState, ScheduleCfg, ScheduleState, SelectCfg,
                    ECHO_BF16, ECHO_F32, check)
 
@@ -361,7 +367,7 @@ class BlockStack:
         self.y_sel = torch.empty((L, D), dtype=torch.float32, **kw)
         self.all_idx = torch.arange(L, dtype=torch.int32, **kw)
         self.all_mask = torch.ones(L, dtype=torch.uint8, **kw)
-        self._w = [block_weights(p) for p in params]
+        self._w = [None if is_int8_block(p) else block_weights(p) for p in params]
         self.ws, self.sel_ws, self.sel = Workspace(), Workspace(), None
         self._unit = None
         self.history = []   # (k, full, delta_t) per step; k per segment in the two-stage form
@@ -432,7 +438,12 @@ def block_partial(params: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int, 
                   workspace: Workspace | None = None, _weights: BlockWeights | None = None,
                   batch_invariant: bool = False):
     """y_sel [n_sel, D] fp32 = block output of tokens idx[:n_sel].  With
-    batch_invariant, each row is bit-identical for any selection containing it."""
+    batch_invariant, each row is bit-identical for any selection containing it.
+    With weights in 8 bits (quantize_block) the block runs on 8-bit rows."""
+    if is_int8_block(params):
+        if batch_invariant:
+            raise ValueError("batch_invariant does not go with weights in 8 bits")
+        return _block_partial_int8(params, x, idx, n_sel, H, ln_eps, y_sel)
     lib = _lib_handle()
     _dev(x, "x")
     _dev(idx, "idx", torch.int32)
@@ -458,6 +469,53 @@ def block_partial(params: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int, 
           lib.echo_block_partial(ctypes.byref(cfg), ctypes.byref(w), _ptr(x), _ptr(idx), n_sel,
                                  _ptr(y_sel), _ptr(ws), ws.numel(), _stream()))
     return y_sel[:n_sel]
+
+
+MATRIX_NAMES = ("wq", "wk", "wv", "wo", "w1", "w2")
+
+
+def quantize_block(params: dict) -> dict:
+    """The block's parameters with its six weight matrices in 8 bits, a scale for
+    each output channel (Int8Rows); biases and modulation as they are.
+    block_partial, CachedBlock and BlockStack take them in place of params."""
+    return {**params, **{n: quantize_rows(params[n]) for n in MATRIX_NAMES}}
+
+
+def is_int8_block(params: dict) -> bool:
+    return isinstance(params["wq"], Int8Rows)
+
+
+def _block_partial_int8(p: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int, H: int, ln_eps: float,
+                        y_sel: torch.Tensor | None) -> torch.Tensor:
+    """block_partial on 8-bit rows: the tokens are quantized in front of every
+    product, one scale a token; attention, residuals and LayerNorms as there."""
+    _dev(x, "x")
+    L, D = x.shape
+    _dev(p["mod"], "mod", torch.float32)
+    if p["mod"].shape != (6, D):
+        raise ValueError(f"mod must be [6, {D}]")
+    if D % H:
+        raise ValueError("H must divide D")
+    for n in ("bq", "bk", "bv", "bo", "b1", "b2"):
+        _dev(p[n], n, x.dtype)
+    if y_sel is None:
+        y_sel = torch.empty((max(n_sel, 1), D), dtype=torch.float32, device=x.device)
+    y = y_sel[:n_sel]
+    if n_sel == 0:
+        return y
+    rows = _dev(idx, "idx", torch.int32)[:n_sel]
+    mod, dt = p["mod"], x.dtype
+    a = quantize_rows(x, shift=mod[0], scale=mod[1], ln_eps=ln_eps)
+    a_sel = quantize_rows(x, rows=rows, shift=mod[0], scale=mod[1], ln_eps=ln_eps)
+    q = linear_int8(a_sel, p["wq"], p["bq"], dtype=dt).view(1, n_sel, H, D // H)
+    k = linear_int8(a, p["wk"], p["bk"], dtype=dt).view(1, L, H, D // H)
+    v = linear_int8(a, p["wv"], p["bv"], dtype=dt).view(1, L, H, D // H)
+    o = cross_attention(q, k, v).view(n_sel, D)
+    x1 = linear_int8(quantize_rows(o), p["wo"], p["bo"], gate=mod[2], residual=x, residual_rows=rows,
+                     dtype=torch.float32)
+    b = quantize_rows(x1, shift=mod[3], scale=mod[4], ln_eps=ln_eps)
+    h = linear_int8(b, p["w1"], p["b1"], activation="gelu", dtype=dt)
+    return linear_int8(quantize_rows(h), p["w2"], p["b2"], gate=mod[5], residual=x1, out=y)
 
 
 # ----------------------------------------------------------- Wan-style block
@@ -623,6 +681,243 @@ class RefCache:
         return self.live_refs() * self.D * self.pool.element_size() + self.codes.numel() + 4 * self.L
 
 
+# ------------------------------------------------------------- rows in 8 bits
+
+@dataclasses.dataclass
+class Int8Rows:
+    """Rows held in 8 bits: value [i, j] = scale[i] * codes[i, j], j < cols.
+    The codes' pitch is a multiple of 128, with zeros behind the last column
+    (quantize_rows writes them so; weights are quantized once, by channel)."""
+    codes: torch.Tensor        # int8 [rows, pitch]
+    scale: torch.Tensor        # fp32 [rows]
+    cols: int
+
+    def __len__(self) -> int:
+        return self.codes.shape[0]
+
+
+def _here(first: torch.Tensor, **others) -> None:
+    """Every tensor on the current device: the kernels run on its current stream."""
+    if first.get_device() != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current device")
+    for name, t in others.items():
+        if t is not None and t.get_device() != first.get_device():
+            raise ValueError(f"{name} must be on the same device as the other tensors")
+
+
+def _rows_of(t: torch.Tensor, name: str, dtype=None) -> torch.Tensor:
+    """A [rows, columns] device tensor whose columns are contiguous (rows may lie apart)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [rows, columns] with contiguous columns")
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"{name} must not have overlapping rows")
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _vector(t: torch.Tensor, name: str, n: int, dtype=None) -> torch.Tensor:
+    _dev(t, name, dtype)
+    if t.dim() != 1 or t.numel() != n:
+        raise ValueError(f"{name} must be [{n}]")
+    return t
+
+
+def _int8_rows(r: Int8Rows, name: str) -> Int8Rows:
+    if not isinstance(r, Int8Rows):
+        raise TypeError(f"{name} must be Int8Rows (see quantize_rows)")
+    _rows_of(r.codes, f"{name}.codes", torch.int8)
+    _vector(r.scale, f"{name}.scale", r.codes.shape[0], torch.float32)
+    pitch = _lib_handle().echo_int8_pitch(int(r.cols))
+    if pitch == 0 or r.codes.shape[1] < pitch or r.codes.shape[1] % 128 or _ld(r.codes) % 128:
+        raise ValueError(f"{name}.codes must have a pitch of {pitch} bytes or a larger multiple of 128")
+    return r
+
+
+def quantize_rows(x: torch.Tensor, rows: torch.Tensor | None = None, shift: torch.Tensor | None = None,
+                  scale: torch.Tensor | None = None, ln_eps: float = 1e-6,
+                  out: Int8Rows | None = None) -> Int8Rows:
+    """Rows of x ([M, D], contiguous columns) as 8-bit codes with one scale each
+    (echo_quantize_rows); rows (int32) picks rows of x, shift and scale (fp32
+    [D]) put a modulated LayerNorm in front.  Quantizes a weight matrix
+    [channels, inputs] as well as tokens."""
+    lib = _lib_handle()
+    _rows_of(x, "x")
+    n, D = x.shape
+    M = n
+    if rows is not None:
+        M = _dev(rows, "rows", torch.int32).numel()
+        if rows.dim() != 1:
+            raise ValueError("rows must be one-dimensional")
+        if M > 0 and n == 0:
+            raise ValueError("x has no rows to pick")
+    if (shift is None) != (scale is None):
+        raise ValueError("pass shift and scale together")
+    if shift is not None:
+        _vector(shift, "shift", D, torch.float32)
+        _vector(scale, "scale", D, torch.float32)
+    pitch = lib.echo_int8_pitch(D)
+    if pitch == 0:
+        raise ValueError("rows of at most 65536 columns")
+    if out is None:
+        out = Int8Rows(torch.empty((M, pitch), dtype=torch.int8, device=x.device),
+                       torch.empty(M, dtype=torch.float32, device=x.device), D)
+    elif len(_int8_rows(out, "out")) != M or out.cols != D:
+        raise ValueError(f"out must hold {M} rows of {D} columns")
+    _here(x, rows=rows, shift=shift, scale=scale, codes=out.codes, row_scale=out.scale)
+    cfg = QuantizeCfg(M, D, _echo_dtype(x), n, _ld(x), _ld(out.codes), float(ln_eps))
+    check("echo_quantize_rows",
+          lib.echo_quantize_rows(ctypes.byref(cfg), _ptr(x), _ptr(rows), _ptr(shift), _ptr(scale),
+                                 _ptr(out.codes), _ptr(out.scale), _stream()))
+    return out
+
+
+def dequantize_rows(r: Int8Rows, dtype=torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values the codes stand for, [rows, cols] in dtype (echo_dequantize_rows)."""
+    lib = _lib_handle()
+    _int8_rows(r, "r")
+    M, D = len(r), int(r.cols)
+    if out is None:
+        out = torch.empty((M, D), dtype=dtype, device=r.codes.device)
+    elif _rows_of(out, "out").shape != (M, D):
+        raise ValueError(f"out must be [{M}, {D}]")
+    _here(r.codes, scale=r.scale, out=out)
+    cfg = QuantizeCfg(M, D, _echo_dtype(out), M, _ld(out), _ld(r.codes), 0.0)
+    check("echo_dequantize_rows",
+          lib.echo_dequantize_rows(ctypes.byref(cfg), _ptr(r.codes), _ptr(r.scale), _ptr(out), _stream()))
+    return out
+
+
+def linear_int8(a: Int8Rows, w: Int8Rows, bias: torch.Tensor | None = None, activation: str | None = None,
+                gate: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+                residual_rows: torch.Tensor | None = None, dtype=torch.bfloat16,
+                out: torch.Tensor | None = None, workspace: Workspace | None = None) -> torch.Tensor:
+    """Linear layer on 8-bit rows (echo_linear_int8): a [M tokens], w [N channels]
+    -> [M, N] in dtype.  activation: None or "gelu" (tanh form); or gate (fp32
+    [N]) and residual ([rows, N], picked by residual_rows): residual + gate * y."""
+    lib = _lib_handle()
+    _int8_rows(a, "a")
+    _int8_rows(w, "w")
+    M, N, K = len(a), len(w), int(a.cols)
+    if w.cols != K:
+        raise ValueError(f"a has {K} columns, w {w.cols}")
+    if activation not in (None, "gelu"):
+        raise ValueError('activation must be None or "gelu"')
+    if (gate is None) != (residual is None) or (residual is None and residual_rows is not None):
+        raise ValueError("pass gate and residual together (residual_rows with them)")
+    if gate is not None and activation is not None:
+        raise ValueError("activation does not go with gate and residual")
+    bias_dt = res_dt = ECHO_F32
+    if bias is not None:
+        bias_dt = _echo_dtype(_vector(bias, "bias", N))
+    nres = ldr = 0
+    if gate is not None:
+        _vector(gate, "gate", N, torch.float32)
+        res_dt = _echo_dtype(_rows_of(residual, "residual"))
+        nres, ldr = residual.shape[0], _ld(residual)
+        if residual.shape[1] != N:
+            raise ValueError(f"residual must have {N} columns")
+        if residual_rows is not None:
+            _vector(residual_rows, "residual_rows", M, torch.int32)
+        elif nres != M:
+            raise ValueError(f"residual must have {M} rows")
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype, device=a.codes.device)
+    elif _rows_of(out, "out").shape != (M, N):
+        raise ValueError(f"out must be [{M}, {N}]")
+    _here(a.codes, a_scale=a.scale, w=w.codes, w_scale=w.scale, bias=bias, gate=gate, residual=residual,
+          residual_rows=residual_rows, out=out)
+    epi = (_lib.ECHO_LINEAR_GATE_RESIDUAL if gate is not None
+           else _lib.ECHO_LINEAR_GELU_TANH if activation else _lib.ECHO_LINEAR_NONE)
+    cfg = LinearInt8Cfg(M, N, K, epi, _echo_dtype(out), bias_dt, res_dt, nres, _ld(a.codes), _ld(w.codes),
+                        _ld(out), ldr)
+    need = lib.echo_linear_int8_workspace(ctypes.byref(cfg))
+    ws = _scratch(need, workspace, out.device)
+    check("echo_linear_int8",
+          lib.echo_linear_int8(ctypes.byref(cfg), _ptr(a.codes), _ptr(a.scale), _ptr(w.codes), _ptr(w.scale),
+                               _ptr(bias), _ptr(gate), _ptr(residual), _ptr(residual_rows), _ptr(out),
+                               _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+    return out
+
+
+def _scratch(need: int, workspace: Workspace | None, device) -> torch.Tensor | None:
+    """`need` bytes from the caller's workspace, or of this call's own (ordered
+    on its stream by torch's allocator, so that calls on several streams and
+    captured graphs never share one)."""
+    if need == 0:
+        return None
+    if workspace is not None:
+        return workspace.get(need, device)
+    return torch.empty(need, dtype=torch.uint8, device=device)
+
+
+# ------------------------------------------------------------ cross attention
+
+def _heads_of(t: torch.Tensor, name: str, dtype=None) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 4 or t.shape[2] < 1 or (t.shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError(f"{name} must be [elements, rows, heads, dh] with contiguous dh")
+    return t
+
+
+def _strides(t: torch.Tensor) -> Strides:
+    """(element, row, head) strides; those of a single one are not used."""
+    return Strides(*[t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)])
+
+
+def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: torch.Tensor | None = None,
+                    key_mask: torch.Tensor | None = None, scale: float | None = None,
+                    out: torch.Tensor | None = None, workspace: Workspace | None = None) -> torch.Tensor:
+    """Attention of q [B, Lq, H, dh] to the states k, v [B, Lk, Hkv, dh]
+    (echo_cross_attention; any strides with contiguous dh): the first k_len[b]
+    (int32 [B]) states that key_mask (uint8 or bool [B, Lk]) leaves; a query
+    without any gets zeros.  scale: 1 / sqrt(dh) by default.  Returns
+    [B, Lq, H, dh]."""
+    lib = _lib_handle()
+    _heads_of(q, "q")
+    _heads_of(k, "k", q.dtype)
+    _heads_of(v, "v", q.dtype)
+    B, Lq, H, dh = q.shape
+    Lk, Hkv = k.shape[1], k.shape[2]
+    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != dh or H % Hkv:
+        raise ValueError("k and v must be [B, Lk, Hkv, dh] with Hkv dividing q's heads")
+    if k_len is not None:
+        _vector(k_len, "k_len", B, torch.int32)
+    if key_mask is not None:
+        if key_mask.dtype == torch.bool:
+            key_mask = key_mask.view(torch.uint8)
+        _dev(key_mask, "key_mask", torch.uint8)
+        if key_mask.shape != (B, Lk):
+            raise ValueError(f"key_mask must be [{B}, {Lk}]")
+    if out is None:
+        out = torch.empty((B, Lq, H, dh), dtype=q.dtype, device=q.device)
+    elif _heads_of(out, "out", q.dtype).shape != q.shape or any(
+            out.stride(i) == 0 for i in range(3) if out.shape[i] > 1):
+        raise ValueError("out must have the shape of q, and no row twice")
+    _here(q, k=k, v=v, k_len=k_len, key_mask=key_mask, out=out)
+    cfg = CrossAttentionCfg(B, Lq, Lk, H, Hkv, dh, _echo_dtype(q), dh ** -0.5 if scale is None else float(scale),
+                            _strides(q), _strides(k), _strides(v), _strides(out))
+    need = lib.echo_cross_attention_workspace(ctypes.byref(cfg), 0 if key_mask is None else 1)
+    ws = _scratch(need, workspace, q.device)
+    check("echo_cross_attention",
+          lib.echo_cross_attention(ctypes.byref(cfg), _ptr(q), _ptr(k), _ptr(v), _ptr(k_len), _ptr(key_mask),
+                                   _ptr(out), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+    return out
+
+
 # ------------------------------------------------------------- kernel timing
 
 def profile_enable(on: bool = True) -> None:
@@ -677,7 +972,7 @@ class CachedBlock:
         self.ws = Workspace()
         self.sel_ws = Workspace()
         self.sel = None
-        self._w = block_weights(params)
+        self._w = None if is_int8_block(params) else block_weights(params)
 
     def init(self, x: torch.Tensor) -> torch.Tensor:
         ys = block_partial(self.params, x, self.all_idx, self.L, self.H, self.ln_eps,

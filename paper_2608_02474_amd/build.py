@@ -22,7 +22,7 @@ ARCH = "gfx950"
 
 SOURCES = ["echo_abi.cpp", "energy.hip", "select.hip", "cache.hip", "block_ln.hip",
            "gemm_bf16.hip", "attn_bf16.hip", "block_f32.hip", "refcache.hip", "wan.hip",
-           "mfma_ceiling.hip"]
+           "mfma_ceiling.hip", "quant.hip", "gemm_int8.hip", "attn_cross.hip"]
 
 # Packed fp32 instructions are disabled for every device pass.
 COMMON_FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",

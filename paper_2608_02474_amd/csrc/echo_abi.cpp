@@ -288,6 +288,58 @@ bool wan_weights_ok(const echo_wan_block_weights* w) {
 }
 }  // namespace
 
+namespace {
+// ---- rows in 8 bits
+bool elem_aligned(const void* p, size_t es) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) % es) == 0; }
+bool quantize_cfg_ok(const echo_quantize_cfg* c) {
+  return c != nullptr && c->M >= 0 && c->D >= 1 && c->D <= 65536 && ok_dtype(c->dtype) && c->ldx >= c->D &&
+         c->ldq >= echo_int8_pitch(c->D) && c->ldq <= 65536 && (c->ldq % 128) == 0 && c->ln_eps >= 0.0f;
+}
+bool linear_cfg_ok(const echo_linear_int8_cfg* c) {
+  return c != nullptr && c->M >= 0 && c->N >= 1 && c->K >= 1 && c->K <= 65536 && ok_dtype(c->out_dtype) &&
+         ok_dtype(c->bias_dtype) && ok_dtype(c->residual_dtype) &&
+         (c->epilogue == ECHO_LINEAR_NONE || c->epilogue == ECHO_LINEAR_GELU_TANH ||
+          c->epilogue == ECHO_LINEAR_GATE_RESIDUAL) &&
+         c->lda >= echo_int8_pitch(c->K) && (c->lda % 128) == 0 && c->ldw >= echo_int8_pitch(c->K) &&
+         (c->ldw % 128) == 0 && c->lda <= 65536 && c->ldw <= 65536 && c->ldc >= c->N &&
+         (c->epilogue != ECHO_LINEAR_GATE_RESIDUAL || c->ldr >= c->N);
+}
+// a launch holds fewer than 2^32 threads: 2^24 workgroups of 256
+constexpr int64_t kMaxGroups = int64_t(1) << 24;
+bool linear_supported(const echo_linear_int8_cfg* c) {
+  return c->N <= (1 << 22) && ((int64_t(c->M) + 63) / 64) * ((int64_t(c->N) + 63) / 64) < kMaxGroups;
+}
+
+// ---- cross attention
+bool strides_ok(const echo_strides& s, int per16) {
+  return s.batch >= 0 && s.row >= 0 && s.head >= 0 && s.batch % per16 == 0 && s.row % per16 == 0 &&
+         s.head % per16 == 0;
+}
+bool cross_cfg_ok(const echo_cross_attention_cfg* c) {
+  if (c == nullptr || c->B < 0 || c->Lq < 0 || c->Lk < 0 || c->H < 1 || c->Hkv < 1 || c->H % c->Hkv != 0 ||
+      c->dh < 1 || !ok_dtype(c->dtype) || !std::isfinite(c->scale) || !(c->scale > 0.0f))
+    return false;
+  const int per16 = c->dtype == ECHO_BF16 ? 8 : 4;
+  return strides_ok(c->q, per16) && strides_ok(c->k, per16) && strides_ok(c->v, per16) && strides_ok(c->out, per16);
+}
+bool cross_supported(const echo_cross_attention_cfg* c) {
+  if (c->dtype == ECHO_BF16 ? (c->dh != 64 && c->dh != 128) : (c->dh % 4 != 0 || c->dh > 128)) return false;
+  if (!std::isfinite(c->scale * 1.4426950408889634f)) return false;  // the scale in units of log2
+  const int64_t rows = int64_t(c->H / c->Hkv) * c->Lq, groups = int64_t(c->B) * c->Hkv;
+  return rows < (int64_t(1) << 31) - 128 && groups < kMaxGroups && groups * ((rows + 127) / 128) < kMaxGroups;
+}
+CrossArgs cross_args(const echo_cross_attention_cfg* c) {
+  CrossArgs a{};
+  a.qb = c->q.batch; a.qr = c->q.row; a.qh = c->q.head;
+  a.kb = c->k.batch; a.kr = c->k.row; a.kh = c->k.head;
+  a.vb = c->v.batch; a.vr = c->v.row; a.vh = c->v.head;
+  a.ob = c->out.batch; a.orow = c->out.row; a.oh = c->out.head;
+  a.B = c->B; a.Lq = c->Lq; a.Lk = c->Lk; a.H = c->H; a.Hkv = c->Hkv; a.dh = c->dh;
+  a.scale_log2 = static_cast<float>(c->scale * 1.4426950408889634);
+  return a;
+}
+}  // namespace
+
 extern "C" {
 
 const char* echo_status_str(int status) {
@@ -720,6 +772,88 @@ int echo_refcache_update(const echo_refcache_cfg* cfg, const echo_refcache_state
       cfg->dtype == ECHO_BF16, x, idx, mask, n_sel, cfg->L, cfg->D, cfg->chain_len, cfg->tau, y_sel, st->pool,
       st->refcount, st->free_list, st->free_top, st->chain_ref, st->ent_slot, st->ent_kind, st->codes,
       st->scale, xref, y, static_cast<hipStream_t>(stream)));
+}
+
+int64_t echo_int8_pitch(int32_t D) { return D < 1 || D > 65536 ? 0 : (int64_t(D) + 127) / 128 * 128; }
+
+int echo_quantize_rows(const echo_quantize_cfg* cfg, const void* x, const int32_t* rows, const float* shift,
+                       const float* scale, int8_t* codes, float* row_scale, void* stream) {
+  if (!quantize_cfg_ok(cfg) || (shift == nullptr) != (scale == nullptr)) return ECHO_EINVAL;
+  if (cfg->M == 0) return ECHO_OK;
+  if (!elem_aligned(x, esize(cfg->dtype)) || !ok_ptr(codes) || !elem_aligned(row_scale, 4) ||
+      (rows != nullptr ? !elem_aligned(rows, 4) || cfg->x_rows < 1 : cfg->x_rows < cfg->M) ||
+      (shift != nullptr && (!ok_ptr(shift) || !ok_ptr(scale))))
+    return ECHO_EINVAL;
+  const QuantizeArgs a{x,    cfg->ldx, rows,  cfg->x_rows, cfg->M, cfg->D, shift, scale, cfg->ln_eps,
+                       codes, cfg->ldq, row_scale};
+  return device_status(launch_quantize_rows(cfg->dtype == ECHO_BF16, a, static_cast<hipStream_t>(stream)));
+}
+
+int echo_dequantize_rows(const echo_quantize_cfg* cfg, const int8_t* codes, const float* row_scale, void* x,
+                         void* stream) {
+  if (!quantize_cfg_ok(cfg)) return ECHO_EINVAL;
+  if (cfg->M == 0) return ECHO_OK;
+  if (!ok_ptr(codes) || !elem_aligned(row_scale, 4) || !elem_aligned(x, esize(cfg->dtype))) return ECHO_EINVAL;
+  const DequantizeArgs a{codes, cfg->ldq, row_scale, cfg->M, cfg->D, x, cfg->ldx};
+  return device_status(launch_dequantize_rows(cfg->dtype == ECHO_BF16, a, static_cast<hipStream_t>(stream)));
+}
+
+size_t echo_linear_int8_workspace(const echo_linear_int8_cfg* cfg) {
+  if (!linear_cfg_ok(cfg) || !linear_supported(cfg) || cfg->M == 0) return 0;
+  return gemm_i8_partial_bytes(cfg->M, cfg->N, static_cast<int>(echo_int8_pitch(cfg->K)));
+}
+
+int echo_linear_int8(const echo_linear_int8_cfg* cfg, const int8_t* a, const float* a_scale, const int8_t* w,
+                     const float* w_scale, const void* bias, const float* gate, const void* residual,
+                     const int32_t* residual_rows, void* c, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!linear_cfg_ok(cfg)) return ECHO_EINVAL;
+  if (!linear_supported(cfg)) return ECHO_EUNSUPPORTED;
+  if (cfg->M == 0) return ECHO_OK;
+  const bool gated = cfg->epilogue == ECHO_LINEAR_GATE_RESIDUAL;
+  if (!ok_ptr(a) || !elem_aligned(a_scale, 4) || !ok_ptr(w) || !elem_aligned(w_scale, 4) || !elem_aligned(c, esize(cfg->out_dtype)) ||
+      (bias != nullptr && !elem_aligned(bias, esize(cfg->bias_dtype))))
+    return ECHO_EINVAL;
+  if (gated ? (!elem_aligned(gate, 4) || !elem_aligned(residual, esize(cfg->residual_dtype)) ||
+               (residual_rows != nullptr ? !elem_aligned(residual_rows, 4) || cfg->residual_nrows < 1
+                                         : cfg->residual_nrows < cfg->M))
+            : (gate != nullptr || residual != nullptr || residual_rows != nullptr))
+    return ECHO_EINVAL;
+  const size_t need = echo_linear_int8_workspace(cfg);
+  if (need > 0 && (!ok_ptr(workspace) || workspace_bytes < need)) return ECHO_EWORKSPACE;
+  GemmI8Args g{};
+  g.A = a; g.lda = cfg->lda; g.sa = a_scale;
+  g.B = w; g.ldb = cfg->ldw; g.sb = w_scale;
+  g.M = cfg->M; g.N = cfg->N; g.K = static_cast<int>(echo_int8_pitch(cfg->K));
+  g.bias = bias; g.bias_bf16 = cfg->bias_dtype == ECHO_BF16;
+  g.C = c; g.c_bf16 = cfg->out_dtype == ECHO_BF16; g.ldc = cfg->ldc;
+  g.gate = gate; g.res = residual; g.res_bf16 = cfg->residual_dtype == ECHO_BF16; g.ldr = cfg->ldr;
+  g.res_rows = residual_rows; g.res_nrows = cfg->residual_nrows;
+  g.part = static_cast<int32_t*>(workspace); g.part_bytes = workspace_bytes;
+  return device_status(launch_gemm_i8(cfg->epilogue, g, static_cast<hipStream_t>(stream)));
+}
+
+size_t echo_cross_attention_workspace(const echo_cross_attention_cfg* cfg, int32_t masked) {
+  if (!cross_cfg_ok(cfg) || !cross_supported(cfg) || cfg->B == 0 || cfg->Lq == 0) return 0;
+  return cross_workspace_bytes(cfg->dtype == ECHO_BF16, cfg->B, cfg->Lq, cfg->Lk, cfg->H, cfg->Hkv, cfg->dh,
+                               masked != 0 && cfg->Lk > 0);
+}
+
+int echo_cross_attention(const echo_cross_attention_cfg* cfg, const void* q, const void* k, const void* v,
+                         const int32_t* k_len, const uint8_t* key_mask, void* out, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  if (!cross_cfg_ok(cfg)) return ECHO_EINVAL;
+  if (!cross_supported(cfg)) return ECHO_EUNSUPPORTED;
+  if (cfg->B == 0 || cfg->Lq == 0) return ECHO_OK;
+  const bool states = cfg->Lk > 0;  // without any, k, v and the masks are not looked at
+  if (!ok_ptr(q) || !ok_ptr(out) || (states && (!ok_ptr(k) || !ok_ptr(v) || (k_len != nullptr && !elem_aligned(k_len, 4)))))
+    return ECHO_EINVAL;
+  const size_t need = echo_cross_attention_workspace(cfg, key_mask != nullptr);
+  if (need > 0 && (!ok_ptr(workspace) || workspace_bytes < need)) return ECHO_EWORKSPACE;
+  CrossArgs a = cross_args(cfg);
+  a.q = q; a.k = k; a.v = v; a.out = out;
+  a.k_len = states ? k_len : nullptr;
+  a.key_mask = states ? key_mask : nullptr;
+  return device_status(launch_cross(cfg->dtype == ECHO_BF16, a, workspace, static_cast<hipStream_t>(stream)));
 }
 
 int echo_mfma_ceiling(int32_t pattern, int32_t data, double seconds, double* tflops, void* stream) {

@@ -154,4 +154,74 @@ hipError_t run_mfma_ceiling(int pattern, int gaussian, double seconds, double* t
 hipError_t launch_attn_f32(const float* q, int64_t ldq, const float* k, const float* v, int64_t ldkv,
                            int Mq, int L, int H, int dh, float* out, int64_t ldo, hipStream_t stream);
 
+// ---- rows in 8 bits (quant.hip, gemm_int8.hip): codes int8 [M][ldq], one fp32
+// scale per row, zeros between D and ldq (ldq % 128 == 0)
+struct QuantizeArgs {
+  const void* x;
+  int64_t ldx;
+  const int32_t* rows;   // optional: row i is x row rows[i]
+  int x_rows;
+  int M, D;
+  const float* shift;    // optional modulated LayerNorm in front
+  const float* scale;
+  float ln_eps;
+  int8_t* codes;
+  int64_t ldq;
+  float* row_scale;
+};
+struct DequantizeArgs {
+  const int8_t* codes;
+  int64_t ldq;
+  const float* row_scale;
+  int M, D;
+  void* y;
+  int64_t ldy;
+};
+hipError_t launch_quantize_rows(int dtype_bf16, const QuantizeArgs& p, hipStream_t stream);
+hipError_t launch_dequantize_rows(int dtype_bf16, const DequantizeArgs& p, hipStream_t stream);
+
+// C[m, n] = epilogue(sa[m] sb[n] sum_k A[m, k] B[n, k] + bias[n]), see gemm_int8.hip
+struct GemmI8Args {
+  const int8_t* A;
+  int64_t lda;
+  const float* sa;
+  const int8_t* B;
+  int64_t ldb;
+  const float* sb;
+  int M, N, K;             // K in bytes, a multiple of 128
+  const void* bias;        // [N], optional
+  int bias_bf16;
+  void* C;
+  int c_bf16;
+  int64_t ldc;
+  const float* gate;       // [N], EPI_GATE_RES
+  const void* res;         // EPI_GATE_RES residual rows
+  int res_bf16;
+  int64_t ldr;
+  const int32_t* res_rows; // optional gather of residual rows
+  int res_nrows;
+  int32_t* part;           // partial sums of split products
+  size_t part_bytes;
+  int nsplit, kps;         // set by the launcher: k-ranges of a tile, k-steps of a range
+};
+size_t gemm_i8_partial_bytes(int M, int N, int K);
+hipError_t launch_gemm_i8(int epi, const GemmI8Args& a, hipStream_t stream);
+
+// ---- attention to states of another length (attn_cross.hip)
+struct CrossArgs {
+  const void *q, *k, *v;
+  void* out;
+  int64_t qb, qr, qh, kb, kr, kh, vb, vr, vh, ob, orow, oh;  // strides of batch, row and head in elements
+  int B, Lq, Lk, H, Hkv, dh;
+  float scale_log2;        // scale log2 e
+  const int32_t* k_len;    // [B], optional
+  const uint8_t* key_mask; // [B][Lk], optional
+  int32_t* key_list;       // [B][Lk] and key_count [B], with a mask
+  int32_t* key_count;
+  float* part;
+  int nsplit;
+};
+size_t cross_workspace_bytes(int bf16, int B, int Lq, int Lk, int H, int Hkv, int dh, bool masked);
+hipError_t launch_cross(int bf16, CrossArgs a, void* workspace, hipStream_t stream);
+
 }  // namespace echo

@@ -1,0 +1,234 @@
+"""GPU parity of the cross attention against a plain 64-bit computation on the
+CPU: head layouts, lengths from none to long, masks, strides, types.
+
+Bound of an output: with p the weights, the output's error is at most
+(2 e_p + e_s) sum p |v| plus half a step of its type, where e_p is the relative
+error of a weight (its rounding to bf16, 2^-8; fp32: the sums' n 2^-24) and e_s that
+of an exponential from the error of its score (a dot product of dh terms in
+fp32: dh 2^-24 |q| |k| scale, and a few steps of the exponent's argument)."""
+import math
+
+import pytest
+import torch
+
+from paper_2608_02474_amd import api
+
+from gpu_util import device, say
+
+pytestmark = pytest.mark.gpu
+
+U32 = 2.0 ** -24
+
+
+def _gen(seed):
+    g = torch.Generator(device="cpu")
+    g.manual_seed(seed)
+    return g
+
+
+def _oracle(q, k, v, left, scale):
+    """out and bound [B, Lq, H, dh] in 64 bits; left: bool [B, Lk]."""
+    B, Lq, H, dh = q.shape
+    G = H // k.shape[2]
+    out = torch.zeros(B, Lq, H, dh, dtype=torch.float64)
+    bound = torch.zeros_like(out)
+    bf = q.dtype == torch.bfloat16
+    for b in range(B):
+        at = left[b].nonzero()[:, 0]
+        if not len(at):
+            continue
+        for h in range(H):
+            kk, vv, qq = k[b, at, h // G].double(), v[b, at, h // G].double(), q[b, :, h].double()
+            s = qq @ kk.T * scale
+            p = torch.softmax(s, 1)
+            out[b, :, h] = p @ vv
+            reach = float(qq.norm(dim=1).max() * kk.norm(dim=1).max()) * scale
+            e_s = (dh + 8) * U32 * reach * 2
+            e_p = 2.0 ** -8 if bf else len(at) * U32 + 4 * U32
+            bound[b, :, h] = (2 * e_p * 1.02 + e_s) * (p @ vv.abs())
+    return out, bound + (2.0 ** -8 if bf else U32) * out.abs() + 1e-37
+
+
+def _check(got, q, k, v, left=None, scale=None, what=""):
+    B, Lk = k.shape[:2]
+    if left is None:
+        left = torch.ones(B, Lk, dtype=torch.bool)
+    want, bound = _oracle(q, k, v, left, q.shape[3] ** -0.5 if scale is None else scale)
+    off = (got.cpu().double() - want).abs()
+    worst = float((off / bound).max())
+    say(f"  {what}: worst error {worst:.3f} of its bound")
+    assert worst <= 1.0
+    empty = ~left.any(1)
+    assert (got.cpu()[empty] == 0).all()
+
+
+def _make(g, B, Lq, Lk, H, Hkv, dh, dtype):
+    r = lambda *s: torch.randn(*s, generator=g).to(dtype)  # noqa: E731
+    return r(B, Lq, H, dh), r(B, Lk, Hkv, dh), r(B, Lk, Hkv, dh)
+
+
+BF, F32 = torch.bfloat16, torch.float32
+SHAPES = [  # B, Lq, Lk, H, Hkv, dh, dtype
+    (1, 1, 1, 1, 1, 64, BF), (1, 1, 1, 1, 1, 128, BF), (2, 3, 5, 4, 2, 64, BF), (1, 33, 63, 2, 2, 128, BF),
+    (2, 32, 64, 3, 1, 128, BF), (1, 127, 65, 1, 1, 64, BF), (1, 129, 128, 2, 1, 128, BF), (3, 7, 129, 10, 2, 64, BF),
+    (2, 1, 700, 8, 1, 128, BF), (1, 1, 4099, 5, 5, 64, BF), (1, 40, 1500, 12, 12, 128, BF), (1, 300, 513, 4, 4, 128, BF),
+    (2, 257, 77, 6, 3, 64, BF), (1, 2000, 200, 2, 2, 128, BF), (40, 1, 300, 8, 8, 128, BF), (1, 1, 200, 200, 1, 128, BF),
+    (1, 1, 1, 1, 1, 4, F32), (2, 5, 3, 4, 2, 8, F32), (1, 32, 31, 2, 2, 32, F32), (1, 33, 33, 2, 1, 36, F32),
+    (2, 129, 65, 3, 3, 64, F32), (1, 1, 900, 8, 2, 100, F32), (1, 200, 300, 2, 1, 128, F32), (3, 2, 40, 5, 1, 12, F32),
+]
+
+
+@pytest.mark.parametrize("B,Lq,Lk,H,Hkv,dh,dtype", SHAPES)
+def test_cross_attention_shapes(B, Lq, Lk, H, Hkv, dh, dtype):
+    g = _gen(B + 3 * Lq + 5 * Lk + 7 * H + dh)
+    say(f"cross B={B} Lq={Lq} Lk={Lk} H={H}/{Hkv} dh={dh} {dtype}")
+    q, k, v = _make(g, B, Lq, Lk, H, Hkv, dh, dtype)
+    got = api.cross_attention(*(t.to(device()) for t in (q, k, v)))
+    torch.cuda.synchronize()
+    _check(got, q, k, v, what="full")
+
+
+@pytest.mark.parametrize("Lq", [1, 70])
+@pytest.mark.parametrize("dh,dtype", [(64, BF), (128, BF), (32, F32), (128, F32)])
+def test_cross_attention_lengths_and_masks(Lq, dh, dtype):
+    """Lengths of none, one, a tile's edges and beyond; a mask; both.  What lies in
+    masked states is NaN or infinite."""
+    B, Lk, H, Hkv = 8, 1100, 4, 2
+    g = _gen(dh + Lq)
+    lens = torch.tensor([0, 1, 63, 64, 65, 1100, 5000, -3], dtype=torch.int32)
+    mask = torch.rand(B, Lk, generator=g) < 0.4
+    mask[2] = False                                             # nothing left
+    mask[3, :60] = False                                        # a few of the last states of its length
+    q, k, v = _make(g, B, Lq, Lk, H, Hkv, dh, dtype)
+    inlen = torch.arange(Lk) < lens[:, None]
+    Q = q.to(device())
+    for use_len, use_mask in ((True, False), (False, True), (True, True)):
+        left = torch.ones(B, Lk, dtype=torch.bool)
+        if use_len:
+            left &= inlen
+        if use_mask:
+            left &= mask
+        kk, vv = k.clone(), v.clone()
+        kk[~left], vv[~left] = float("nan"), float("inf")
+        got = api.cross_attention(Q, kk.to(device()), vv.to(device()), k_len=lens.to(device()) if use_len else None,
+                                  key_mask=mask.to(device()) if use_mask else None)
+        torch.cuda.synchronize()
+        assert torch.isfinite(got).all()
+        _check(got, q, k, v, left, what=f"len {use_len} mask {use_mask}")
+        if use_mask:        # a mask of bytes, any value but 0
+            m8 = mask.to(torch.uint8) * 7
+            again = api.cross_attention(Q, kk.to(device()), vv.to(device()), key_mask=m8.to(device()),
+                                        k_len=lens.to(device()) if use_len else None)
+            assert torch.equal(again, got)
+
+
+@pytest.mark.parametrize("dtype,dh", [(BF, 128), (BF, 64), (F32, 32)])
+def test_cross_attention_layouts(dtype, dh):
+    """Heads in front of rows, keys and values of one product, states shared by all
+    elements (stride 0), an output inside a larger buffer whose rest is left."""
+    g = _gen(11)
+    B, Lq, Lk, H, Hkv = 3, 37, 90, 4, 2
+    q = torch.randn(B, H, Lq, dh, generator=g).to(dtype)
+    kv = torch.randn(1, Lk, 2, Hkv, dh, generator=g).to(dtype)
+    Q, KV = q.to(device()).transpose(1, 2), kv.to(device()).expand(B, -1, -1, -1, -1)
+    buf = torch.full((B, Lq + 3, H, dh), 9.0, dtype=dtype, device=device())
+    got = api.cross_attention(Q, KV[:, :, 0], KV[:, :, 1], scale=0.3, out=buf[:, 1:Lq + 1])
+    torch.cuda.synchronize()
+    kv = kv.expand(B, -1, -1, -1, -1)
+    _check(got, q.transpose(1, 2), kv[:, :, 0], kv[:, :, 1], scale=0.3, what="strided")
+    assert (buf[:, 0] == 9).all() and (buf[:, Lq + 1:] == 9).all()
+
+
+@pytest.mark.parametrize("dtype,dh", [(BF, 128), (F32, 64)])
+@pytest.mark.parametrize("Lq", [1, 150])
+def test_cross_attention_values_of_every_size(dtype, dh, Lq):
+    """Rising and huge scores move the running maximum; infinities and NaN of states
+    that are left spread as in the formula, in their own rows and columns only."""
+    g = _gen(23)
+    B, Lk, H = 1, 700, 2
+    q, k, v = _make(g, B, Lq, Lk, H, H, dh, dtype)
+    rise = k * torch.linspace(0.01, 30.0, Lk)[None, :, None, None].to(dtype)
+    got = api.cross_attention(q.to(device()), rise.to(device()), v.to(device()))
+    _check(got, q, rise, v, what="rising")
+    same = k[:, :1].expand(-1, Lk, -1, -1).contiguous()
+    got = api.cross_attention(q.to(device()), same.to(device()), v.to(device()))
+    _check(got, q, same, v, what="equal scores")
+    wide = v.clone()
+    wide[0, -1, 0, 5] = float("inf")                            # the last state of a ragged tile
+    wide[0, 3, 1, 7] = float("nan")
+    got = api.cross_attention(q.to(device()), k.to(device()), wide.to(device())).cpu()
+    assert (got[0, :, 0, 5] == float("inf")).all() and torch.isnan(got[0, :, 1, 7]).all()
+    rest = torch.ones(H, dh, dtype=torch.bool)
+    rest[0, 5] = rest[1, 7] = False
+    assert torch.isfinite(got[0, :, rest]).all()
+    bad = k.clone()
+    bad[0, 9, 1, 0] = float("nan")
+    got = api.cross_attention(q.to(device()), bad.to(device()), v.to(device())).cpu()
+    assert torch.isnan(got[0, :, 1]).all() and torch.isfinite(got[0, :, 0]).all()
+    low = torch.full_like(k, -float("inf"))                     # every score -inf: no weight at all
+    one = torch.ones_like(q)
+    got = api.cross_attention(one.to(device()), low.to(device()), v.to(device())).cpu()
+    assert (got == 0).all()
+
+
+def test_cross_attention_empty():
+    q = torch.randn(2, 3, 4, 64, device=device()).bfloat16()
+    none = q[:, :0, :2]
+    assert (api.cross_attention(q, none, none) == 0).all()
+    assert (api.cross_attention(q, none, none, key_mask=torch.zeros(2, 0, dtype=torch.bool, device=device())) == 0).all()
+    assert api.cross_attention(q[:, :0], q, q).shape == (2, 0, 4, 64)
+    assert api.cross_attention(q[:0], q[:0], q[:0]).shape == (0, 3, 4, 64)
+
+
+def test_cross_attention_long_states_pass_32_bits():
+    """One query over states whose last ones lie beyond 2^32 bytes from the first."""
+    Lk, Hkv, dh = 70000, 1, 128
+    row = 34000                                                  # elements between states: 70000 * 68 kB = 4.76 GB
+    kv = torch.empty(Lk * row, dtype=BF, device=device())
+    k = kv.as_strided((1, Lk, Hkv, dh), (Lk * row, row, dh, 1))
+    v = kv.as_strided((1, Lk, Hkv, dh), (Lk * row, row, dh, 1), storage_offset=dh)
+    g = torch.Generator(device=device())
+    g.manual_seed(2)
+    k.copy_(torch.randn(1, Lk, Hkv, dh, generator=g, device=device()))
+    v.copy_(torch.randn(1, Lk, Hkv, dh, generator=g, device=device()))
+    q = torch.randn(1, 1, 4, dh, generator=g, device=device()).to(BF)
+    mask = torch.zeros(1, Lk, dtype=torch.uint8, device=device())
+    mask[0, -300:] = 1
+    got = api.cross_attention(q, k, v)
+    some = api.cross_attention(q, k, v, key_mask=mask)
+    torch.cuda.synchronize()
+    kc, vc = k.cpu(), v.cpu()
+    _check(got, q.cpu(), kc, vc, what="all")
+    _check(some, q.cpu(), kc, vc, mask.cpu() != 0, what="the last 300")
+
+
+def test_cross_attention_streams_and_graphs():
+    """Captured calls (split over the states, masked) replayed between eager ones."""
+    g = _gen(9)
+    made = []
+    for B, Lq, Lk, H, Hkv, dh in ((2, 1, 2000, 8, 2, 128), (1, 300, 500, 4, 4, 64)):
+        q, k, v = (t.to(device()) for t in _make(g, B, Lq, Lk, H, Hkv, dh, BF))
+        n = torch.full((B,), Lk - 100, dtype=torch.int32, device=device())
+        m = (torch.rand(B, Lk, generator=g) < 0.5).to(device())
+        made.append((q, k, v, n, m))
+    ref = [api.cross_attention(q, k, v, k_len=n, key_mask=m) for q, k, v, n, m in made]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = [api.cross_attention(q, k, v, k_len=n, key_mask=m) for q, k, v, n, m in made]
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(ref, got))
+    graphs = []
+    for q, k, v, n, m in made:
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            y = api.cross_attention(q, k, v, k_len=n, key_mask=m)
+        graphs.append((gr, y))
+    for turn in range(3):
+        for (gr, y), (q, k, v, n, m) in zip(graphs, made):
+            q.mul_(-0.5)
+            n.sub_(37)
+            gr.replay()
+            want = api.cross_attention(q, k, v, k_len=n, key_mask=m)
+            torch.cuda.synchronize()
+            assert torch.equal(y, want), turn
