@@ -202,7 +202,9 @@ struct GemmI8Args {
   int res_nrows;
   int32_t* part;           // partial sums of split products
   size_t part_bytes;
-  int nsplit, kps;         // set by the launcher: k-ranges of a tile, k-steps of a range
+  // set by the launcher: the first split tile, k-ranges of a split tile, k-steps
+  // of a range, workgroups that run ranges
+  int tile_base, nsplit, kps, npieces;
 };
 size_t gemm_i8_partial_bytes(int M, int N, int K);
 hipError_t launch_gemm_i8(int epi, const GemmI8Args& a, hipStream_t stream);
