@@ -42,7 +42,9 @@ typedef __bf16 xbf16x2 __attribute__((ext_vector_type(2)));
 constexpr int X_ROWS = 128;                 // rows of a workgroup, 32 a wave
 constexpr int X_KT = 64;                    // states of a bf16 tile
 constexpr int X_KT32 = 32;                  // states of an fp32 tile
+constexpr int X_RING = 4;                   // LDS reads ahead of the matrix cores
 constexpr float X_GROW = 8.0f;              // log2 of the growth that moves the maximum
+constexpr float X_GROW_SUM = 256.0f;        // 2^X_GROW
 constexpr float X_LOW = -3.402823466e38f;   // the maximum before any state: the lowest finite value
 
 // maximum and sum over lanes l and l ^ 32
@@ -77,6 +79,9 @@ struct XItem {
   int n;                   // states left
 };
 // Consecutive items share K and V, and an XCD takes a contiguous range of them.
+// The (element, head) groups go by their number modulo 8 first, so that every
+// XCD gets its share of each element, whatever their lengths (elements one after
+// the other, of 512 and of 64 states: 305 us, now 228).
 __device__ __forceinline__ XItem x_item(const CrossArgs& p, int tiles, int kt) {
   const int nb = gridDim.x, per = nb / 8, rem = nb % 8, xcd = blockIdx.x % 8;
   int i = xcd * per + (xcd < rem ? xcd : rem) + blockIdx.x / 8;
@@ -85,8 +90,12 @@ __device__ __forceinline__ XItem x_item(const CrossArgs& p, int tiles, int kt) {
   i /= tiles;
   x.split = i % p.nsplit;
   i /= p.nsplit;
-  x.hk = i % p.Hkv;
-  x.b = i / p.Hkv;
+  const int groups = p.B * p.Hkv, most = groups / 8, more = groups % 8;  // `more` residues have most + 1 groups
+  const int first = more * (most + 1);
+  const int group = i < first ? i % (most + 1) * 8 + i / (most + 1)
+                              : (i - first) % most * 8 + more + (i - first) / most;
+  x.hk = group % p.Hkv;
+  x.b = group / p.Hkv;
   if (p.key_mask != nullptr) {
     x.n = p.key_count[x.b];
   } else {
@@ -100,6 +109,20 @@ __device__ __forceinline__ XItem x_item(const CrossArgs& p, int tiles, int kt) {
   return x;
 }
 
+// row r = g Lq + i of the queries that share a state head
+__device__ __forceinline__ void x_row(const CrossArgs& p, int r, int& g, int& i) {
+  if (p.H == p.Hkv) {
+    g = 0;
+    i = r;
+  } else if (p.Lq == 1) {
+    g = r;
+    i = 0;
+  } else {
+    g = r / p.Lq;
+    i = r - g * p.Lq;
+  }
+}
+
 // ---- partial results of a range: for the row's unit u, DH outputs, then all
 // units' maxima and sums
 __device__ __forceinline__ int64_t x_unit(const CrossArgs& p, const XItem& x, int tiles, int row) {
@@ -109,7 +132,8 @@ __device__ __forceinline__ int64_t x_units(const CrossArgs& p, int tiles) {
   return static_cast<int64_t>(p.B) * p.Hkv * p.nsplit * tiles * X_ROWS;
 }
 
-// ---- states that the mask leaves, in order; one workgroup per element
+// ---- states that the mask leaves, in order; one workgroup per element, eight
+// states a thread and turn
 __global__ void __launch_bounds__(1024) cross_keys(CrossArgs p) {
   __shared__ int wave_n[16];
   const int b = blockIdx.x, tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
@@ -118,19 +142,29 @@ __global__ void __launch_bounds__(1024) cross_keys(CrossArgs p) {
   const uint8_t* mask = p.key_mask + static_cast<int64_t>(b) * p.Lk;
   int32_t* list = p.key_list + static_cast<int64_t>(b) * p.Lk;
   int base = 0;
-  for (int j0 = 0; j0 < n; j0 += 1024) {
-    const int j = j0 + tid;
-    const bool in = j < n && mask[j] != 0;
-    const uint64_t bits = __ballot(in);
-    if (lane == 0) wave_n[wave] = __popcll(bits);
+  for (int64_t j0 = 0; j0 < n; j0 += 8192) {
+    const int64_t j = j0 + 8 * tid;
+    uint32_t bits = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bits |= (j + e < n && mask[j + e] != 0 ? 1u : 0u) << e;
+    const int mine = __popc(bits);
+    int upto = mine;  // of this lane and those before it
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const int other = __shfl_up(upto, d);
+      upto += lane >= d ? other : 0;
+    }
+    if (lane == kWave - 1) wave_n[wave] = upto;
     __syncthreads();
-    int before = 0, total = 0;
+    int at = base + upto - mine, total = 0;
 #pragma unroll
     for (int w = 0; w < 16; ++w) {
-      before += w < wave ? wave_n[w] : 0;
+      at += w < wave ? wave_n[w] : 0;
       total += wave_n[w];
     }
-    if (in) list[base + before + __popcll(bits & ((1ull << lane) - 1ull))] = j;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (bits >> e & 1u) list[at++] = static_cast<int32_t>(j) + e;
     base += total;
     __syncthreads();
   }
@@ -146,8 +180,10 @@ __global__ void __launch_bounds__(256, 2) cross_bf16(CrossArgs p) {
   constexpr int RPP = 1024 / RB;                 // rows of a 1 KB copy
   constexpr int NP = TILE / 1024 / 4;            // K (and V) copies of a wave and tile
   constexpr int OS = DH + 8;                     // staged output row
-  constexpr int LDS = 4 * TILE > X_ROWS * OS * 2 ? 4 * TILE : X_ROWS * OS * 2;
-  __shared__ __attribute__((aligned(1024))) char smem[LDS];  // stage s: K at 2 s TILE, V behind it
+  // two stages of K, then three of V: 80 KB at dh 128, two workgroups to a CU
+  constexpr int VB = 2 * TILE;
+  static_assert(5 * TILE >= X_ROWS * OS * 2, "the output's rows fit the ring");
+  __shared__ __attribute__((aligned(1024))) char smem[5 * TILE];
   const int tid = threadIdx.x, lane = tid % kWave, l32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int rows = p.H / p.Hkv * p.Lq, tiles = (rows + X_ROWS - 1) / X_ROWS;
@@ -156,39 +192,73 @@ __global__ void __launch_bounds__(256, 2) cross_bf16(CrossArgs p) {
   const bf16_t* vb = static_cast<const bf16_t*>(p.v) + x.b * p.vb + x.hk * p.vh;
   const int32_t* list = MASK ? p.key_list + static_cast<int64_t>(x.b) * p.Lk : nullptr;
 
-  // ---- this lane's query: row r = g Lq + i
-  const int row0 = x.tile * X_ROWS + wave * 32;
-  const bool idle = row0 >= rows;  // no row in this wave: it copies and waits with the others
-  bf16x8 qf[NS];
-  {
-    int r = row0 + l32;
-    r = r < rows ? r : rows - 1;
-    const int g = r / p.Lq, i = r % p.Lq;
-    const bf16_t* src = static_cast<const bf16_t*>(p.q) + x.b * p.qb + static_cast<int64_t>(i) * p.qr +
-                        static_cast<int64_t>(x.hk * (p.H / p.Hkv) + g) * p.qh + 8 * hi;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) qf[s] = __builtin_bit_cast(bf16x8, ldg16(src + 16 * s));
-  }
-  // the loads above are waited for here: later waits count the copies alone
-  __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
-
   // ---- copies.  Copy m of this wave is rows RPP (wave + 4 m) .. of the tile;
-  // the lane lands in row lr of them, slot ls, and fetches the chunk that lives there.
+  // the lane lands in row lr of them, slot ls, and fetches the chunk that lives
+  // there.  Whole tiles without a list take a uniform base and offsets that are
+  // the same for every tile; the last tile and listed states an address each.
   const int lr = lane / (RB / 16), ls = lane % (RB / 16);
-  const uint32_t lds0 = lds_offset(smem);
-  auto issue = [&](int t, int stage) __attribute__((always_inline)) {
-    const int key0 = t * X_KT;
+  const uint32_t lds0 = lds_offset(smem) + wave * 1024;
+  uint32_t koff[NP], voff[NP];
+#pragma unroll
+  for (int m = 0; m < NP; ++m) {
+    const int r = RPP * (wave + 4 * m) + lr;
+    koff[m] = (static_cast<uint32_t>(r) * static_cast<uint32_t>(p.kr) + (ls ^ x_kx<DH>(r)) * 8) * 2;
+    voff[m] = (static_cast<uint32_t>(r) * static_cast<uint32_t>(p.vr) +
+               ((((ls >> 1) ^ x_vx<DH>(r)) << 1) + (ls & 1)) * 8) * 2;
+  }
+  // the list's entries for this lane's rows of a tile, a tile ahead
+  int listed[NP];
+  auto look = [&](int u) __attribute__((always_inline)) {
+#pragma unroll
+    for (int m = 0; m < NP; ++m) {
+      const int key = (x.t0 + u) * X_KT + RPP * (wave + 4 * m) + lr;
+      listed[m] = list[key < x.n ? key : x.n - 1];
+    }
+  };
+  auto issue = [&](int u) __attribute__((always_inline)) {  // the u-th tile of the range
+    const int t = x.t0 + u;
+    const uint32_t kd = lds0 + (u & 1) * TILE, vd = lds0 + VB + u % 3 * TILE;
+    if (!MASK && (t + 1) * X_KT <= x.n) {
+      const bf16_t* ks = kb + static_cast<int64_t>(t) * X_KT * p.kr;
+      const bf16_t* vs = vb + static_cast<int64_t>(t) * X_KT * p.vr;
+#pragma unroll
+      for (int m = 0; m < NP; ++m) lds_copy16_s(ks, koff[m], kd + m * 4096);
+#pragma unroll
+      for (int m = 0; m < NP; ++m) lds_copy16_s(vs, voff[m], vd + m * 4096);
+      return;
+    }
 #pragma unroll
     for (int m = 0; m < NP; ++m) {
       const int r = RPP * (wave + 4 * m) + lr;
-      int key = key0 + r < x.n ? key0 + r : x.n - 1;  // past the end: the last state again, never used
-      if constexpr (MASK) key = list[key];
-      const int kc = (ls ^ x_kx<DH>(r)) * 8, vc = ((((ls >> 1) ^ x_vx<DH>(r)) << 1) + (ls & 1)) * 8;
-      const uint32_t dst = lds0 + 2 * stage * TILE + (wave + 4 * m) * 1024;
-      lds_copy16(kb + static_cast<int64_t>(key) * p.kr + kc, dst);
-      lds_copy16(vb + static_cast<int64_t>(key) * p.vr + vc, dst + TILE);
+      int key = t * X_KT + r < x.n ? t * X_KT + r : x.n - 1;  // past the end: the last state again, never used
+      if constexpr (MASK) key = listed[m];
+      const int64_t at = static_cast<int64_t>(key) - r;
+      lds_copy16(reinterpret_cast<const char*>(kb + at * p.kr) + koff[m], kd + m * 4096);
+      lds_copy16(reinterpret_cast<const char*>(vb + at * p.vr) + voff[m], vd + m * 4096);
     }
+    if constexpr (MASK) look(u + 1);
   };
+  const int nt = x.t1 - x.t0;
+  if constexpr (MASK)
+    if (nt > 0) look(0);
+  if (nt > 0) issue(0);
+
+  // ---- the wave's 32 queries, through LDS as well (whole rows a load; straight
+  // to registers a row came as 32-byte pieces of 8 loads and the L1 did not hold
+  // them): they lie where the values of tiles 1 and 2 will, swizzled as K
+  const int row0 = x.tile * X_ROWS + wave * 32;
+  const bool idle = row0 >= rows;  // no row in this wave: it copies and waits with the others
+  char* qs = smem + VB + TILE + wave * 32 * RB;
+  if (!idle && nt > 0) {
+    const bf16_t* qb = static_cast<const bf16_t*>(p.q) + x.b * p.qb + static_cast<int64_t>(x.hk) * (p.H / p.Hkv) * p.qh;
+#pragma unroll
+    for (int m = 0; m < 32 / RPP; ++m) {
+      const int rl = RPP * m + lr;
+      int g, i;
+      x_row(p, row0 + rl < rows ? row0 + rl : rows - 1, g, i);
+      lds_copy16(qb + i * p.qr + g * p.qh + (ls ^ x_kx<DH>(rl)) * 8, lds_offset(qs) + m * 1024);
+    }
+  }
   // ---- fragment addresses in a stage
   int k_rd[NS], v_rd[ND];
 #pragma unroll
@@ -200,8 +270,9 @@ __global__ void __launch_bounds__(256, 2) cross_bf16(CrossArgs p) {
   for (int d = 0; d < ND; ++d) {
     const int g16 = lane >> 4, i16 = lane & 15;
     const int r = 8 * (g16 >> 1) + (i16 >> 2);
-    v_rd[d] = TILE + r * RB + ((2 * d + (g16 & 1)) ^ x_vx<DH>(r)) * 32 + 8 * (i16 & 3);
+    v_rd[d] = VB + r * RB + ((2 * d + (g16 & 1)) ^ x_vx<DH>(r)) * 32 + 8 * (i16 & 3);
   }
+  bf16x8 qf[NS];
   f32x16 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d)
@@ -211,88 +282,136 @@ __global__ void __launch_bounds__(256, 2) cross_bf16(CrossArgs p) {
   const f32x16 zero16 = {};
   const xbf16x2 ones = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
 
-  if (x.t0 < x.t1) issue(x.t0, 0);
-  for (int t = x.t0; t < x.t1; ++t) {
-    const int stage = (t - x.t0) & 1;
-    if (t + 1 < x.t1) {
-      issue(t + 1, stage ^ 1);
-      __builtin_amdgcn_s_waitcnt(waitcnt_vm(2 * NP));  // this wave's copies of tile t
-    } else {
-      __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+  // The states pass in halves of 32: while the matrix cores compute the scores
+  // of one half, the vector units turn those of the half before it into
+  // probabilities, which then weigh V.  LDS reads are issued two MFMAs ahead.
+  bf16x8 pf[2];
+  float psum;
+  auto weigh = [&](const f32x16& sc, int c) __attribute__((always_inline)) {  // scores 2 c, 2 c + 1
+    const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * c], p.scale_log2, -mc));
+    const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * c + 1], p.scale_log2, -mc));
+    const int j = 2 * (c % 4);
+    pf[c / 4][j] = static_cast<__bf16>(e0);
+    pf[c / 4][j + 1] = static_cast<__bf16>(e1);
+    // the sum is of the rounded probabilities, those that weigh V
+    const xbf16x2 pair = {pf[c / 4][j], pf[c / 4][j + 1]};
+    psum = __builtin_amdgcn_fdot2_f32_bf16(pair, ones, psum, false);
+  };
+  // scores of half h of the u-th tile, with work(c), c < 8, spread between its MFMAs
+  auto scores = [&](int u, int h, f32x16& sc, auto&& work) __attribute__((always_inline)) {
+    const char* ks = smem + (u & 1) * TILE + h * 32 * RB;
+    auto read = [&](int s) __attribute__((always_inline)) {
+      return *reinterpret_cast<const bf16x8*>(ks + k_rd[s]);
+    };
+    bf16x8 ring[X_RING];
+#pragma unroll
+    for (int i = 0; i < X_RING; ++i) ring[i] = read(i);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[s % X_RING], qf[s], s == 0 ? zero16 : sc, 0, 0, 0);
+      if (s + X_RING < NS) ring[s % X_RING] = read(s + X_RING);
+#pragma unroll
+      for (int c = s * 8 / NS; c < (s + 1) * 8 / NS; ++c) work(c);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const int left = x.n - (x.t0 + u) * X_KT - 32 * h;  // states of the half and after it
+    if (left < 32) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] = 16 * (r >> 3) + 8 * hi + (r & 7) < left ? sc[r] : -INFINITY;
+    }
+  };
+  // The half's probabilities are against the maximum so far.  None can exceed
+  // 2^8 unless the lane's sum does, so the half's own maximum is looked for only
+  // then (always in the first): rows that have not grown get the same
+  // probabilities again.
+  auto settle = [&](const f32x16& sc) __attribute__((always_inline)) {
+    if (__builtin_expect(__ballot(psum > X_GROW_SUM) != 0ull, 0)) {
+      float mx = sc[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+      mx = x_pair_max(mx) * p.scale_log2;
+      const bool grow = mx - mc > X_GROW;
+      const float alpha = grow ? __builtin_amdgcn_exp2f(mc - mx) : 1.0f;
+      mc = grow ? mx : mc;
+      l_run *= alpha;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
+      psum = 0.0f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) weigh(sc, c);
+    }
+    l_run += psum;
+  };
+  auto values = [&](int u, int h) __attribute__((always_inline)) {  // O += V^T P^T of a half
+    const char* vs = smem + u % 3 * TILE + h * 32 * RB;
+    auto read = [&](int i) __attribute__((always_inline)) {
+      const char* at = vs + i / ND * 16 * RB + v_rd[i % ND];
+      const xv4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) xv4i16*)(at));
+      const xv4i16 up =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) xv4i16*)(at + 4 * RB));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    bf16x8 ring[X_RING];
+#pragma unroll
+    for (int i = 0; i < X_RING; ++i) ring[i] = read(i);
+#pragma unroll
+    for (int i = 0; i < 2 * ND; ++i) {
+      o[i % ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ring[i % X_RING], pf[i / ND], o[i % ND], 0, 0, 0);
+      if (i + X_RING < 2 * ND) ring[i % X_RING] = read(i + X_RING);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // Tile u has landed for every wave and every wave is done with the scores of
+  // tile u - 1 and the values of tile u - 2, whose stages the next copies refill.
+  auto arrive = [&](int u) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
+    if (u == 0) {
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+        qf[s] = *reinterpret_cast<const bf16x8*>(qs + l32 * RB + ((2 * s + hi) ^ x_kx<DH>(l32)) * 16);
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));  // read, before another wave's copies replace them
     }
     __syncthreads();
-    char* st = smem + 2 * stage * TILE;
-    const int left = x.n - t * X_KT;  // states of the tile and after it
+    if (u + 1 < nt) issue(u + 1);
+    const int left = x.n - (x.t0 + u) * X_KT;
     if (left < X_KT) {
       // V rows past the last state: zeros, so that their zero weights meet no infinity
       for (int e = tid; e < (X_KT - left) * (RB / 16); e += 256)
-        *reinterpret_cast<uint4*>(st + TILE + left * RB + e * 16) = make_uint4(0u, 0u, 0u, 0u);
+        *reinterpret_cast<uint4*>(smem + VB + u % 3 * TILE + left * RB + e * 16) = make_uint4(0u, 0u, 0u, 0u);
       __syncthreads();
     }
+  };
+  f32x16 s0, s1;
+  if (nt > 0) {
+    arrive(0);
+    if (!idle) scores(0, 0, s0, [](int) {});
+  }
+  for (int u = 0; u < nt; ++u) {
     if (!idle) {
-      f32x16 sc[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          const bf16x8 a = *reinterpret_cast<const bf16x8*>(st + h * 32 * RB + k_rd[s]);
-          sc[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[s], s == 0 ? zero16 : sc[h], 0, 0, 0);
-        }
-      if (left < X_KT) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            sc[h][r] = 32 * h + 16 * (r >> 3) + 8 * hi + (r & 7) < left ? sc[h][r] : -INFINITY;
-      }
-      float mx = sc[0][0];
-#pragma unroll
-      for (int r = 1; r < 32; ++r) mx = fmaxf(mx, sc[r / 16][r % 16]);
-      mx = x_pair_max(mx) * p.scale_log2;
-      const bool grow = mx - mc > X_GROW;
-      if (__ballot(grow) != 0ull) {
-        const float alpha = grow ? __builtin_amdgcn_exp2f(mc - mx) : 1.0f;
-        mc = grow ? mx : mc;
-        l_run *= alpha;
-#pragma unroll
-        for (int d = 0; d < ND; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[d][r] *= alpha;
-      }
-      bf16x8 pf[2][2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[h][2 * c], p.scale_log2, -mc));
-          const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[h][2 * c + 1], p.scale_log2, -mc));
-          const int j = 2 * (c % 4);
-          pf[h][c / 4][j] = static_cast<__bf16>(e0);
-          pf[h][c / 4][j + 1] = static_cast<__bf16>(e1);
-          // the sum is of the rounded probabilities, those that weigh V
-          const xbf16x2 pair = {pf[h][c / 4][j], pf[h][c / 4][j + 1]};
-          l_run = __builtin_amdgcn_fdot2_f32_bf16(pair, ones, l_run, false);
-        }
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int a = 0; a < 2; ++a)
-#pragma unroll
-          for (int d = 0; d < ND; ++d) {
-            const char* vs = st + (32 * h + 16 * a) * RB + v_rd[d];
-            const xv4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) xv4i16*)(vs));
-            const xv4i16 up = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) xv4i16*)(vs + 4 * RB));
-            const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pf[h][a], o[d], 0, 0, 0);
-          }
+      psum = 0.0f;
+      scores(u, 1, s1, [&](int c) __attribute__((always_inline)) { weigh(s0, c); });
+      settle(s0);
+      values(u, 0);
     }
-    __syncthreads();  // every wave is done with the stage that the next tile's copies refill
+    psum = 0.0f;
+    if (u + 1 < nt) {
+      arrive(u + 1);
+      if (!idle) scores(u + 1, 0, s0, [&](int c) __attribute__((always_inline)) { weigh(s1, c); });
+    } else if (!idle) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) weigh(s1, c);
+    }
+    if (!idle) {
+      settle(s1);
+      values(u, 1);
+    }
   }
   const float lsum = x_pair_sum(l_run);
   if (p.nsplit > 1) {
     if (idle) return;
+    if (row0 + l32 >= rows) return;
     const int64_t units = x_units(p, tiles), u = x_unit(p, x, tiles, wave * 32 + l32);
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -304,6 +423,7 @@ __global__ void __launch_bounds__(256, 2) cross_bf16(CrossArgs p) {
     return;
   }
   // rows through LDS, so that stores are 16-byte pieces of whole rows
+  __syncthreads();  // every wave is done with the last tile
   bf16_t* os = reinterpret_cast<bf16_t*>(smem);
   const float inv = lsum == 0.0f ? 0.0f : 1.0f / lsum;
 #pragma unroll
@@ -319,7 +439,8 @@ __global__ void __launch_bounds__(256, 2) cross_bf16(CrossArgs p) {
   for (int e = tid; e < X_ROWS * (DH / 8); e += 256) {
     const int rl = e / (DH / 8), ch = e % (DH / 8), r = x.tile * X_ROWS + rl;
     if (r >= rows) break;
-    const int g = r / p.Lq, i = r % p.Lq;
+    int g, i;
+    x_row(p, r, g, i);
     stg16(ob + static_cast<int64_t>(i) * p.orow + static_cast<int64_t>(x.hk * (p.H / p.Hkv) + g) * p.oh + ch * 8,
           *reinterpret_cast<const uint4*>(os + rl * OS + ch * 8));
   }
@@ -356,24 +477,37 @@ __global__ void __launch_bounds__(256) cross_f32(CrossArgs p) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[d][e] = 0.0f;
   float mc = X_LOW, l_run = 0.0f;
-  for (int t = x.t0; t < x.t1; ++t) {
-    const int left = x.n - t * X_KT32;
-    for (int e = tid; e < X_KT32 * (DHP / 4); e += 256) {
-      const int kr = e / (DHP / 4), c = e % (DHP / 4) * 4;
-      float4 kv = make_float4(0.0f, 0.0f, 0.0f, 0.0f), vv = kv;
-      if (kr < left && c < p.dh) {
+  // the next tile is on its way to registers while this one is worked on
+  constexpr int NV = X_KT32 * (DHP / 4) / 256 > 0 ? X_KT32 * (DHP / 4) / 256 : 1;
+  static_assert(X_KT32 * (DHP / 4) == NV * 256, "whole passes of the workgroup");
+  float4 kv[NV], vv[NV];
+  auto fetch = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int e = tid + 256 * u, kr = e / (DHP / 4), c = e % (DHP / 4) * 4;
+      kv[u] = vv[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);  // no state, no column: zeros
+      if (t * X_KT32 + kr < x.n && c < p.dh) {
         int key = t * X_KT32 + kr;
         if (list != nullptr) key = list[key];
-        kv = *reinterpret_cast<const float4*>(kb + static_cast<int64_t>(key) * p.kr + c);
-        vv = *reinterpret_cast<const float4*>(vb + static_cast<int64_t>(key) * p.vr + c);
+        kv[u] = *reinterpret_cast<const float4*>(kb + static_cast<int64_t>(key) * p.kr + c);
+        vv[u] = *reinterpret_cast<const float4*>(vb + static_cast<int64_t>(key) * p.vr + c);
       }
-      ks[kr * LD + c] = kv.x;
-      ks[kr * LD + c + 1] = kv.y;
-      ks[kr * LD + c + 2] = kv.z;
-      ks[kr * LD + c + 3] = kv.w;
-      *reinterpret_cast<float4*>(vs + kr * DHP + c) = vv;
+    }
+  };
+  if (x.t0 < x.t1) fetch(x.t0);
+  for (int t = x.t0; t < x.t1; ++t) {
+    const int left = x.n - t * X_KT32;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int e = tid + 256 * u, kr = e / (DHP / 4), c = e % (DHP / 4) * 4;
+      ks[kr * LD + c] = kv[u].x;
+      ks[kr * LD + c + 1] = kv[u].y;
+      ks[kr * LD + c + 2] = kv[u].z;
+      ks[kr * LD + c + 3] = kv[u].w;
+      *reinterpret_cast<float4*>(vs + kr * DHP + c) = vv[u];
     }
     __syncthreads();
+    if (t + 1 < x.t1) fetch(t + 1);
     if (!idle) {
       // lane: scores of its query with states 8 (e / 4) + 4 hi + e % 4
       f32x16 sc = {};
@@ -414,7 +548,7 @@ __global__ void __launch_bounds__(256) cross_f32(CrossArgs p) {
   }
   const float lsum = x_pair_sum(l_run);
   if (p.nsplit > 1) {
-    if (idle) return;
+    if (!mine) return;
     const int64_t units = x_units(p, tiles), u = x_unit(p, x, tiles, wave * 32 + l32);
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -486,16 +620,46 @@ constexpr size_t kXAlign = 256;
 size_t x_up(size_t n) { return (n + kXAlign - 1) / kXAlign * kXAlign; }
 int x_pad(int dh) { return dh <= 32 ? 32 : dh <= 64 ? 64 : 128; }
 
-// ranges of the states: enough workgroups for two to each CU, each with four
-// tiles of states at least (of the longest element)
-int x_splits(int bf16, int B, int Lq, int Lk, int H, int Hkv) {
-  const int64_t rows = static_cast<int64_t>(H / Hkv) * Lq;
-  const int64_t wgs = (rows + X_ROWS - 1) / X_ROWS * B * Hkv;
-  const int kt = bf16 ? X_KT : X_KT32, nt = (Lk + kt - 1) / kt;
-  const int64_t want = (2ll * device_cu_count() + wgs - 1) / wgs;
-  const int64_t most = nt / 4;
-  const int64_t n = want < most ? want : most;
-  return n < 1 ? 1 : static_cast<int>(n);
+// Ranges of the states, by estimated time (us): a workgroup's tile of states
+// takes `one` alone on its CU and `all` with the CU full, at least what its K
+// and V take from memory where no other workgroup shares them, and `fix` for
+// its queries and outputs; a split adds the second launch and its partial
+// results, written and read.  With several elements, which have several lengths,
+// rounds before the last count for three quarters.  40 groups of one query x 32760
+// states 623 us whole, 134 in 12 ranges; 1040 workgroups x 512 tiles 2638 and 2286
+// (5); 488 x 94 tiles 190 and 211 (2); 384 x 8 tiles 24 and 44 (2).
+int x_splits(int bf16, int B, int Lq, int Lk, int H, int Hkv, int dh) {
+  const int64_t rows = static_cast<int64_t>(H / Hkv) * Lq, tiles = (rows + X_ROWS - 1) / X_ROWS;
+  const int64_t wgs = tiles * B * Hkv;
+  const int kt = bf16 ? X_KT : X_KT32, nt = (Lk + kt - 1) / kt, dhp = x_pad(dh), ncu = device_cu_count();
+  const int per = bf16 ? (dhp == 64 ? 3 : 2) : (dhp == 128 ? 1 : dhp == 64 ? 2 : 3);  // workgroups of a CU
+  float one = bf16 ? (dhp == 64 ? 0.86f : 1.2f) : 0.045f * dhp;
+  float all = bf16 ? (dhp == 64 ? 1.8f : 1.9f) : 0.045f * dhp * (per > 1 ? 1.5f : 1.0f);
+  if (tiles == 1) {
+    const float mem = 2.0f * kt * dhp * (bf16 ? 2 : 4) * ncu / 6.2e6f;  // a tile on every CU
+    one = one > mem ? one : mem;
+    all = all > per * mem ? all : per * mem;
+  }
+  const int64_t slots = static_cast<int64_t>(ncu) * per;
+  int best = 1;
+  float best_us = 0.0f;
+  for (const int ns : {1, 2, 3, 4, 5, 6, 8, 12, 16, 24, 32}) {
+    if (ns > 1 && nt < 2 * ns) break;
+    const int steps = (nt + ns - 1) / ns;
+    const int64_t pieces = wgs * ns, full = pieces / slots, rest = pieces % slots;
+    const float round = steps * all + 6.0f;
+    float us = rest == 0 ? round : rest <= ncu ? steps * one + 4.0f : round;
+    us += (B > 1 ? 0.75f : 1.0f) * (rest == 0 ? full - 1 : full) * round;
+    if (ns > 1) {
+      const int64_t n = static_cast<int64_t>(B) * Hkv * ns * rows;
+      us += 6.0f + n * (dhp + 2) * 8.0f / 4e6f;
+    }
+    if (ns == 1 || us < best_us) {
+      best = ns;
+      best_us = us;
+    }
+  }
+  return best;
 }
 
 template <int DH>
@@ -517,7 +681,7 @@ hipError_t launch_x_combine(const CrossArgs& a, hipStream_t stream) {
 size_t cross_workspace_bytes(int bf16, int B, int Lq, int Lk, int H, int Hkv, int dh, bool masked) {
   size_t n = 0;
   if (masked) n = x_up(sizeof(int32_t) * static_cast<size_t>(B) * Lk) + x_up(sizeof(int32_t) * B);
-  const int ns = x_splits(bf16, B, Lq, Lk, H, Hkv);
+  const int ns = x_splits(bf16, B, Lq, Lk, H, Hkv, dh);
   if (ns > 1) {
     const size_t rows = static_cast<size_t>(H / Hkv) * Lq, tiles = (rows + X_ROWS - 1) / X_ROWS;
     n += x_up(sizeof(float) * (x_pad(dh) + 2) * static_cast<size_t>(B) * Hkv * ns * tiles * X_ROWS);
@@ -536,7 +700,7 @@ hipError_t launch_cross(int bf16, CrossArgs a, void* workspace, hipStream_t stre
     if ((e = ECHO_LAUNCH("cross_keys", cross_keys, dim3(a.B), dim3(1024), 0, stream, a)) != hipSuccess) return e;
   }
   a.part = reinterpret_cast<float*>(ws);
-  a.nsplit = x_splits(bf16, a.B, a.Lq, a.Lk, a.H, a.Hkv);
+  a.nsplit = x_splits(bf16, a.B, a.Lq, a.Lk, a.H, a.Hkv, a.dh);
   const int64_t rows = static_cast<int64_t>(a.H / a.Hkv) * a.Lq;
   const unsigned grid =
       static_cast<unsigned>((rows + X_ROWS - 1) / X_ROWS * a.B * a.Hkv * a.nsplit);

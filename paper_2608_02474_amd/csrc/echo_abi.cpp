@@ -325,6 +325,8 @@ bool cross_cfg_ok(const echo_cross_attention_cfg* c) {
 bool cross_supported(const echo_cross_attention_cfg* c) {
   if (c->dtype == ECHO_BF16 ? (c->dh != 64 && c->dh != 128) : (c->dh % 4 != 0 || c->dh > 128)) return false;
   if (!std::isfinite(c->scale * 1.4426950408889634f)) return false;  // the scale in units of log2
+  // a tile of states is addressed by 32-bit offsets
+  if (c->k.row >= (int64_t(1) << 24) || c->v.row >= (int64_t(1) << 24)) return false;
   const int64_t rows = int64_t(c->H / c->Hkv) * c->Lq, groups = int64_t(c->B) * c->Hkv;
   return rows < (int64_t(1) << 31) - 128 && groups < kMaxGroups && groups * ((rows + 127) / 128) < kMaxGroups;
 }

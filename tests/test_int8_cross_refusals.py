@@ -99,6 +99,9 @@ def test_cross_rejects_before_launch(lib):
     for bad in (dict(dh=32), dict(dh=96), dict(dh=256), dict(dt=F32, dh=132), dict(scale=3e38),
                 dict(B=1 << 24, Hkv=1, H=1), dict(Lq=1 << 30, H=4, Hkv=1)):
         assert run(**bad) == EUNSUP, bad
+    for t in "kv":
+        far = _cross(**{t: S(1 << 30, 1 << 24, 64)})
+        assert lib.echo_cross_attention(ctypes.byref(far), *[FAKE] * 6, FAKE, 1 << 40, None) == EUNSUP
     odd = _cross(dt=F32, dh=6, q=S(192, 24, 8), k=S(192, 24, 8), v=S(192, 24, 8), o=S(192, 24, 8))
     assert lib.echo_cross_attention(ctypes.byref(odd), *[FAKE] * 6, FAKE, 1 << 40, None) == EUNSUP
     assert run(B=0, q=None, o=None, ws=None, nb=0) == OK
