@@ -26,7 +26,7 @@ import torch
 
 from . import _lib
 from ._lib import (BlockCfg, BlockWeights, CacheCfg, CrossAttentionCfg, EnergyCfg, KernelTime, LinearInt8Cfg,
-                   QuantizeCfg, RefCacheCfg, Strides, WanBlockCfg, WanBlockWeights,
+                   QuantizeCfg, RefCacheCfg, WanBlockCfg, WanBlockWeights,
                    RefCacheState, ScheduleCfg, ScheduleState, SelectCfg,
                    ECHO_BF16, ECHO_F32, check)
 
@@ -696,32 +696,39 @@ class Int8Rows:
         return self.codes.shape[0]
 
 
-def _here(first: torch.Tensor, **others) -> None:
-    """Every tensor on the current device: the kernels run on its current stream."""
-    if first.get_device() != torch.cuda.current_device():
+# A small call is bound by the host here too: the helpers below take a tensor's
+# shape and strides once, and say what is wrong only after something is.
+
+def _here(dev: int, *others) -> int:
+    """The stream of the current device, which has to be that of every tensor:
+    `dev` the first one's, (name, tensor or None) the others'."""
+    if dev != torch.cuda.current_device():
         raise ValueError("tensors must be on the current device")
-    for name, t in others.items():
-        if t is not None and t.get_device() != first.get_device():
+    for name, t in others:
+        if t is not None and t.get_device() != dev:
             raise ValueError(f"{name} must be on the same device as the other tensors")
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(dev)
 
 
-def _rows_of(t: torch.Tensor, name: str, dtype=None) -> torch.Tensor:
-    """A [rows, columns] device tensor whose columns are contiguous (rows may lie apart)."""
+def _rows_of(t: torch.Tensor, name: str, dtype=None) -> tuple:
+    """(rows, columns, elements between rows) of a [rows, columns] device tensor
+    whose columns are contiguous (rows may lie apart)."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 2 or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be [rows, columns] with contiguous columns")
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
-        raise ValueError(f"{name} must not have overlapping rows")
-    return t
-
-
-def _ld(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if t.dim() == 2:
+        n, d = t.shape
+        s, u = t.stride()
+        if d >= 1 and (u == 1 or d == 1):
+            if n <= 1:
+                return n, d, d
+            if s >= d:
+                return n, d, s
+            raise ValueError(f"{name} must not have overlapping rows")
+    raise ValueError(f"{name} must be [rows, columns] with contiguous columns")
 
 
 def _vector(t: torch.Tensor, name: str, n: int, dtype=None) -> torch.Tensor:
@@ -731,15 +738,16 @@ def _vector(t: torch.Tensor, name: str, n: int, dtype=None) -> torch.Tensor:
     return t
 
 
-def _int8_rows(r: Int8Rows, name: str) -> Int8Rows:
+def _int8_rows(r: Int8Rows, name: str) -> tuple:
+    """(rows, pitch) of checked 8-bit rows."""
     if not isinstance(r, Int8Rows):
         raise TypeError(f"{name} must be Int8Rows (see quantize_rows)")
-    _rows_of(r.codes, f"{name}.codes", torch.int8)
-    _vector(r.scale, f"{name}.scale", r.codes.shape[0], torch.float32)
-    pitch = _lib_handle().echo_int8_pitch(int(r.cols))
-    if pitch == 0 or r.codes.shape[1] < pitch or r.codes.shape[1] % 128 or _ld(r.codes) % 128:
+    n, width, ld = _rows_of(r.codes, f"{name}.codes", torch.int8)
+    _vector(r.scale, f"{name}.scale", n, torch.float32)
+    pitch = (r.cols + 127) // 128 * 128
+    if not 1 <= r.cols <= 65536 or width < pitch or ld % 128 or width % 128:
         raise ValueError(f"{name}.codes must have a pitch of {pitch} bytes or a larger multiple of 128")
-    return r
+    return n, ld
 
 
 def quantize_rows(x: torch.Tensor, rows: torch.Tensor | None = None, shift: torch.Tensor | None = None,
@@ -750,8 +758,7 @@ def quantize_rows(x: torch.Tensor, rows: torch.Tensor | None = None, shift: torc
     [D]) put a modulated LayerNorm in front.  Quantizes a weight matrix
     [channels, inputs] as well as tokens."""
     lib = _lib_handle()
-    _rows_of(x, "x")
-    n, D = x.shape
+    n, D, ldx = _rows_of(x, "x")
     M = n
     if rows is not None:
         M = _dev(rows, "rows", torch.int32).numel()
@@ -764,35 +771,43 @@ def quantize_rows(x: torch.Tensor, rows: torch.Tensor | None = None, shift: torc
     if shift is not None:
         _vector(shift, "shift", D, torch.float32)
         _vector(scale, "scale", D, torch.float32)
-    pitch = lib.echo_int8_pitch(D)
-    if pitch == 0:
+    if D > 65536:
         raise ValueError("rows of at most 65536 columns")
     if out is None:
-        out = Int8Rows(torch.empty((M, pitch), dtype=torch.int8, device=x.device),
-                       torch.empty(M, dtype=torch.float32, device=x.device), D)
-    elif len(_int8_rows(out, "out")) != M or out.cols != D:
-        raise ValueError(f"out must hold {M} rows of {D} columns")
-    _here(x, rows=rows, shift=shift, scale=scale, codes=out.codes, row_scale=out.scale)
-    cfg = QuantizeCfg(M, D, _echo_dtype(x), n, _ld(x), _ld(out.codes), float(ln_eps))
-    check("echo_quantize_rows",
-          lib.echo_quantize_rows(ctypes.byref(cfg), _ptr(x), _ptr(rows), _ptr(shift), _ptr(scale),
-                                 _ptr(out.codes), _ptr(out.scale), _stream()))
+        ldq = (D + 127) // 128 * 128
+        out = Int8Rows(x.new_empty((M, ldq), dtype=torch.int8), x.new_empty(M, dtype=torch.float32), D)
+    else:
+        m, ldq = _int8_rows(out, "out")
+        if m != M or out.cols != D:
+            raise ValueError(f"out must hold {M} rows of {D} columns")
+        if out.codes.shape[1] != ldq:
+            raise ValueError("out.codes must have rows of whole pitches")
+    stream = _here(x.get_device(), ("rows", rows), ("shift", shift), ("scale", scale), ("out.codes", out.codes),
+                   ("out.scale", out.scale))
+    cfg = QuantizeCfg(M, D, _echo_dtype(x), n, ldx, ldq, ln_eps)
+    st = lib.echo_quantize_rows(ctypes.byref(cfg), x.data_ptr(), _ptr(rows), _ptr(shift), _ptr(scale),
+                                out.codes.data_ptr(), out.scale.data_ptr(), stream)
+    if st:
+        check("echo_quantize_rows", st)
     return out
 
 
 def dequantize_rows(r: Int8Rows, dtype=torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
     """The values the codes stand for, [rows, cols] in dtype (echo_dequantize_rows)."""
     lib = _lib_handle()
-    _int8_rows(r, "r")
-    M, D = len(r), int(r.cols)
+    M, ldq = _int8_rows(r, "r")
+    D = r.cols
     if out is None:
-        out = torch.empty((M, D), dtype=dtype, device=r.codes.device)
-    elif _rows_of(out, "out").shape != (M, D):
-        raise ValueError(f"out must be [{M}, {D}]")
-    _here(r.codes, scale=r.scale, out=out)
-    cfg = QuantizeCfg(M, D, _echo_dtype(out), M, _ld(out), _ld(r.codes), 0.0)
-    check("echo_dequantize_rows",
-          lib.echo_dequantize_rows(ctypes.byref(cfg), _ptr(r.codes), _ptr(r.scale), _ptr(out), _stream()))
+        out, ldx = r.codes.new_empty((M, D), dtype=dtype), D
+    else:
+        m, d, ldx = _rows_of(out, "out")
+        if (m, d) != (M, D):
+            raise ValueError(f"out must be [{M}, {D}]")
+    stream = _here(r.codes.get_device(), ("scale", r.scale), ("out", out))
+    cfg = QuantizeCfg(M, D, _echo_dtype(out), M, ldx, ldq, 0.0)
+    st = lib.echo_dequantize_rows(ctypes.byref(cfg), r.codes.data_ptr(), r.scale.data_ptr(), out.data_ptr(), stream)
+    if st:
+        check("echo_dequantize_rows", st)
     return out
 
 
@@ -804,78 +819,82 @@ def linear_int8(a: Int8Rows, w: Int8Rows, bias: torch.Tensor | None = None, acti
     -> [M, N] in dtype.  activation: None or "gelu" (tanh form); or gate (fp32
     [N]) and residual ([rows, N], picked by residual_rows): residual + gate * y."""
     lib = _lib_handle()
-    _int8_rows(a, "a")
-    _int8_rows(w, "w")
-    M, N, K = len(a), len(w), int(a.cols)
+    M, lda = _int8_rows(a, "a")
+    N, ldw = _int8_rows(w, "w")
+    K = a.cols
     if w.cols != K:
         raise ValueError(f"a has {K} columns, w {w.cols}")
-    if activation not in (None, "gelu"):
-        raise ValueError('activation must be None or "gelu"')
-    if (gate is None) != (residual is None) or (residual is None and residual_rows is not None):
-        raise ValueError("pass gate and residual together (residual_rows with them)")
-    if gate is not None and activation is not None:
-        raise ValueError("activation does not go with gate and residual")
+    epi = _lib.ECHO_LINEAR_NONE
+    if activation is not None:
+        if activation != "gelu":
+            raise ValueError('activation must be None or "gelu"')
+        epi = _lib.ECHO_LINEAR_GELU_TANH
     bias_dt = res_dt = ECHO_F32
     if bias is not None:
         bias_dt = _echo_dtype(_vector(bias, "bias", N))
     nres = ldr = 0
-    if gate is not None:
+    if gate is not None or residual is not None or residual_rows is not None:
+        if gate is None or residual is None:
+            raise ValueError("pass gate and residual together (residual_rows with them)")
+        if activation is not None:
+            raise ValueError("activation does not go with gate and residual")
+        epi = _lib.ECHO_LINEAR_GATE_RESIDUAL
         _vector(gate, "gate", N, torch.float32)
-        res_dt = _echo_dtype(_rows_of(residual, "residual"))
-        nres, ldr = residual.shape[0], _ld(residual)
-        if residual.shape[1] != N:
+        nres, width, ldr = _rows_of(residual, "residual")
+        res_dt = _echo_dtype(residual)
+        if width != N:
             raise ValueError(f"residual must have {N} columns")
         if residual_rows is not None:
             _vector(residual_rows, "residual_rows", M, torch.int32)
         elif nres != M:
             raise ValueError(f"residual must have {M} rows")
     if out is None:
-        out = torch.empty((M, N), dtype=dtype, device=a.codes.device)
-    elif _rows_of(out, "out").shape != (M, N):
-        raise ValueError(f"out must be [{M}, {N}]")
-    _here(a.codes, a_scale=a.scale, w=w.codes, w_scale=w.scale, bias=bias, gate=gate, residual=residual,
-          residual_rows=residual_rows, out=out)
-    epi = (_lib.ECHO_LINEAR_GATE_RESIDUAL if gate is not None
-           else _lib.ECHO_LINEAR_GELU_TANH if activation else _lib.ECHO_LINEAR_NONE)
-    cfg = LinearInt8Cfg(M, N, K, epi, _echo_dtype(out), bias_dt, res_dt, nres, _ld(a.codes), _ld(w.codes),
-                        _ld(out), ldr)
-    need = lib.echo_linear_int8_workspace(ctypes.byref(cfg))
-    ws = _scratch(need, workspace, out.device)
-    check("echo_linear_int8",
-          lib.echo_linear_int8(ctypes.byref(cfg), _ptr(a.codes), _ptr(a.scale), _ptr(w.codes), _ptr(w.scale),
-                               _ptr(bias), _ptr(gate), _ptr(residual), _ptr(residual_rows), _ptr(out),
-                               _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+        out, ldc = a.codes.new_empty((M, N), dtype=dtype), N
+    else:
+        m, d, ldc = _rows_of(out, "out")
+        if (m, d) != (M, N):
+            raise ValueError(f"out must be [{M}, {N}]")
+    stream = _here(a.codes.get_device(), ("a.scale", a.scale), ("w.codes", w.codes), ("w.scale", w.scale),
+                   ("bias", bias), ("gate", gate), ("residual", residual), ("residual_rows", residual_rows),
+                   ("out", out))
+    cfg = ctypes.byref(LinearInt8Cfg(M, N, K, epi, _echo_dtype(out), bias_dt, res_dt, nres, lda, ldw, ldc, ldr))
+    ws = _scratch(lib.echo_linear_int8_workspace(cfg), workspace, out)
+    st = lib.echo_linear_int8(cfg, a.codes.data_ptr(), a.scale.data_ptr(), w.codes.data_ptr(), w.scale.data_ptr(),
+                              _ptr(bias), _ptr(gate), _ptr(residual), _ptr(residual_rows), out.data_ptr(),
+                              _ptr(ws), 0 if ws is None else ws.numel(), stream)
+    if st:
+        check("echo_linear_int8", st)
     return out
 
 
-def _scratch(need: int, workspace: Workspace | None, device) -> torch.Tensor | None:
+def _scratch(need: int, workspace: Workspace | None, like: torch.Tensor) -> torch.Tensor | None:
     """`need` bytes from the caller's workspace, or of this call's own (ordered
     on its stream by torch's allocator, so that calls on several streams and
     captured graphs never share one)."""
     if need == 0:
         return None
     if workspace is not None:
-        return workspace.get(need, device)
-    return torch.empty(need, dtype=torch.uint8, device=device)
+        return workspace.get(need, like.device)
+    return like.new_empty(need, dtype=torch.uint8)
 
 
 # ------------------------------------------------------------ cross attention
 
-def _heads_of(t: torch.Tensor, name: str, dtype=None) -> torch.Tensor:
+def _heads_of(t: torch.Tensor, name: str, dtype=None) -> tuple:
+    """((elements, rows, heads, dh), strides) of a device tensor with contiguous dh;
+    the stride of a dimension of one is not used."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 4 or t.shape[2] < 1 or (t.shape[3] > 1 and t.stride(3) != 1):
-        raise ValueError(f"{name} must be [elements, rows, heads, dh] with contiguous dh")
-    return t
-
-
-def _strides(t: torch.Tensor) -> Strides:
-    """(element, row, head) strides; those of a single one are not used."""
-    return Strides(*[t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)])
+    if t.dim() == 4:
+        b, n, h, d = shape = t.shape
+        sb, sn, sh, sd = t.stride()
+        if h >= 1 and (sd == 1 or d == 1):
+            return shape, (sb if b > 1 else 0, sn if n > 1 else 0, sh if h > 1 else 0)
+    raise ValueError(f"{name} must be [elements, rows, heads, dh] with contiguous dh")
 
 
 def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: torch.Tensor | None = None,
@@ -887,34 +906,36 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: to
     without any gets zeros.  scale: 1 / sqrt(dh) by default.  Returns
     [B, Lq, H, dh]."""
     lib = _lib_handle()
-    _heads_of(q, "q")
-    _heads_of(k, "k", q.dtype)
-    _heads_of(v, "v", q.dtype)
-    B, Lq, H, dh = q.shape
-    Lk, Hkv = k.shape[1], k.shape[2]
-    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != dh or H % Hkv:
+    shape, qs = _heads_of(q, "q")
+    kshape, ks = _heads_of(k, "k", q.dtype)
+    vshape, vs = _heads_of(v, "v", q.dtype)
+    B, Lq, H, dh = shape
+    Bk, Lk, Hkv, dk = kshape
+    if kshape != vshape or Bk != B or dk != dh or H % Hkv:
         raise ValueError("k and v must be [B, Lk, Hkv, dh] with Hkv dividing q's heads")
     if k_len is not None:
         _vector(k_len, "k_len", B, torch.int32)
     if key_mask is not None:
-        if key_mask.dtype == torch.bool:
+        if isinstance(key_mask, torch.Tensor) and key_mask.dtype == torch.bool:
             key_mask = key_mask.view(torch.uint8)
         _dev(key_mask, "key_mask", torch.uint8)
         if key_mask.shape != (B, Lk):
             raise ValueError(f"key_mask must be [{B}, {Lk}]")
     if out is None:
-        out = torch.empty((B, Lq, H, dh), dtype=q.dtype, device=q.device)
-    elif _heads_of(out, "out", q.dtype).shape != q.shape or any(
-            out.stride(i) == 0 for i in range(3) if out.shape[i] > 1):
-        raise ValueError("out must have the shape of q, and no row twice")
-    _here(q, k=k, v=v, k_len=k_len, key_mask=key_mask, out=out)
-    cfg = CrossAttentionCfg(B, Lq, Lk, H, Hkv, dh, _echo_dtype(q), dh ** -0.5 if scale is None else float(scale),
-                            _strides(q), _strides(k), _strides(v), _strides(out))
-    need = lib.echo_cross_attention_workspace(ctypes.byref(cfg), 0 if key_mask is None else 1)
-    ws = _scratch(need, workspace, q.device)
-    check("echo_cross_attention",
-          lib.echo_cross_attention(ctypes.byref(cfg), _ptr(q), _ptr(k), _ptr(v), _ptr(k_len), _ptr(key_mask),
-                                   _ptr(out), _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+        out = q.new_empty(shape)
+        os = (Lq * H * dh, H * dh, dh)
+    else:
+        oshape, os = _heads_of(out, "out", q.dtype)
+        if oshape != shape or any(s == 0 for s, n in zip(os, shape) if n > 1):
+            raise ValueError("out must have the shape of q, and no row twice")
+    stream = _here(q.get_device(), ("k", k), ("v", v), ("k_len", k_len), ("key_mask", key_mask), ("out", out))
+    cfg = ctypes.byref(CrossAttentionCfg(B, Lq, Lk, H, Hkv, dh, _echo_dtype(q), dh ** -0.5 if scale is None else scale,
+                                         qs, ks, vs, os))
+    ws = _scratch(lib.echo_cross_attention_workspace(cfg, 0 if key_mask is None else 1), workspace, q)
+    st = lib.echo_cross_attention(cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(k_len), _ptr(key_mask),
+                                  out.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(), stream)
+    if st:
+        check("echo_cross_attention", st)
     return out
 
 
