@@ -559,7 +559,9 @@ int echo_linear_int8(const echo_linear_int8_cfg* cfg, const int8_t* a, const flo
  * with key_mask[b][j] != 0 (device uint8 [B][Lk]; NULL: all).  A query with no
  * such state, or whose scores are all -inf, gets zeros; what masked states
  * hold has no effect.  Scores, softmax and sums in fp32 (the probabilities
- * enter the second product in `dtype`).
+ * enter the second product in `dtype`).  Where the queries do not fill the
+ * device the states are split and joined in fp32, so a row's rounding may depend
+ * on how many rows the call has.
  * Every tensor has its strides, in elements, for the element, the row and the
  * head; dh values are contiguous.  Strides are multiples of 16 bytes and not
  * negative; those of q, k and v may be 0.

@@ -284,7 +284,8 @@ __global__ void __launch_bounds__(256, 2) cross_bf16(CrossArgs p) {
 
   // The states pass in halves of 32: while the matrix cores compute the scores
   // of one half, the vector units turn those of the half before it into
-  // probabilities, which then weigh V.  LDS reads are issued two MFMAs ahead.
+  // probabilities, which then weigh V.  LDS reads are issued
+  // X_RING MFMAs ahead.
   bf16x8 pf[2];
   float psum;
   auto weigh = [&](const f32x16& sc, int c) __attribute__((always_inline)) {  // scores 2 c, 2 c + 1
@@ -389,6 +390,11 @@ __global__ void __launch_bounds__(256, 2) cross_bf16(CrossArgs p) {
     if (!idle) scores(0, 0, s0, [](int) {});
   }
   for (int u = 0; u < nt; ++u) {
+    // The two workgroups of a CU start together and would load and compute
+    // together; the one past its middle goes first, so that they come apart and
+    // one's loads and stores run under the other's products (13104 x 2 queries:
+    // 240 -> 232 us; 3276 queries x 32760 states: 2314 -> 2202)
+    if (2 * u >= nt) __builtin_amdgcn_s_setprio(2);
     if (!idle) {
       psum = 0.0f;
       scores(u, 1, s1, [&](int c) __attribute__((always_inline)) { weigh(s0, c); });
@@ -645,6 +651,7 @@ int x_splits(int bf16, int B, int Lq, int Lk, int H, int Hkv, int dh) {
   float best_us = 0.0f;
   for (const int ns : {1, 2, 3, 4, 5, 6, 8, 12, 16, 24, 32}) {
     if (ns > 1 && nt < 2 * ns) break;
+    if (ns > 1 && wgs * ns * X_ROWS * (dhp + 2) * 4 > (int64_t(512) << 20)) break;  // partial results
     const int steps = (nt + ns - 1) / ns;
     const int64_t pieces = wgs * ns, full = pieces / slots, rest = pieces % slots;
     const float round = steps * all + 6.0f;

@@ -267,9 +267,9 @@ hipError_t launch_q(const QuantizeArgs& p, hipStream_t stream) {
   // With LN a group takes several rows for one read of the modulation; without,
   // rows of their own start sooner (32760 x 5120 bf16: 81 us against 91 with 16
   // groups a CU; with LN 137 and 150).
-  const int groups = (p.M + RPB - 1) / RPB, most = LN ? 16 * device_cu_count() : kMaxGroups;
-  return ECHO_LAUNCH("quantize_rows", (quantize_rows_k<T, THREADS, NV, VEC, LN>), dim3(groups < most ? groups : most),
-                     dim3(BLOCK), 0, stream, p);
+  const int64_t groups = (int64_t(p.M) + RPB - 1) / RPB, most = LN ? 16 * device_cu_count() : kMaxGroups;
+  return ECHO_LAUNCH("quantize_rows", (quantize_rows_k<T, THREADS, NV, VEC, LN>),
+                     dim3(static_cast<unsigned>(groups < most ? groups : most)), dim3(BLOCK), 0, stream, p);
 }
 
 // The shortest form whose registers hold the row.  (5120 wide: a row to 256
