@@ -522,7 +522,8 @@ int echo_dequantize_rows(const echo_quantize_cfg* cfg, const int8_t* codes, cons
  * echo_quantize_rows writes them: multiples of 128, at least
  * echo_int8_pitch(K), zeros behind K in one of the two at least.  bias [N] in
  * bias_dtype or NULL; gate fp32 [N]; residual rows ldr elements apart in
- * residual_dtype; c rows ldc elements apart.
+ * residual_dtype; c rows ldc elements apart (c may be the residual itself where
+ * residual_rows is NULL).
  * a, w: 16-byte aligned; every other pointer by its element type.
  * Requires 1 <= N <= 2^22, 1 <= K <= 65536, M >= 0 (0: no-op), and fewer than
  * 2^24 tiles of 64 x 64 outputs.

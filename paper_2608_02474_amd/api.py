@@ -529,6 +529,8 @@ def wan_block_partial(params: dict, x: torch.Tensor, ctx: torch.Tensor, idx: tor
     ints); grid (T, gh, gw).  Returns y_sel [sum(n_sel), D] fp32 in idx order.
     params: the block weights plus wqc, wkc, wvc, woc, bqc, bkc, bvc, boc (in
     x's dtype) and gq, gk, gqc, gkc, g3, b3 (fp32 [D])."""
+    if is_int8_block(params):
+        raise ValueError("the Wan-style block takes no weights in 8 bits")
     lib = _lib_handle()
     _dev(x, "x")
     _dev(ctx, "ctx", x.dtype)
@@ -701,12 +703,12 @@ class Int8Rows:
 
 def _here(dev: int, *others) -> int:
     """The stream of the current device, which has to be that of every tensor:
-    `dev` the first one's, (name, tensor or None) the others'."""
+    `dev` the first one's; others may be None."""
     if dev != torch.cuda.current_device():
         raise ValueError("tensors must be on the current device")
-    for name, t in others:
+    for t in others:
         if t is not None and t.get_device() != dev:
-            raise ValueError(f"{name} must be on the same device as the other tensors")
+            raise ValueError("tensors must be on one device")
     return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(dev)
 
 
@@ -742,8 +744,17 @@ def _int8_rows(r: Int8Rows, name: str) -> tuple:
     """(rows, pitch) of checked 8-bit rows."""
     if not isinstance(r, Int8Rows):
         raise TypeError(f"{name} must be Int8Rows (see quantize_rows)")
-    n, width, ld = _rows_of(r.codes, f"{name}.codes", torch.int8)
-    _vector(r.scale, f"{name}.scale", n, torch.float32)
+    c, s = r.codes, r.scale
+    if (isinstance(c, torch.Tensor) and isinstance(s, torch.Tensor) and c.dim() == 2 and c.is_cuda and s.is_cuda
+            and c.dtype == torch.int8 and s.dtype == torch.float32):
+        n, width = c.shape
+        ld, unit = c.stride()
+        if (unit == 1 and ld >= width >= r.cols and ld % 128 == 0 and width % 128 == 0 and 0 < r.cols <= 65536
+                and s.shape == (n,) and s.is_contiguous()):
+            return n, ld
+    # not the usual case: the other checks say what is wrong, or take it
+    n, width, ld = _rows_of(c, f"{name}.codes", torch.int8)
+    _vector(s, f"{name}.scale", n, torch.float32)
     pitch = (r.cols + 127) // 128 * 128
     if not 1 <= r.cols <= 65536 or width < pitch or ld % 128 or width % 128:
         raise ValueError(f"{name}.codes must have a pitch of {pitch} bytes or a larger multiple of 128")
@@ -782,8 +793,7 @@ def quantize_rows(x: torch.Tensor, rows: torch.Tensor | None = None, shift: torc
             raise ValueError(f"out must hold {M} rows of {D} columns")
         if out.codes.shape[1] != ldq:
             raise ValueError("out.codes must have rows of whole pitches")
-    stream = _here(x.get_device(), ("rows", rows), ("shift", shift), ("scale", scale), ("out.codes", out.codes),
-                   ("out.scale", out.scale))
+    stream = _here(x.get_device(), rows, shift, scale, out.codes, out.scale)
     cfg = QuantizeCfg(M, D, _echo_dtype(x), n, ldx, ldq, ln_eps)
     st = lib.echo_quantize_rows(ctypes.byref(cfg), x.data_ptr(), _ptr(rows), _ptr(shift), _ptr(scale),
                                 out.codes.data_ptr(), out.scale.data_ptr(), stream)
@@ -803,7 +813,7 @@ def dequantize_rows(r: Int8Rows, dtype=torch.bfloat16, out: torch.Tensor | None 
         m, d, ldx = _rows_of(out, "out")
         if (m, d) != (M, D):
             raise ValueError(f"out must be [{M}, {D}]")
-    stream = _here(r.codes.get_device(), ("scale", r.scale), ("out", out))
+    stream = _here(r.codes.get_device(), r.scale, out)
     cfg = QuantizeCfg(M, D, _echo_dtype(out), M, ldx, ldq, 0.0)
     st = lib.echo_dequantize_rows(ctypes.byref(cfg), r.codes.data_ptr(), r.scale.data_ptr(), out.data_ptr(), stream)
     if st:
@@ -854,9 +864,7 @@ def linear_int8(a: Int8Rows, w: Int8Rows, bias: torch.Tensor | None = None, acti
         m, d, ldc = _rows_of(out, "out")
         if (m, d) != (M, N):
             raise ValueError(f"out must be [{M}, {N}]")
-    stream = _here(a.codes.get_device(), ("a.scale", a.scale), ("w.codes", w.codes), ("w.scale", w.scale),
-                   ("bias", bias), ("gate", gate), ("residual", residual), ("residual_rows", residual_rows),
-                   ("out", out))
+    stream = _here(a.codes.get_device(), a.scale, w.codes, w.scale, bias, gate, residual, residual_rows, out)
     cfg = ctypes.byref(LinearInt8Cfg(M, N, K, epi, _echo_dtype(out), bias_dt, res_dt, nres, lda, ldw, ldc, ldr))
     ws = _scratch(lib.echo_linear_int8_workspace(cfg), workspace, out)
     st = lib.echo_linear_int8(cfg, a.codes.data_ptr(), a.scale.data_ptr(), w.codes.data_ptr(), w.scale.data_ptr(),
@@ -928,7 +936,7 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: to
         oshape, os = _heads_of(out, "out", q.dtype)
         if oshape != shape or any(s == 0 for s, n in zip(os, shape) if n > 1):
             raise ValueError("out must have the shape of q, and no row twice")
-    stream = _here(q.get_device(), ("k", k), ("v", v), ("k_len", k_len), ("key_mask", key_mask), ("out", out))
+    stream = _here(q.get_device(), k, v, k_len, key_mask, out)
     cfg = ctypes.byref(CrossAttentionCfg(B, Lq, Lk, H, Hkv, dh, _echo_dtype(q), dh ** -0.5 if scale is None else scale,
                                          qs, ks, vs, os))
     ws = _scratch(lib.echo_cross_attention_workspace(cfg, 0 if key_mask is None else 1), workspace, q)

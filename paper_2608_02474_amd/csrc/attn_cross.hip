@@ -384,32 +384,30 @@ __global__ void __launch_bounds__(256, 2) cross_bf16(CrossArgs p) {
       __syncthreads();
     }
   };
-  f32x16 s0, s1;
-  if (nt > 0) {
+  if (idle) {
+    for (int u = 0; u < nt; ++u) arrive(u);
+  } else if (nt > 0) {
+    f32x16 s0, s1;
     arrive(0);
-    if (!idle) scores(0, 0, s0, [](int) {});
-  }
-  for (int u = 0; u < nt; ++u) {
-    // The two workgroups of a CU start together and would load and compute
-    // together; the one past its middle goes first, so that they come apart and
-    // one's loads and stores run under the other's products (13104 x 2 queries:
-    // 240 -> 232 us; 3276 queries x 32760 states: 2314 -> 2202)
-    if (2 * u >= nt) __builtin_amdgcn_s_setprio(2);
-    if (!idle) {
+    scores(0, 0, s0, [](int) {});
+    for (int u = 0; u < nt; ++u) {
+      // The two workgroups of a CU start together and would load and compute
+      // together; the one past its middle goes first, so that they come apart and
+      // one's loads and stores run under the other's products (13104 x 2 queries:
+      // 240 -> 232 us; 3276 queries x 32760 states: 2314 -> 2202)
+      if (2 * u >= nt) __builtin_amdgcn_s_setprio(2);
       psum = 0.0f;
       scores(u, 1, s1, [&](int c) __attribute__((always_inline)) { weigh(s0, c); });
       settle(s0);
       values(u, 0);
-    }
-    psum = 0.0f;
-    if (u + 1 < nt) {
-      arrive(u + 1);
-      if (!idle) scores(u + 1, 0, s0, [&](int c) __attribute__((always_inline)) { weigh(s1, c); });
-    } else if (!idle) {
+      psum = 0.0f;
+      if (u + 1 < nt) {
+        arrive(u + 1);
+        scores(u + 1, 0, s0, [&](int c) __attribute__((always_inline)) { weigh(s1, c); });
+      } else {
 #pragma unroll
-      for (int c = 0; c < 8; ++c) weigh(s1, c);
-    }
-    if (!idle) {
+        for (int c = 0; c < 8; ++c) weigh(s1, c);
+      }
       settle(s1);
       values(u, 1);
     }

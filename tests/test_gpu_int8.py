@@ -266,6 +266,16 @@ def test_linear_int8_largest_sums():
         assert (got.cpu().double() == float(np.float32(-127 * 127 * K))).all()
 
 
+@pytest.mark.parametrize("M,N,K", [(3, 40, 128), (12, 100, 256), (100, 200, 4096), (600, 516, 256), (300, 203, 128)])
+def test_linear_int8_onto_its_residual(M, N, K):
+    g = _gen(M)
+    a, w = _random_rows(g, M, K), _random_rows(g, N, K, 0.05)
+    gate, res = _rand(g, N).to(device()), _rand(g, M, N).to(device())
+    want = api.linear_int8(_on(*a, K), _on(*w, K), gate=gate, residual=res, dtype=torch.float32)
+    got = api.linear_int8(_on(*a, K), _on(*w, K), gate=gate, residual=res, out=res)
+    assert got is res and torch.equal(got, want)
+
+
 def test_linear_int8_rows_are_independent_and_behind_is_left():
     """A row's result does not depend on how many rows come with it, NaN rows stay
     alone, missing residual rows are NaN, and the output's surroundings stay."""

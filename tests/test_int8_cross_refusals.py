@@ -135,3 +135,5 @@ def test_int8_block_weights_are_told_from_others():
     assert api.is_int8_block({"wq": w}) and not api.is_int8_block({"wq": torch.zeros(4, 64)})
     with pytest.raises(ValueError, match="batch_invariant"):
         api.block_partial({"wq": w}, None, None, 0, 1, batch_invariant=True)
+    with pytest.raises(ValueError, match="8 bits"):
+        api.wan_block_partial({"wq": w}, None, None, None, [0], 1, (1, 1, 1))
