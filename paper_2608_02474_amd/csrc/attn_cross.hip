@@ -624,14 +624,16 @@ constexpr size_t kXAlign = 256;
 size_t x_up(size_t n) { return (n + kXAlign - 1) / kXAlign * kXAlign; }
 int x_pad(int dh) { return dh <= 32 ? 32 : dh <= 64 ? 64 : 128; }
 
-// Ranges of the states, by estimated time (us): a workgroup's tile of states
-// takes `one` alone on its CU and `all` with the CU full, at least what its K
-// and V take from memory where no other workgroup shares them, and `fix` for
-// its queries and outputs; a split adds the second launch and its partial
-// results, written and read.  With several elements, which have several lengths,
-// rounds before the last count for three quarters.  40 groups of one query x 32760
-// states 623 us whole, 134 in 12 ranges; 1040 workgroups x 512 tiles 2638 and 2286
-// (5); 488 x 94 tiles 190 and 211 (2); 384 x 8 tiles 24 and 44 (2).
+// Ranges of the states, by estimated time (us).  A workgroup's tile of states
+// takes `one` alone on its CU and `all` with the CU full (in between by their
+// number), and no less than its K and V take from memory where no other
+// workgroup shares them; a round has 4 or 6 us beside its tiles for queries and
+// outputs; a split adds the second launch and its partial results, written and
+// read.  With several elements, which have several lengths, rounds before the
+// last count for three quarters.  Measured (us): 40 groups of one query x 32760
+// states 623 whole, 134 in 12 ranges; 1040 workgroups x 512 tiles 2638 and 2286
+// (5); 488 x 94 tiles 190 and 211 (2), at dh 64 121 and 126 (3); 384 x 8 tiles 24
+// and 44 (2).
 int x_splits(int bf16, int B, int Lq, int Lk, int H, int Hkv, int dh) {
   const int64_t rows = static_cast<int64_t>(H / Hkv) * Lq, tiles = (rows + X_ROWS - 1) / X_ROWS;
   const int64_t wgs = tiles * B * Hkv;
@@ -653,11 +655,11 @@ int x_splits(int bf16, int B, int Lq, int Lk, int H, int Hkv, int dh) {
     const int steps = (nt + ns - 1) / ns;
     const int64_t pieces = wgs * ns, full = pieces / slots, rest = pieces % slots;
     const float round = steps * all + 6.0f;
-    float us = rest == 0 ? round : rest <= ncu ? steps * one + 4.0f : round;
+    const int n = static_cast<int>((rest + ncu - 1) / ncu);  // workgroups on the busiest CU of the last round
+    float us = rest == 0 ? round : n == 1 ? steps * one + 4.0f : steps * (one + (all - one) * (n - 1) / (per - 1)) + 6.0f;
     us += (B > 1 ? 0.75f : 1.0f) * (rest == 0 ? full - 1 : full) * round;
     if (ns > 1) {
-      const int64_t n = static_cast<int64_t>(B) * Hkv * ns * rows;
-      us += 6.0f + n * (dhp + 2) * 8.0f / 4e6f;
+      us += 6.0f + static_cast<int64_t>(B) * Hkv * ns * rows * (dhp + 2) * 8.0f / 4e6f;
     }
     if (ns == 1 || us < best_us) {
       best = ns;
