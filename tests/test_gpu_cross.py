@@ -232,3 +232,18 @@ def test_cross_attention_streams_and_graphs():
             want = api.cross_attention(q, k, v, k_len=n, key_mask=m)
             torch.cuda.synchronize()
             assert torch.equal(y, want), turn
+
+
+def test_cross_attention_queries_pass_32_bits():
+    """More than 2^31 query values: the first and the last rows."""
+    B, Lq, H, dh, Lk = 1, 420000, 40, 128, 70
+    g = torch.Generator(device=device())
+    g.manual_seed(3)
+    q = torch.empty(B, Lq, H, dh, dtype=BF, device=device())
+    for i in range(0, Lq, 60000):
+        q[:, i:i + 60000] = torch.randn(B, 60000, H, dh, device=device(), generator=g)
+    k = torch.randn(B, Lk, H, dh, device=device(), generator=g).to(BF)
+    v = torch.randn(B, Lk, H, dh, device=device(), generator=g).to(BF)
+    got = api.cross_attention(q, k, v)
+    at = [0, 127, 128, 419300, Lq - 1]
+    _check(got[:, at], q[:, at].cpu(), k.cpu(), v.cpu(), what="first and last")

@@ -405,3 +405,50 @@ def test_block_in_8_bits(dtype):
     st.step(xref, fw, w.N)
     out = st.step(x, fw, w.N)
     assert torch.isfinite(out.float()).all() and st.history[1][0] == api.topk_count(0.3, w.L)
+
+
+# ------------------------------------------------- offsets of more than 32 bits
+
+def test_rows_beyond_32_bit_offsets():
+    """More than 2^31 codes, and with them the values read back (both loop over their
+    launches), and products over them: the first and the last rows against the CPU."""
+    M, D = 32800, 65536
+    g = torch.Generator(device=device())
+    g.manual_seed(1)
+    x = torch.empty(M, D, dtype=torch.bfloat16, device=device())
+    for i in range(0, M, 4100):
+        x[i:i + 4100] = torch.randn(4100, D, device=device(), generator=g)
+    r = api.quantize_rows(x)
+    back = api.dequantize_rows(r)
+    at = [0, 1, 16383, 32767, 32768, M - 1]
+    want, top = codes_of(x[at].cpu().double())
+    assert torch.equal(r.codes[at].cpu().double(), want)
+    assert torch.equal(back[at].cpu(), (want.float() * (top.float() / 127)).bfloat16())
+    del back
+    w = _random_rows(_gen(2), 8, D, 0.05)
+    y = api.linear_int8(r, _on(*w, D), dtype=torch.float32)         # tokens far apart
+    _check_linear(y[at].cpu(), (r.codes[at].cpu(), r.scale[at].cpu()), w, D, None, torch.float32, what="tokens")
+    a = _random_rows(_gen(3), 100, D)
+    for m in (3, 12, 100):                                          # channels far apart
+        y = api.linear_int8(api.Int8Rows(a[0][:m].to(device()), a[1][:m].to(device()), D), r, dtype=torch.float32)
+        _check_linear(y[:, at].cpu(), (a[0][:m], a[1][:m]), (r.codes[at].cpu(), r.scale[at].cpu()), D, None,
+                      torch.float32, what=f"channels, {m} tokens")
+
+
+def test_linear_int8_output_beyond_32_bit_offsets():
+    M, N, K = 70000, 32768, 128
+    g = _gen(4)
+    a, w = _random_rows(g, M, K), _random_rows(g, N, K, 0.05)
+    y = api.linear_int8(_on(*a, K), _on(*w, K))
+    at = [0, 255, 65535, 65536, M - 1]
+    _check_linear(y[at].cpu(), (a[0][at], a[1][at]), w, K, None, torch.bfloat16, what="last rows")
+
+
+def test_quantize_rows_more_than_a_launch_of_rows():
+    M, D = 4 * 2 ** 20 + 37, 136                                    # 4 rows to each of at most 2^20 workgroups
+    x = torch.randn(M, D, device=device()).bfloat16()
+    r = api.quantize_rows(x)
+    at = [0, 4 * 2 ** 20 - 1, 4 * 2 ** 20, M - 1]
+    want, top = codes_of(x[at].cpu().double())
+    assert torch.equal(r.codes[at].cpu()[:, :D].double(), want)
+    assert torch.equal(r.scale[at].cpu(), top[:, 0].float() / 127)
