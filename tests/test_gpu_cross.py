@@ -247,3 +247,37 @@ def test_cross_attention_queries_pass_32_bits():
     got = api.cross_attention(q, k, v)
     at = [0, 127, 128, 419300, Lq - 1]
     _check(got[:, at], q[:, at].cpu(), k.cpu(), v.cpu(), what="first and last")
+
+
+@pytest.mark.parametrize("seed", range(32))
+def test_cross_attention_random(seed):
+    """Any numbers of elements, queries, states and heads, lengths, masks, layouts."""
+    import numpy as np
+    rng = np.random.default_rng(seed)
+    g = _gen(500 + seed)
+    log = lambda lo, hi: int(np.exp(rng.uniform(np.log(lo), np.log(hi))))  # noqa: E731
+    dtype = [BF, BF, F32][int(rng.integers(3))]
+    dh = int(rng.choice([64, 128])) if dtype == BF else 4 * log(1, 33)
+    B, Lq, Lk, Hkv, G = log(1, 6), log(1, 600), log(1, 1500), log(1, 5), log(1, 9)
+    if B * Lq * Lk * Hkv * G > 3e7:
+        Lq = max(1, Lq // 16)
+    H = Hkv * G
+    r = lambda *s: torch.randn(*s, generator=g).to(dtype)  # noqa: E731
+    q = r(B, H, Lq, dh).transpose(1, 2) if rng.integers(2) else r(B, Lq, H, dh)
+    k, v = (r(B, Hkv, Lk, dh).transpose(1, 2), r(B, Lk, Hkv, dh)) if rng.integers(2) else (r(B, Lk, 2 * Hkv, dh)[:, :, :Hkv],
+                                                                                       r(B, Lk, Hkv, dh))
+    left, kw = torch.ones(B, Lk, dtype=torch.bool), {}
+    if rng.integers(2):
+        n = torch.randint(-1, Lk + 3, (B,), generator=g, dtype=torch.int32)
+        left &= torch.arange(Lk) < n[:, None]
+        kw["k_len"] = n.to(device())
+    if rng.integers(2):
+        m = torch.rand(B, Lk, generator=g) < float(rng.uniform(0, 1))
+        left &= m
+        kw["key_mask"] = m.to(device())
+    keep = k.to(device()), v.to(device())
+    out = torch.full((B, Lq + 2, H, dh), 4.0, dtype=dtype, device=device())
+    got = api.cross_attention(q.to(device()), *keep, out=out[:, 1:-1], **kw)
+    torch.cuda.synchronize()
+    assert (out[:, 0] == 4).all() and (out[:, -1] == 4).all()
+    _check(got, q, k, v, left, what=f"B{B} Lq{Lq} Lk{Lk} H{H}/{Hkv} dh{dh} {dtype}")

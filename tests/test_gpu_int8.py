@@ -4,6 +4,7 @@
 Codes and scales are exact by definition, and so are the integer sums; what is
 left are fp32 roundings (half a step each, 2^-24 of the value) and the rounding
 of the output (half a step of its type: bf16 2^-8, fp32 2^-24)."""
+import ctypes
 import math
 
 import numpy as np
@@ -11,7 +12,7 @@ import pytest
 import torch
 
 import synth
-from paper_2608_02474_amd import api
+from paper_2608_02474_amd import _lib, api
 
 from gpu_util import device, say
 
@@ -452,3 +453,66 @@ def test_quantize_rows_more_than_a_launch_of_rows():
     want, top = codes_of(x[at].cpu().double())
     assert torch.equal(r.codes[at].cpu()[:, :D].double(), want)
     assert torch.equal(r.scale[at].cpu(), top[:, 0].float() / 127)
+
+
+# ------------------------------------------------------- plans and random shapes
+
+@pytest.mark.parametrize("M,N,K,act", [(8813, 2304, 8320, None), (3276, 5120, 5120, "gelu"), (1950, 1536, 8960, "gate"),
+                                       (771, 11072, 5504, None), (100, 5120, 5120, "gate"), (20, 5120, 13824, "gelu"),
+                                       (4100, 4106, 4096, None), (700, 130, 9000, "gate")])
+def test_linear_int8_split_products(M, N, K, act):
+    """Deep products, whose tiles are split along the depth (all of them, those of the
+    last round, or none): the join runs just where the plan asks for a workspace, and
+    sampled rows and the last ones match."""
+    g = _gen(M + K)
+    a, w = _random_rows(g, M, K), _random_rows(g, N, K, 0.05)
+    A, W, bias = _on(*a, K), _on(*w, K), _rand(g, N)
+    kw, gate, res = {}, None, None
+    if act == "gate":
+        gate, res = _rand(g, N), _rand(g, M, N, dtype=torch.bfloat16)
+        kw = dict(gate=gate.to(device()), residual=res.to(device()))
+    elif act:
+        kw = dict(activation=act)
+    api.profile_enable(True)
+    try:
+        api.profile_read()
+        y = api.linear_int8(A, W, bias.to(device()), dtype=torch.float32, **kw)
+        names = set(api.profile_read())
+    finally:
+        api.profile_enable(False)
+    cfg = _lib.LinearInt8Cfg(M=M, N=N, K=K, out_dtype=_lib.ECHO_F32, bias_dtype=_lib.ECHO_F32,
+                             residual_dtype=_lib.ECHO_F32, lda=A.codes.stride(0), ldw=W.codes.stride(0), ldc=N)
+    assert ("gemm_int8_reduce" in names) == (_lib.load().echo_linear_int8_workspace(ctypes.byref(cfg)) > 0), names
+    at = torch.unique(torch.cat([torch.randint(0, M, (24,), generator=g), torch.tensor([0, M // 2, M - 1])]))
+    _check_linear(y[at.to(device())].cpu(), (a[0][at], a[1][at]), w, K, bias, torch.float32, act=act if act == "gelu" else None,
+                  gate=gate, res=None if res is None else res[at], what=f"{M}x{N}x{K}")
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_linear_int8_random_shapes(seed):
+    """Any tokens, channels and depth, any epilogue and type, rows of the operands and
+    of the output inside wider buffers."""
+    rng = np.random.default_rng(seed)
+    g = _gen(1000 + seed)
+    M, N, K = (int(np.exp(rng.uniform(np.log(lo), np.log(hi)))) for lo, hi in ((1, 3000), (1, 3000), (1, 3000)))
+    out_dtype = [torch.bfloat16, torch.float32][int(rng.integers(2))]
+    a, w = _random_rows(g, M, K), _random_rows(g, N, K, 0.05)
+    wide = torch.full((M, a[0].shape[1] + 256), 77, dtype=torch.int8)
+    wide[:, 128:-128] = a[0]
+    A = api.Int8Rows(wide.to(device())[:, 128:-128], a[1].to(device()), K)
+    buf = torch.full((M, N + int(rng.integers(0, 9))), 5.0, dtype=out_dtype, device=device())
+    bias = _rand(g, N, dtype=out_dtype) if rng.integers(2) else None
+    kw, act, gate, res = {}, None, None, None
+    kind = int(rng.integers(3))
+    if kind == 1:
+        act = "gelu"
+        kw["activation"] = act
+    elif kind == 2:
+        gate, rows = _rand(g, N), torch.randint(0, M + 3, (M,), generator=g, dtype=torch.int32)
+        full = _rand(g, M + 3, N + 5, dtype=[torch.bfloat16, torch.float32][int(rng.integers(2))])[:, :N]
+        res = full[rows.long()]
+        kw.update(gate=gate.to(device()), residual=full.to(device()), residual_rows=rows.to(device()))
+    y = api.linear_int8(A, _on(*w, K), None if bias is None else bias.to(device()), out=buf[:, :N], **kw)
+    torch.cuda.synchronize()
+    assert (buf[:, N:] == 5).all()
+    _check_linear(y.cpu(), a, w, K, bias, out_dtype, act=act, gate=gate, res=res, what=f"{M}x{N}x{K} kind {kind}")
