@@ -489,6 +489,8 @@ def _block_partial_int8(p: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int,
                         y_sel: torch.Tensor | None) -> torch.Tensor:
     """block_partial on 8-bit rows: the tokens are quantized in front of every
     product, one scale a token; attention, residuals and LayerNorms as there."""
+    if n_sel < 0 or H < 1:
+        check("echo_block_partial", _lib.ECHO_EINVAL)
     _dev(x, "x")
     L, D = x.shape
     _dev(p["mod"], "mod", torch.float32)

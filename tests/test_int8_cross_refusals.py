@@ -137,3 +137,11 @@ def test_int8_block_weights_are_told_from_others():
         api.block_partial({"wq": w}, None, None, 0, 1, batch_invariant=True)
     with pytest.raises(ValueError, match="8 bits"):
         api.wan_block_partial({"wq": w}, None, None, None, [0], 1, (1, 1, 1))
+
+
+@pytest.mark.parametrize("n_sel,H", [(-1, 1), (2, 0)])
+def test_int8_block_refuses_counts_as_the_block_does(lib, n_sel, H):
+    """A negative count is no slice that leaves the last tokens out."""
+    w = api.Int8Rows(torch.zeros(4, 128, dtype=torch.int8), torch.zeros(4), 64)
+    with pytest.raises(RuntimeError, match="echo_block_partial"):
+        api.block_partial({"wq": w}, None, None, n_sel, H)
