@@ -902,7 +902,7 @@ def _heads_of(t: torch.Tensor, name: str, dtype=None) -> tuple:
     if t.dim() == 4:
         b, n, h, d = shape = t.shape
         sb, sn, sh, sd = t.stride()
-        if h >= 1 and (sd == 1 or d == 1):
+        if h >= 1 and d >= 1 and (sd == 1 or d == 1):
             return shape, (sb if b > 1 else 0, sn if n > 1 else 0, sh if h > 1 else 0)
     raise ValueError(f"{name} must be [elements, rows, heads, dh] with contiguous dh")
 

@@ -281,3 +281,9 @@ def test_cross_attention_random(seed):
     torch.cuda.synchronize()
     assert (out[:, 0] == 4).all() and (out[:, -1] == 4).all()
     _check(got, q, k, v, left, what=f"B{B} Lq{Lq} Lk{Lk} H{H}/{Hkv} dh{dh} {dtype}")
+
+
+def test_cross_attention_refuses_heads_of_no_width():
+    q = torch.empty(1, 2, 2, 0, dtype=BF, device=device())
+    with pytest.raises(ValueError, match="contiguous dh"):
+        api.cross_attention(q, q, q)
