@@ -520,7 +520,7 @@ int echo_dequantize_rows(const echo_quantize_cfg* cfg, const int8_t* codes, cons
  * residual_nrows) gives NaN).  c is written in out_dtype, rounded once.
  * a: rows lda bytes apart, w: rows ldw bytes apart, both as
  * echo_quantize_rows writes them: multiples of 128, at least
- * echo_int8_pitch(K), zeros behind K in one of the two at least.  bias [N] in
+ * echo_int8_pitch(K), at most 65536, zeros behind K in one of the two at least.  bias [N] in
  * bias_dtype or NULL; gate fp32 [N]; residual rows ldr elements apart in
  * residual_dtype; c rows ldc elements apart (c may be the residual itself where
  * residual_rows is NULL).
@@ -565,7 +565,7 @@ int echo_linear_int8(const echo_linear_int8_cfg* cfg, const int8_t* a, const flo
  * on how many rows the call has.
  * Every tensor has its strides, in elements, for the element, the row and the
  * head; dh values are contiguous.  Strides are multiples of 16 bytes and not
- * negative; those of q, k and v may be 0.
+ * negative; those of q, k and v may be 0.  out overlaps no input.
  * Supported: ECHO_BF16 with dh 64 or 128; ECHO_F32 with dh % 4 == 0, dh <= 128;
  * scale > 0 and finite; row strides of k and v below 2^24;
  * B * Hkv * ceil(Lq * (H / Hkv) / 128) below 2^24.
