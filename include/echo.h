@@ -567,7 +567,7 @@ int echo_linear_int8(const echo_linear_int8_cfg* cfg, const int8_t* a, const flo
  * head; dh values are contiguous.  Strides are multiples of 16 bytes and not
  * negative; those of q, k and v may be 0.  out overlaps no input.
  * Supported: ECHO_BF16 with dh 64 or 128; ECHO_F32 with dh % 4 == 0, dh <= 128;
- * scale > 0 and finite; row strides of k and v below 2^24;
+ * scale > 0 and finite; row strides of k and v below 2^24; Lk <= 2^31 - 128;
  * B * Hkv * ceil(Lq * (H / Hkv) / 128) below 2^24.
  * B, Lq >= 0 (0: no-op), Lk >= 0 (0: every output is zero).
  */

@@ -311,6 +311,7 @@ bool linear_supported(const echo_linear_int8_cfg* c) {
 }
 
 // ---- cross attention
+constexpr int32_t kMaxStates = INT32_MAX - 127;  // 2^31 - 128: two tiles of 64 short of overflow
 bool strides_ok(const echo_strides& s, int per16) {
   return s.batch >= 0 && s.row >= 0 && s.head >= 0 && s.batch % per16 == 0 && s.row % per16 == 0 &&
          s.head % per16 == 0;
@@ -327,6 +328,8 @@ bool cross_supported(const echo_cross_attention_cfg* c) {
   if (!std::isfinite(c->scale * 1.4426950408889634f)) return false;  // the scale in units of log2
   // a tile of states is addressed by 32-bit offsets
   if (c->k.row >= (int64_t(1) << 24) || c->v.row >= (int64_t(1) << 24)) return false;
+  // states are numbered in 32 bits, up to the end of the tile after the last one
+  if (c->Lk > kMaxStates) return false;
   const int64_t rows = int64_t(c->H / c->Hkv) * c->Lq, groups = int64_t(c->B) * c->Hkv;
   return rows < (int64_t(1) << 31) - 128 && groups < kMaxGroups && groups * ((rows + 127) / 128) < kMaxGroups;
 }

@@ -145,3 +145,18 @@ def test_int8_block_refuses_counts_as_the_block_does(lib, n_sel, H):
     w = api.Int8Rows(torch.zeros(4, 128, dtype=torch.int8), torch.zeros(4), 64)
     with pytest.raises(RuntimeError, match="echo_block_partial"):
         api.block_partial({"wq": w}, None, None, n_sel, H)
+
+
+@pytest.mark.parametrize("dt,dh", [(BF, 64), (BF, 128), (F32, 32)])
+def test_cross_refuses_states_whose_numbers_overflow(lib, dt, dh):
+    """Tiles are counted, and states past the last one numbered, in 32 bits: 2^31 - 128
+    states are the most, with state strides of 0 no large tensor is needed for more."""
+    S = _lib.Strides
+    def cfg(Lk):
+        return _cross(B=1, Lq=1, Lk=Lk, H=1, Hkv=1, dh=dh, dt=dt, k=S(0, 0, 0), v=S(0, 0, 0))
+    most = 2 ** 31 - 128
+    assert lib.echo_cross_attention_workspace(ctypes.byref(cfg(most)), 0) > 0      # split over the states
+    assert lib.echo_cross_attention_workspace(ctypes.byref(cfg(most)), 1) > 4 * most
+    for Lk in (most + 1, 2 ** 31 - 64, 2 ** 31 - 1):
+        assert lib.echo_cross_attention_workspace(ctypes.byref(cfg(Lk)), 0) == 0
+        assert lib.echo_cross_attention(ctypes.byref(cfg(Lk)), *[FAKE] * 6, FAKE, 1 << 40, None) == EUNSUP
