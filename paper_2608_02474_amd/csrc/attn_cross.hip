@@ -132,43 +132,46 @@ __device__ __forceinline__ int64_t x_units(const CrossArgs& p, int tiles) {
   return static_cast<int64_t>(p.B) * p.Hkv * p.nsplit * tiles * X_ROWS;
 }
 
-// ---- states that the mask leaves, in order; one workgroup per element, eight
-// states a thread and turn
+// ---- states that the mask leaves, in order; a workgroup per element (it goes on
+// to others where there are more elements than workgroups), eight states a
+// thread and turn
 __global__ void __launch_bounds__(1024) cross_keys(CrossArgs p) {
   __shared__ int wave_n[16];
-  const int b = blockIdx.x, tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
-  int n = p.k_len != nullptr ? p.k_len[b] : p.Lk;
-  n = n < 0 ? 0 : (n < p.Lk ? n : p.Lk);
-  const uint8_t* mask = p.key_mask + static_cast<int64_t>(b) * p.Lk;
-  int32_t* list = p.key_list + static_cast<int64_t>(b) * p.Lk;
-  int base = 0;
-  for (int64_t j0 = 0; j0 < n; j0 += 8192) {
-    const int64_t j = j0 + 8 * tid;
-    uint32_t bits = 0;
+  const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
+  for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
+    int n = p.k_len != nullptr ? p.k_len[b] : p.Lk;
+    n = n < 0 ? 0 : (n < p.Lk ? n : p.Lk);
+    const uint8_t* mask = p.key_mask + static_cast<int64_t>(b) * p.Lk;
+    int32_t* list = p.key_list + static_cast<int64_t>(b) * p.Lk;
+    int base = 0;
+    for (int64_t j0 = 0; j0 < n; j0 += 8192) {
+      const int64_t j = j0 + 8 * tid;
+      uint32_t bits = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) bits |= (j + e < n && mask[j + e] != 0 ? 1u : 0u) << e;
-    const int mine = __popc(bits);
-    int upto = mine;  // of this lane and those before it
+      for (int e = 0; e < 8; ++e) bits |= (j + e < n && mask[j + e] != 0 ? 1u : 0u) << e;
+      const int mine = __popc(bits);
+      int upto = mine;  // of this lane and those before it
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const int other = __shfl_up(upto, d);
-      upto += lane >= d ? other : 0;
+      for (int d = 1; d < kWave; d *= 2) {
+        const int other = __shfl_up(upto, d);
+        upto += lane >= d ? other : 0;
+      }
+      if (lane == kWave - 1) wave_n[wave] = upto;
+      __syncthreads();
+      int at = base + upto - mine, total = 0;
+#pragma unroll
+      for (int w = 0; w < 16; ++w) {
+        at += w < wave ? wave_n[w] : 0;
+        total += wave_n[w];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (bits >> e & 1u) list[at++] = static_cast<int32_t>(j) + e;
+      base += total;
+      __syncthreads();
     }
-    if (lane == kWave - 1) wave_n[wave] = upto;
-    __syncthreads();
-    int at = base + upto - mine, total = 0;
-#pragma unroll
-    for (int w = 0; w < 16; ++w) {
-      at += w < wave ? wave_n[w] : 0;
-      total += wave_n[w];
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (bits >> e & 1u) list[at++] = static_cast<int32_t>(j) + e;
-    base += total;
-    __syncthreads();
+    if (tid == 0) p.key_count[b] = base;
   }
-  if (tid == 0) p.key_count[b] = base;
 }
 
 // ------------------------------------------------------------------- bf16
@@ -621,6 +624,9 @@ __global__ void __launch_bounds__(256) cross_combine(CrossArgs p) {
 namespace {
 
 constexpr size_t kXAlign = 256;
+// workgroups that compact masks: with 1024 threads each, far below the 2^32
+// threads of a launch, which one for each of up to 2^24 elements would pass
+constexpr int kXListGroups = 1 << 16;
 size_t x_up(size_t n) { return (n + kXAlign - 1) / kXAlign * kXAlign; }
 int x_pad(int dh) { return dh <= 32 ? 32 : dh <= 64 ? 64 : 128; }
 
@@ -704,7 +710,8 @@ hipError_t launch_cross(int bf16, CrossArgs a, void* workspace, hipStream_t stre
     ws += x_up(sizeof(int32_t) * static_cast<size_t>(a.B) * a.Lk);
     a.key_count = reinterpret_cast<int32_t*>(ws);
     ws += x_up(sizeof(int32_t) * a.B);
-    if ((e = ECHO_LAUNCH("cross_keys", cross_keys, dim3(a.B), dim3(1024), 0, stream, a)) != hipSuccess) return e;
+    const int groups = a.B < kXListGroups ? a.B : kXListGroups;
+    if ((e = ECHO_LAUNCH("cross_keys", cross_keys, dim3(groups), dim3(1024), 0, stream, a)) != hipSuccess) return e;
   }
   a.part = reinterpret_cast<float*>(ws);
   a.nsplit = x_splits(bf16, a.B, a.Lq, a.Lk, a.H, a.Hkv, a.dh);

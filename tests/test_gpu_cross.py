@@ -287,3 +287,27 @@ def test_cross_attention_refuses_heads_of_no_width():
     q = torch.empty(1, 2, 2, 0, dtype=BF, device=device())
     with pytest.raises(ValueError, match="contiguous dh"):
         api.cross_attention(q, q, q)
+
+
+def test_cross_attention_masks_of_very_many_elements():
+    """More masked elements than a launch holds workgroups of 1024 threads: the first
+    elements, those around each workgroup's second and last one, and a random few."""
+    B, Lk, dh = (1 << 22) + 37, 3, 64
+    g = torch.Generator(device=device())
+    g.manual_seed(12)
+    q = torch.randn(B, 1, 1, dh, device=device(), generator=g, dtype=BF)
+    k, v = (torch.randn(1, Lk, 1, dh, device=device(), generator=g, dtype=BF) for _ in range(2))
+    mask = (torch.rand(B, Lk, device=device(), generator=g) < 0.5).to(torch.uint8)
+    lens = torch.randint(0, Lk + 1, (B,), device=device(), generator=g, dtype=torch.int32)
+    got = api.cross_attention(q, k.expand(B, -1, -1, -1), v.expand(B, -1, -1, -1), k_len=lens, key_mask=mask)
+    torch.cuda.synchronize()
+    left = (mask != 0) & (torch.arange(Lk, device=device()) < lens[:, None])
+    assert (got[~left.any(1)] == 0).all()
+    at = torch.cat([torch.tensor([0, 1, (1 << 16) - 1, 1 << 16, (1 << 22) - 1, 1 << 22, B - 1]),
+                    torch.randint(0, B, (500,), generator=_gen(1))]).to(device())
+    n = len(at)
+    _check(got[at], q[at].cpu(), k.cpu().expand(n, -1, -1, -1), v.cpu().expand(n, -1, -1, -1), left[at].cpu(),
+           what="sampled elements")
+    one = left.sum(1) == 1                              # a single state: its values themselves
+    where = left.to(torch.uint8).argmax(1)[one]
+    assert torch.equal(got[one][:, 0, 0], v[0, where, 0])
