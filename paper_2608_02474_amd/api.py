@@ -700,6 +700,9 @@ class Int8Rows:
         return self.codes.shape[0]
 
 
+_MAX_COUNT = 2 ** 31 - 1   # the ABI's counts are 32 bits, and ctypes would wrap a larger one
+
+
 # A small call is bound by the host here too: the helpers below take a tensor's
 # shape and strides once, and say what is wrong only after something is.
 
@@ -726,6 +729,8 @@ def _rows_of(t: torch.Tensor, name: str, dtype=None) -> tuple:
     if t.dim() == 2:
         n, d = t.shape
         s, u = t.stride()
+        if n > _MAX_COUNT or d > _MAX_COUNT:
+            raise ValueError(f"{name} must have fewer than 2^31 rows and columns")
         if d >= 1 and (u == 1 or d == 1):
             if n <= 1:
                 return n, d, d
@@ -752,7 +757,7 @@ def _int8_rows(r: Int8Rows, name: str) -> tuple:
         n, width = c.shape
         ld, unit = c.stride()
         if (unit == 1 and ld >= width >= r.cols and ld % 128 == 0 and width % 128 == 0 and 0 < r.cols <= 65536
-                and s.shape == (n,) and s.is_contiguous()):
+                and s.shape == (n,) and s.is_contiguous() and n <= _MAX_COUNT):
             return n, ld
     # not the usual case: the other checks say what is wrong, or take it
     n, width, ld = _rows_of(c, f"{name}.codes", torch.int8)
@@ -775,8 +780,8 @@ def quantize_rows(x: torch.Tensor, rows: torch.Tensor | None = None, shift: torc
     M = n
     if rows is not None:
         M = _dev(rows, "rows", torch.int32).numel()
-        if rows.dim() != 1:
-            raise ValueError("rows must be one-dimensional")
+        if rows.dim() != 1 or M > _MAX_COUNT:
+            raise ValueError("rows must be one-dimensional, with fewer than 2^31 entries")
         if M > 0 and n == 0:
             raise ValueError("x has no rows to pick")
     if (shift is None) != (scale is None):
@@ -901,6 +906,8 @@ def _heads_of(t: torch.Tensor, name: str, dtype=None) -> tuple:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.dim() == 4:
         b, n, h, d = shape = t.shape
+        if max(shape) > _MAX_COUNT:
+            raise ValueError(f"{name} must have fewer than 2^31 elements, rows and heads")
         sb, sn, sh, sd = t.stride()
         if h >= 1 and d >= 1 and (sd == 1 or d == 1):
             return shape, (sb if b > 1 else 0, sn if n > 1 else 0, sh if h > 1 else 0)

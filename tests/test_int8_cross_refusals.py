@@ -160,3 +160,41 @@ def test_cross_refuses_states_whose_numbers_overflow(lib, dt, dh):
     for Lk in (most + 1, 2 ** 31 - 64, 2 ** 31 - 1):
         assert lib.echo_cross_attention_workspace(ctypes.byref(cfg(Lk)), 0) == 0
         assert lib.echo_cross_attention(ctypes.byref(cfg(Lk)), *[FAKE] * 6, FAKE, 1 << 40, None) == EUNSUP
+
+
+class _AsOnDevice(torch.Tensor):
+    """A host tensor that says it is on the device: the checks of a call run as for
+    one that is, and nothing is launched."""
+    is_cuda = property(lambda self: True)
+
+    @staticmethod
+    def of(*shape, dtype=torch.bfloat16):
+        """Of any size, in the memory of one row."""
+        return torch.zeros(shape[-1], dtype=dtype).expand(*shape).as_subclass(_AsOnDevice)
+
+
+def test_binding_refuses_counts_that_32_bits_would_wrap():
+    """2^32 + 5 states are not 5."""
+    n = 2 ** 32 + 5
+    q = _AsOnDevice.of(1, 2, 1, 64)
+    few, many = _AsOnDevice.of(1, 5, 1, 64), _AsOnDevice.of(1, n, 1, 64)
+    with pytest.raises(ValueError, match=r"2\^31"):
+        api.cross_attention(q, many, many)
+    with pytest.raises(ValueError, match=r"2\^31"):
+        api.cross_attention(many, few, few)
+    with pytest.raises(ValueError, match=r"2\^31"):
+        api.cross_attention(_AsOnDevice.of(n, 1, 1, 64), _AsOnDevice.of(n, 5, 1, 64), _AsOnDevice.of(n, 5, 1, 64))
+    # rows of one value each, `n` of them (a view of host memory that is never touched)
+    x = torch.zeros(1, dtype=torch.bfloat16).as_strided((1, 1), (1, 1)).expand(n, 1).as_subclass(_AsOnDevice)
+    with pytest.raises(ValueError, match=r"2\^31"):
+        api.quantize_rows(x)
+    with pytest.raises(ValueError, match=r"2\^31"):
+        api.quantize_rows(x, rows=_AsOnDevice.of(3, dtype=torch.int32))
+    with pytest.raises(ValueError, match="2.31"):
+        api.dequantize_rows(api.Int8Rows(_AsOnDevice.of(4, 128, dtype=torch.int8).contiguous().as_subclass(_AsOnDevice),
+                                         torch.zeros(4).as_subclass(_AsOnDevice), 1), out=x)
+    # as many 8-bit rows (the usual case of a pitch that is the width)
+    rows = torch.empty((n, 128), dtype=torch.int8, device="meta").as_subclass(_AsOnDevice)
+    wide = api.Int8Rows(rows, torch.empty(n, device="meta").as_subclass(_AsOnDevice), 64)
+    with pytest.raises(ValueError, match="2.31"):
+        api.linear_int8(wide, wide)
