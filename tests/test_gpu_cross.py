@@ -311,3 +311,48 @@ def test_cross_attention_masks_of_very_many_elements():
     one = left.sum(1) == 1                              # a single state: its values themselves
     where = left.to(torch.uint8).argmax(1)[one]
     assert torch.equal(got[one][:, 0, 0], v[0, where, 0])
+
+
+def _raised(rise, Lq, Lk, H, dh):
+    """Queries and states along one direction: the first 32 states score 0, the others
+    `rise` (log2), all with a spread of 0.3."""
+    g = _gen(31)
+    u = torch.randn(dh, generator=g)
+    u /= u.norm()
+    c = torch.full((Lk,), float(rise))
+    c[:32] = 0
+    c += 0.3 * torch.randn(Lk, generator=g)
+    q = (8 * u + 0.05 * torch.randn(1, Lq, H, dh, generator=g)).to(BF)
+    k = (c[:, None, None] * (dh ** 0.5 * math.log(2) / 8) * u + 0.05 * torch.randn(1, Lk, H, dh, generator=g)).to(BF)
+    return q, k, torch.randn(1, Lk, H, dh, generator=g).to(BF)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("rise", [3, 4, 5, 6, 7, 8, 9])
+def test_cross_attention_scores_above_an_early_maximum(rise, dh):
+    """Later scores around the growth at which the running maximum moves."""
+    q, k, v = _raised(rise, 70, 400, 2, dh)
+    got = api.cross_attention(q.to(device()), k.to(device()), v.to(device()))
+    torch.cuda.synchronize()
+    _check(got, q, k, v, what=f"rise {rise}")
+
+
+def test_cross_attention_time_does_not_hang_on_an_early_maximum():
+    """Scores that stay 2^6 above the first ones take no longer than scores that stay
+    2^20 above: the maximum moves once for either (the slower side by half or more if
+    it does not; the least of nine runs each, in turn)."""
+    made = [tuple(t.to(device()) for t in _raised(rise, 3900, 4096, 16, 64)) for rise in (6, 20)]
+    best = [math.inf, math.inf]
+    for turn in range(11):
+        for i, (q, k, v) in enumerate(made):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            torch.cuda.synchronize()
+            start.record()
+            for _ in range(4):
+                api.cross_attention(q, k, v)
+            end.record()
+            end.synchronize()
+            if turn >= 2:
+                best[i] = min(best[i], start.elapsed_time(end))
+    say(f"  four calls: {best[0] * 1e3:.0f} us, {best[1] * 1e3:.0f} us")
+    assert best[0] <= 1.3 * best[1]
