@@ -500,12 +500,25 @@ def _block_partial_int8(p: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int,
         raise ValueError("H must divide D")
     for n in ("bq", "bk", "bv", "bo", "b1", "b2"):
         _dev(p[n], n, x.dtype)
+    for n in MATRIX_NAMES:
+        if not isinstance(p[n], Int8Rows):
+            raise TypeError(f"{n} must be Int8Rows as wq is (see quantize_block)")
+    F = len(p["w1"])
+    for n, shape in zip(MATRIX_NAMES, ((D, D), (D, D), (D, D), (D, D), (F, D), (D, F))):
+        if (len(p[n]), p[n].cols) != shape:
+            raise ValueError(f"{n} must be {list(shape)}")
     if y_sel is None:
         y_sel = torch.empty((max(n_sel, 1), D), dtype=torch.float32, device=x.device)
+    else:
+        m, d, _ = _rows_of(y_sel, "y_sel", torch.float32)
+        if m < n_sel or d != D:
+            raise ValueError(f"y_sel must be [{n_sel} or more, {D}]")
     y = y_sel[:n_sel]
     if n_sel == 0:
         return y
-    rows = _dev(idx, "idx", torch.int32)[:n_sel]
+    if _dev(idx, "idx", torch.int32).dim() != 1 or idx.numel() < n_sel:
+        raise ValueError(f"idx must hold {n_sel} tokens")
+    rows = idx[:n_sel]
     mod, dt = p["mod"], x.dtype
     a = quantize_rows(x, shift=mod[0], scale=mod[1], ln_eps=ln_eps)
     a_sel = quantize_rows(x, rows=rows, shift=mod[0], scale=mod[1], ln_eps=ln_eps)

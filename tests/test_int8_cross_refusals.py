@@ -198,3 +198,20 @@ def test_binding_refuses_counts_that_32_bits_would_wrap():
     wide = api.Int8Rows(rows, torch.empty(n, device="meta").as_subclass(_AsOnDevice), 64)
     with pytest.raises(ValueError, match="2.31"):
         api.linear_int8(wide, wide)
+
+
+def test_int8_block_refuses_before_any_launch():
+    """An output of another type, width or too few rows, too few indices, matrices that
+    are no codes or of other shapes."""
+    D, F, L = 128, 256, 6
+    on = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt).as_subclass(_AsOnDevice)  # noqa: E731
+    w = lambda n, k: api.Int8Rows(on(n, k, dt=torch.int8), on(n, dt=torch.float32), k)  # noqa: E731
+    p = {"wq": w(D, D), "wk": w(D, D), "wv": w(D, D), "wo": w(D, D), "w1": w(F, D), "w2": w(D, F),
+         "bq": on(D), "bk": on(D), "bv": on(D), "bo": on(D), "b1": on(F), "b2": on(D), "mod": on(6, D, dt=torch.float32)}
+    x, idx = on(L, D), on(L, dt=torch.int32)
+    y = on(L, D, dt=torch.float32)
+    for kw in (dict(y_sel=on(L, D)), dict(y_sel=y[:, :64]), dict(y_sel=y[:3]), dict(idx=idx[:3]), dict(idx=on(L, 1, dt=torch.int32)),
+               dict(idx=on(L, dt=torch.int64)), dict(wk=on(D, D)), dict(w1=w(F, F)), dict(w2=w(D, D)), dict(wo=w(F, D))):
+        q = {**p, **{n: t for n, t in kw.items() if n in p}}
+        with pytest.raises((ValueError, TypeError), match=next(iter(kw))):
+            api.block_partial(q, x, kw.get("idx", idx), 4, 1, y_sel=kw.get("y_sel", y))
