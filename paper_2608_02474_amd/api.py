@@ -21,6 +21,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import math
 
 import torch
 
@@ -82,12 +83,28 @@ class Workspace:
 
     def __init__(self):
         self.buf = None
+        self._laid_out = None   # (key, tensors) of the last `pieces`
 
     def get(self, nbytes: int, device) -> torch.Tensor:
         nbytes = max(int(nbytes), 256)
         if self.buf is None or self.buf.numel() < nbytes or self.buf.device != device:
             self.buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+            self._laid_out = None
         return self.buf
+
+    def pieces(self, key: tuple, specs, device) -> list:
+        """Tensors of the (shape, dtype) that specs() gives, one behind the other at
+        multiples of 256 bytes; laid out again only where key (what the specs follow
+        from) is not the last one's."""
+        if self._laid_out is None or self._laid_out[0] != key or self.buf.device != device:
+            spans, at = [], 0
+            for shape, dtype in specs():
+                n = math.prod(shape) * dtype.itemsize
+                spans.append((at, at + n, dtype, shape))
+                at += (n + 255) // 256 * 256
+            buf = self.get(at, device)
+            self._laid_out = key, [buf[a:b].view(dtype).view(shape) for a, b, dtype, shape in spans]
+        return self._laid_out[1]
 
 
 _WS = {"energy": Workspace(), "select": Workspace(), "block": Workspace()}
@@ -439,11 +456,12 @@ def block_partial(params: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int, 
                   batch_invariant: bool = False):
     """y_sel [n_sel, D] fp32 = block output of tokens idx[:n_sel].  With
     batch_invariant, each row is bit-identical for any selection containing it.
-    With weights in 8 bits (quantize_block) the block runs on 8-bit rows."""
+    With weights in 8 bits (quantize_block) the block runs on 8-bit rows; without a
+    workspace its intermediate tensors are then the call's own."""
     if is_int8_block(params):
         if batch_invariant:
             raise ValueError("batch_invariant does not go with weights in 8 bits")
-        return _block_partial_int8(params, x, idx, n_sel, H, ln_eps, y_sel)
+        return _block_partial_int8(params, x, idx, n_sel, H, ln_eps, y_sel, workspace)
     lib = _lib_handle()
     _dev(x, "x")
     _dev(idx, "idx", torch.int32)
@@ -485,10 +503,31 @@ def is_int8_block(params: dict) -> bool:
     return isinstance(params["wq"], Int8Rows)
 
 
+def _int8_block_pieces(L: int, n: int, D: int, F: int, H: int, dt) -> tuple:
+    """(shape, dtype) of what _block_partial_int8 holds between its calls, and of
+    their scratch: products' partial sums and ranges of the attention (the sizes
+    asked for here fix both; a call that needed more would take its own)."""
+    lib, f32, i8 = _lib_handle(), torch.float32, torch.int8
+    pd, pf = (D + 127) // 128 * 128, (F + 127) // 128 * 128
+    scratch = 256
+    for M, N, K in ((n, D, D), (L, D, D), (n, F, D), (n, D, F)):
+        cfg = LinearInt8Cfg(M, N, K, _lib.ECHO_LINEAR_NONE, ECHO_F32, ECHO_F32, ECHO_F32, 0, pd if K == D else pf,
+                            pd if K == D else pf, N, 0)
+        scratch = max(scratch, lib.echo_linear_int8_workspace(ctypes.byref(cfg)))
+    qs, ks = (n * D, D, D // H), (L * D, D, D // H)
+    cfg = CrossAttentionCfg(1, n, L, H, H, D // H, _DTYPES[dt], (D // H) ** -0.5, qs, ks, ks, qs)
+    scratch = max(scratch, lib.echo_cross_attention_workspace(ctypes.byref(cfg), 0))
+    return (((L, pd), i8), ((L,), f32), ((n, pd), i8), ((n,), f32), ((n, pf), i8), ((n,), f32),
+            ((n, D), dt), ((L, D), dt), ((L, D), dt), ((1, n, H, D // H), dt), ((n, D), f32), ((n, F), dt),
+            ((scratch,), torch.uint8))
+
+
 def _block_partial_int8(p: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int, H: int, ln_eps: float,
-                        y_sel: torch.Tensor | None) -> torch.Tensor:
+                        y_sel: torch.Tensor | None, workspace: Workspace | None) -> torch.Tensor:
     """block_partial on 8-bit rows: the tokens are quantized in front of every
-    product, one scale a token; attention, residuals and LayerNorms as there."""
+    product, one scale a token; attention, residuals and LayerNorms as there.
+    What it holds in between lies in the workspace, or else is allocated by the
+    calls themselves."""
     if n_sel < 0 or H < 1:
         check("echo_block_partial", _lib.ECHO_EINVAL)
     _dev(x, "x")
@@ -519,18 +558,28 @@ def _block_partial_int8(p: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int,
     if _dev(idx, "idx", torch.int32).dim() != 1 or idx.numel() < n_sel:
         raise ValueError(f"idx must hold {n_sel} tokens")
     rows = idx[:n_sel]
-    mod, dt = p["mod"], x.dtype
-    a = quantize_rows(x, shift=mod[0], scale=mod[1], ln_eps=ln_eps)
-    a_sel = quantize_rows(x, rows=rows, shift=mod[0], scale=mod[1], ln_eps=ln_eps)
-    q = linear_int8(a_sel, p["wq"], p["bq"], dtype=dt).view(1, n_sel, H, D // H)
-    k = linear_int8(a, p["wk"], p["bk"], dtype=dt).view(1, L, H, D // H)
-    v = linear_int8(a, p["wv"], p["bv"], dtype=dt).view(1, L, H, D // H)
-    o = cross_attention(q, k, v).view(n_sel, D)
-    x1 = linear_int8(quantize_rows(o), p["wo"], p["bo"], gate=mod[2], residual=x, residual_rows=rows,
-                     dtype=torch.float32)
-    b = quantize_rows(x1, shift=mod[3], scale=mod[4], ln_eps=ln_eps)
-    h = linear_int8(b, p["w1"], p["b1"], activation="gelu", dtype=dt)
-    return linear_int8(quantize_rows(h), p["w2"], p["b2"], gate=mod[5], residual=x1, out=y)
+    mod, dt, dh = p["mod"], x.dtype, D // H
+    a8 = s8 = h8 = q = k = v = o = x1 = h = scratch = None
+    if workspace is not None:
+        _echo_dtype(x)
+        ac, asc, sc, ssc, hc, hsc, q, k, v, o, x1, h, part = workspace.pieces(
+            ("int8 block", L, n_sel, D, F, H, dt), lambda: _int8_block_pieces(L, n_sel, D, F, H, dt), x.device)
+        # (the selected rows' codes: of the input, then of the attention's output, then of x1)
+        a8, s8, h8 = Int8Rows(ac, asc, D), Int8Rows(sc, ssc, D), Int8Rows(hc, hsc, F)
+        scratch = Workspace()
+        scratch.buf = part
+    a = quantize_rows(x, shift=mod[0], scale=mod[1], ln_eps=ln_eps, out=a8)
+    a_sel = quantize_rows(x, rows=rows, shift=mod[0], scale=mod[1], ln_eps=ln_eps, out=s8)
+    q = linear_int8(a_sel, p["wq"], p["bq"], dtype=dt, out=q, workspace=scratch).view(1, n_sel, H, dh)
+    k = linear_int8(a, p["wk"], p["bk"], dtype=dt, out=k, workspace=scratch).view(1, L, H, dh)
+    v = linear_int8(a, p["wv"], p["bv"], dtype=dt, out=v, workspace=scratch).view(1, L, H, dh)
+    o = cross_attention(q, k, v, out=o, workspace=scratch).view(n_sel, D)
+    x1 = linear_int8(quantize_rows(o, out=s8), p["wo"], p["bo"], gate=mod[2], residual=x, residual_rows=rows,
+                     dtype=torch.float32, out=x1, workspace=scratch)
+    b = quantize_rows(x1, shift=mod[3], scale=mod[4], ln_eps=ln_eps, out=s8)
+    h = linear_int8(b, p["w1"], p["b1"], activation="gelu", dtype=dt, out=h, workspace=scratch)
+    return linear_int8(quantize_rows(h, out=h8), p["w2"], p["b2"], gate=mod[5], residual=x1, out=y,
+                       workspace=scratch)
 
 
 # ----------------------------------------------------------- Wan-style block

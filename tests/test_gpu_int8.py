@@ -516,3 +516,82 @@ def test_linear_int8_random_shapes(seed):
     torch.cuda.synchronize()
     assert (buf[:, N:] == 5).all()
     _check_linear(y.cpu(), a, w, K, bias, out_dtype, act=act, gate=gate, res=res, what=f"{M}x{N}x{K} kind {kind}")
+
+
+# ------------------------------------------------ the block, its workspace and graphs
+
+def _block_of(L, D, H, F, dt, seed):
+    """Weights in dt and in 8 bits, tokens."""
+    g = _gen(seed)
+    P = {n: _rand(g, *s) * s[1] ** -0.5 for n, s in (("wq", (D, D)), ("wk", (D, D)), ("wv", (D, D)), ("wo", (D, D)),
+                                                    ("w1", (F, D)), ("w2", (D, F)))}
+    P.update({n: _rand(g, F if n == "b1" else D) * 0.02 for n in ("bq", "bk", "bv", "bo", "b1", "b2")})
+    P = {n: t.to(dt).to(device()) for n, t in P.items()}
+    mod = _rand(g, 6, D) * 0.1
+    mod[2] += 0.25
+    mod[5] += 0.25
+    P["mod"] = mod.to(device())
+    return P, api.quantize_block(P), _rand(g, L, D, dtype=dt).to(device())
+
+
+@pytest.mark.parametrize("L,D,H,F,dt", [(300, 256, 2, 512, torch.bfloat16), (2101, 512, 4, 1300, torch.bfloat16),
+                                        (333, 200, 5, 300, torch.float32)])
+def test_block_in_8_bits_lives_in_its_workspace(L, D, H, F, dt):
+    """With a workspace that has grown once the block allocates nothing, whatever ran in
+    it in between, and its rows are those of a call without one."""
+    _, Q, x = _block_of(L, D, H, F, dt, 3)
+    idx = torch.randperm(L, generator=_gen(4)).to(torch.int32).to(device())
+    ws = api.Workspace()
+    counts = (L, 1, L // 3, 20)
+    want = {n: api.block_partial(Q, x, idx, n, H) for n in counts}
+    y = torch.empty(L, D, device=device())
+    api.block_partial(Q, x, idx, L, H, y_sel=y, workspace=ws)
+    assert ws.buf is not None
+    for n in counts:
+        api.block_partial(Q, x, idx, n, H, y_sel=y, workspace=ws)
+    held = ws.buf.data_ptr()
+    for n in counts + counts[::-1]:
+        ws.buf.fill_(0x7f)
+        y.fill_(5.0)
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_stats()["allocation.all.allocated"]
+        got = api.block_partial(Q, x, idx, n, H, y_sel=y, workspace=ws)
+        assert torch.cuda.memory_stats()["allocation.all.allocated"] == before, n
+        assert ws.buf.data_ptr() == held
+        assert torch.equal(got, want[n]) and (y[n:] == 5).all(), n
+    # another block's larger needs: the pieces follow the buffer
+    ws.get(ws.buf.numel() + 1, device())
+    assert torch.equal(api.block_partial(Q, x, idx, 20, H, workspace=ws), want[20])
+
+
+def test_block_in_8_bits_and_in_16_share_a_workspace():
+    L, D, H, F = 500, 256, 2, 512
+    P, Q, x = _block_of(L, D, H, F, torch.bfloat16, 8)
+    idx = torch.arange(0, L, 3, dtype=torch.int32, device=device())
+    n, ws = len(idx), api.Workspace()
+    want16, want8 = api.block_partial(P, x, idx, n, H), api.block_partial(Q, x, idx, n, H)
+    for turn in range(3):
+        assert torch.equal(api.block_partial(Q, x, idx, n, H, workspace=ws), want8), turn
+        assert torch.equal(api.block_partial(P, x, idx, n, H, workspace=ws), want16), turn
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_block_in_8_bits_captured(given):
+    """The whole block in a graph, replayed on changing tokens between eager calls of
+    the same weights, with a workspace of its own or the call's."""
+    L, D, H, F = 1200, 512, 4, 1024
+    _, Q, x = _block_of(L, D, H, F, torch.bfloat16, 6)
+    idx = torch.arange(0, L, 2, dtype=torch.int32, device=device())
+    ws = api.Workspace() if given else None
+    api.block_partial(Q, x, idx, len(idx), H, workspace=ws)
+    torch.cuda.synchronize()
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr):
+        y = api.block_partial(Q, x, idx, len(idx), H, workspace=ws)
+    for turn in range(4):
+        x.mul_(-0.7)
+        idx.copy_((idx + 1) % L)
+        gr.replay()
+        want = api.block_partial(Q, x, idx, len(idx), H)
+        torch.cuda.synchronize()
+        assert torch.isfinite(y).all() and torch.equal(y, want), turn

@@ -215,3 +215,22 @@ def test_int8_block_refuses_before_any_launch():
         q = {**p, **{n: t for n, t in kw.items() if n in p}}
         with pytest.raises((ValueError, TypeError), match=next(iter(kw))):
             api.block_partial(q, x, kw.get("idx", idx), 4, 1, y_sel=kw.get("y_sel", y))
+
+
+def test_workspace_pieces():
+    """Pieces lie apart at multiples of 256 bytes, stay for the same key, and are laid
+    out again for another one and where the buffer has grown under them."""
+    ws, cpu = api.Workspace(), torch.device("cpu")
+    specs = (((3, 5), torch.float32), ((7,), torch.int8), ((1, 2, 3), torch.bfloat16), ((300,), torch.uint8))
+    calls = []
+    lay = lambda key: ws.pieces(key, lambda: calls.append(key) or specs, cpu)  # noqa: E731
+    one = lay("a")
+    assert [(tuple(t.shape), t.dtype) for t in one] == list(specs)
+    starts = [t.data_ptr() - ws.buf.data_ptr() for t in one]
+    assert starts == [0, 256, 512, 768] and ws.buf.numel() == 768 + 512
+    assert lay("a") is one and calls == ["a"]
+    two = lay("b")
+    assert two is not one and [t.data_ptr() for t in two] == [t.data_ptr() for t in one]   # the same buffer
+    ws.get(1 << 20, cpu)
+    three = lay("b")
+    assert calls == ["a", "b", "b"] and three[0].data_ptr() == ws.buf.data_ptr()
