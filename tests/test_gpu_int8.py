@@ -595,3 +595,20 @@ def test_block_in_8_bits_captured(given):
         want = api.block_partial(Q, x, idx, len(idx), H)
         torch.cuda.synchronize()
         assert torch.isfinite(y).all() and torch.equal(y, want), turn
+
+
+@pytest.mark.parametrize("L,n,D,H,F,dt", [(2500, 901, 512, 4, 1300, torch.bfloat16), (1111, 1111, 640, 5, 2100, torch.bfloat16),
+                                          (1500, 333, 264, 3, 1000, torch.float32)])
+def test_block_in_8_bits_of_many_tokens(L, n, D, H, F, dt):
+    """Tiles, splits and ragged ends together, some tokens more than once: against the
+    64-bit block on the same weights, by the tolerance above."""
+    P, Q, x = _block_of(L, D, H, F, dt, L)
+    idx = torch.randint(0, L, (n,), generator=_gen(n), dtype=torch.int32)
+    idx[1] = idx[0]
+    y = api.block_partial(Q, x, idx.to(device()), n, H)
+    torch.cuda.synchronize()
+    want = _block_oracle(P, Q, x, idx.long(), H)
+    off = y.cpu().double() - want
+    say(f"  8-bit block {L} tokens, {n} of them, {dt}: max {float(off.abs().max()):.2e}, rel {float(off.norm() / want.norm()):.2e}")
+    assert float(off.abs().max()) <= 2e-2 and float(off.norm() / want.norm()) <= 1e-2
+    assert torch.equal(y[0], y[1])
