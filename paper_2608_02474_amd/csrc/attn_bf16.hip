@@ -110,16 +110,6 @@ __device__ __forceinline__ T& pick2(T& a, T& b) {
     return b;
 }
 
-__device__ __forceinline__ float pair_max(float x) {
-  // max over lanes l and l^32
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float pair_sum(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
 // ---- work lists.  Items are (head, query tile) pairs in "full first"
 // order: item i < nf is full tile i % ntqf of head i / ntqf (ntqf = Mq / kQ
 // full tiles per head), item i >= nf the last, partly filled tile of head

@@ -48,16 +48,6 @@ constexpr float X_GROW = 8.0f;              // log2 of the growth that moves the
 constexpr float X_GROW_SUM = 256.0f;        // sum of 16 weights that does (bf16)
 constexpr float X_LOW = -3.402823466e38f;   // the maximum before any state: the lowest finite value
 
-// maximum and sum over lanes l and l ^ 32
-__device__ __forceinline__ float x_pair_max(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float x_pair_sum(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
 __device__ __forceinline__ int x_swap23(int r) { return (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
 
 // K row r (2 DH bytes in chunks of 16): chunk c lives in slot c ^ x_kx(r); the 16
@@ -338,7 +328,7 @@ __global__ void __launch_bounds__(256, 2) cross_bf16(CrossArgs p) {
       float mx = sc[0];
 #pragma unroll
       for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-      mx = x_pair_max(mx) * p.scale_log2;
+      mx = pair_max(mx) * p.scale_log2;
       const bool grow = mx > mc;
       const float alpha = grow ? __builtin_amdgcn_exp2f(mc - mx) : 1.0f;
       mc = grow ? mx : mc;
@@ -420,7 +410,7 @@ __global__ void __launch_bounds__(256, 2) cross_bf16(CrossArgs p) {
       values(u, 1);
     }
   }
-  const float lsum = x_pair_sum(l_run);
+  const float lsum = pair_sum(l_run);
   if (p.nsplit > 1) {
     if (idle) return;
     if (row0 + l32 >= rows) return;
@@ -532,7 +522,7 @@ __global__ void __launch_bounds__(256) cross_f32(CrossArgs p) {
         if (8 * (e / 4) + 4 * hi + e % 4 >= left) sc[e] = -INFINITY;
         mx = fmaxf(mx, sc[e]);
       }
-      mx = x_pair_max(mx) * p.scale_log2;
+      mx = pair_max(mx) * p.scale_log2;
       const bool grow = mx - mc > X_GROW;
       if (__ballot(grow) != 0ull) {
         const float alpha = grow ? __builtin_amdgcn_exp2f(mc - mx) : 1.0f;
@@ -558,7 +548,7 @@ __global__ void __launch_bounds__(256) cross_f32(CrossArgs p) {
     }
     __syncthreads();
   }
-  const float lsum = x_pair_sum(l_run);
+  const float lsum = pair_sum(l_run);
   if (p.nsplit > 1) {
     if (!mine) return;
     const int64_t units = x_units(p, tiles), u = x_unit(p, x, tiles, wave * 32 + l32);

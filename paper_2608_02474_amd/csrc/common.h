@@ -16,6 +16,15 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kWave = 64;
 
+// f(integral_constant<int, I>) for I = B .. E-1, unrolled at compile time
+template <int B, int E, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (B < E) {
+    f(std::integral_constant<int, B>{});
+    static_for<B + 1, E>(f);
+  }
+}
+
 __device__ __forceinline__ float bf16_to_f32(bf16_t b) {
   return __uint_as_float(static_cast<uint32_t>(b) << 16);
 }
@@ -134,6 +143,30 @@ template <> struct Raw8<float> {
   }
 };
 
+// GELU with the tanh approximation, using 0.5 z (1 + tanh u) = z / (1 + e^{-2u})
+// with u = sqrt(2/pi) (z + 0.044715 z^3): e^{-2u} = 2^{z (k1 + k2 z^2)}, k1 =
+// -2 sqrt(2/pi) log2(e), k2 = 0.044715 k1, so the argument is one FMA and two
+// products (the unfolded form took six products, an FMA and an add per
+// element).  exp2 and the reciprocal are the hardware ones (1 ulp), far below
+// the bf16 rounding of the result; z -> -inf gives z * 0, z -> +inf gives z.
+__device__ __forceinline__ float gelu_tanh_fast(float z) {
+  constexpr double kU = 0.7978845608028654 * 1.4426950408889634;  // sqrt(2/pi) log2(e)
+  constexpr float k1 = static_cast<float>(-2.0 * kU), k2 = static_cast<float>(-2.0 * kU * 0.044715);
+  const float e = __builtin_amdgcn_exp2f(z * fmaf(k2, z * z, k1));
+  return z * __builtin_amdgcn_rcpf(1.0f + e);
+}
+
+// Grouped tile order: 8 tile-rows at a time, down the rows first, so that
+// consecutive tiles share B panels and a run of them shares A panels in L2.
+__host__ __device__ __forceinline__ void gemm_tile_of(int pid, int tm, int tn, int& tile_m, int& tile_n) {
+  constexpr int GROUP = 8;
+  const int group_size = GROUP * tn;
+  const int first_m = (pid / group_size) * GROUP;
+  const int gm = (tm - first_m) < GROUP ? (tm - first_m) : GROUP;
+  tile_m = first_m + (pid % group_size) % gm;
+  tile_n = (pid % group_size) / gm;
+}
+
 // wave64 reductions (every lane gets the result).  The partner at lane
 // distance 32 and 16 comes from the gfx950 lane swaps (v_permlane32_swap,
 // v_permlane16_swap: both halves of a pair in two registers), those at 8, 4,
@@ -188,6 +221,16 @@ __device__ __forceinline__ double wave_sum(double v) {
   v = ror(v, std::integral_constant<int, 2>{});
   v = ror(v, std::integral_constant<int, 1>{});
   return v;
+}
+
+// maximum and sum over lanes l and l ^ 32
+__device__ __forceinline__ float pair_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float pair_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
 // Direct global-to-LDS copy of 16 bytes per lane (global_load_lds_dwordx4):

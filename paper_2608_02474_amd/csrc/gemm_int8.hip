@@ -29,22 +29,6 @@ namespace echo {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-template <int B, int E, typename F>
-__device__ __forceinline__ void i8_for(F&& f) {
-  if constexpr (B < E) {
-    f(std::integral_constant<int, B>{});
-    i8_for<B + 1, E>(f);
-  }
-}
-
-// 0.5 z (1 + tanh u) = z / (1 + 2^(z (k1 + k2 z^2))), as in the bf16 products
-__device__ __forceinline__ float i8_gelu(float z) {
-  constexpr double kU = 0.7978845608028654 * 1.4426950408889634;
-  constexpr float k1 = static_cast<float>(-2.0 * kU), k2 = static_cast<float>(-2.0 * kU * 0.044715);
-  const float e = __builtin_amdgcn_exp2f(z * fmaf(k2, z * z, k1));
-  return z * __builtin_amdgcn_rcpf(1.0f + e);
-}
-
 __device__ __forceinline__ float i8_load(const void* p, int bf, int64_t i) {
   return bf ? bf16_to_f32(static_cast<const bf16_t*>(p)[i]) : static_cast<const float*>(p)[i];
 }
@@ -52,7 +36,7 @@ __device__ __forceinline__ float i8_load(const void* p, int bf, int64_t i) {
 // z -> f(z), res being the residual and gate the channel's gate
 template <int EPI>
 __device__ __forceinline__ float i8_finish(float z, float gate, float res) {
-  if constexpr (EPI == EPI_GELU) return i8_gelu(z);
+  if constexpr (EPI == EPI_GELU) return gelu_tanh_fast(z);
   if constexpr (EPI == EPI_GATE_RES) return fmaf(gate, z, res);
   return z;
 }
@@ -179,16 +163,6 @@ __device__ __forceinline__ void i8_put4(const GemmI8Args& p, int m, int n, const
   i8_store4<EPI, CBF>(p, m, n, za, cols, res);
 }
 
-// Grouped order: 8 tile-rows at a time, down the rows first.
-__device__ __forceinline__ void i8_tile_of(int pid, int tm, int tn, int& tile_m, int& tile_n) {
-  constexpr int GROUP = 8;
-  const int group_size = GROUP * tn;
-  const int first_m = (pid / group_size) * GROUP;
-  const int gm = (tm - first_m) < GROUP ? (tm - first_m) : GROUP;
-  tile_m = first_m + (pid % group_size) % gm;
-  tile_n = (pid % group_size) / gm;
-}
-
 // RBF: the residual is bf16
 template <int BM, int BN, int EPI, bool CBF, bool RBF>
 __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_i8_tile(GemmI8Args p) {
@@ -221,7 +195,7 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_i8_tile(Ge
     pid = loc < XW * full_waves ? (loc / XW) * 8 * XW + xcd * XW + loc % XW : g;
   }
   int tile_m, tile_n;
-  i8_tile_of(pid, tm, tn, tile_m, tile_n);
+  gemm_tile_of(pid, tm, tn, tile_m, tile_n);
   const int m0 = tile_m * BM, n0 = tile_n * BN;
   const int nk_all = p.K / 128, kt0 = ks * p.kps;
   const int nk = split && nk_all - kt0 >= p.kps ? p.kps : nk_all - kt0;  // >= 1
@@ -272,7 +246,7 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_i8_tile(Ge
     for (int j = 0; j < TJ; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
   auto mma = [&](auto set_c, auto t0_c, auto t1_c) __attribute__((always_inline)) {
     constexpr int SET = decltype(set_c)::value;
-    i8_for<decltype(t0_c)::value, decltype(t1_c)::value>([&](auto t_c) __attribute__((always_inline)) {
+    static_for<decltype(t0_c)::value, decltype(t1_c)::value>([&](auto t_c) __attribute__((always_inline)) {
       constexpr int T = decltype(t_c)::value;
       acc[T / TJ][T % TJ] =
           __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[SET][T % TJ], fa[SET][T / TJ], acc[T / TJ][T % TJ], 0, 0, 0);
@@ -286,7 +260,7 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_i8_tile(Ge
   // next k-step and the barrier; the rest, with the next k-step's first reads
   // and the copies of the k-step after next into the stage just released.
   auto phase0 = [&](const char* st) __attribute__((always_inline)) {
-    i8_for<0, NR>([&](auto q_c) __attribute__((always_inline)) {
+    static_for<0, NR>([&](auto q_c) __attribute__((always_inline)) {
       constexpr int Q = decltype(q_c)::value;
       __builtin_amdgcn_sched_barrier(0);
       read(S1{}, q_c, st);
@@ -297,23 +271,23 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_i8_tile(Ge
     __builtin_amdgcn_sched_barrier(0);
   };
   set_fill(0);
-  i8_for<0, NCP>(copy);
+  static_for<0, NCP>(copy);
   set_fill(1);
-  i8_for<0, NCP>(copy);
+  static_for<0, NCP>(copy);
   __builtin_amdgcn_s_waitcnt(waitcnt_vm(NCP));
   __syncthreads();
-  i8_for<0, NR>([&](auto q_c) __attribute__((always_inline)) { read(S0{}, q_c, smem); });
+  static_for<0, NR>([&](auto q_c) __attribute__((always_inline)) { read(S0{}, q_c, smem); });
   phase0(smem);
   for (int kt = 0; kt + 1 < nk; ++kt) {
     const char* nxt = smem + ((kt & 1) ^ 1) * kStage;
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));  // this wave's copies of k-step kt + 1
     __syncthreads();
     set_fill(kt + 2);
-    i8_for<0, NR>([&](auto q_c) __attribute__((always_inline)) {
+    static_for<0, NR>([&](auto q_c) __attribute__((always_inline)) {
       constexpr int Q = decltype(q_c)::value, M1 = NM - Mid::value;
       __builtin_amdgcn_sched_barrier(0);
       read(S0{}, q_c, nxt);
-      i8_for<Q * NCP / NR, (Q + 1) * NCP / NR>(copy);
+      static_for<Q * NCP / NR, (Q + 1) * NCP / NR>(copy);
       mma(S1{}, std::integral_constant<int, Mid::value + Q * M1 / NR>{},
           std::integral_constant<int, Mid::value + (Q + 1) * M1 / NR>{});
     });
@@ -373,12 +347,12 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_i8_tile(Ge
       }
     }
   };
-  i8_for<0, NPF>(fetch);
-  i8_for<0, TI>([&](auto i_c) __attribute__((always_inline)) {
+  static_for<0, NPF>(fetch);
+  static_for<0, TI>([&](auto i_c) __attribute__((always_inline)) {
     constexpr int i = decltype(i_c)::value;
     const int mi = m0 + wm * WM + i * 16 + rl;
     fetch(std::integral_constant<int, i + NPF>{});
-    i8_for<0, TJ>([&](auto j_c) __attribute__((always_inline)) {
+    static_for<0, TJ>([&](auto j_c) __attribute__((always_inline)) {
       constexpr int j = decltype(j_c)::value;
       // (the empty asm keeps the compiler from moving all accumulators into
       // vector registers at once ahead of the epilogue: 29 to 77 spilled)
@@ -418,7 +392,7 @@ __global__ void __launch_bounds__(256) gemm_i8_reduce(GemmI8Args p) {
   const int t = static_cast<int>(e / (static_cast<int64_t>(BM) * (BN / 4)));
   if (p.tile_base + t >= tm * tn) return;
   int tile_m, tile_n;
-  i8_tile_of(p.tile_base + t, tm, tn, tile_m, tile_n);
+  gemm_tile_of(p.tile_base + t, tm, tn, tile_m, tile_n);
   const int m = tile_m * BM + r, n = tile_n * BN + 4 * c4;
   if (m >= p.M || n >= p.N) return;
   i32x4 acc = {0, 0, 0, 0};
