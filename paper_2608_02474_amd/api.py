@@ -79,7 +79,9 @@ def _echo_dtype(t: torch.Tensor) -> int:
 
 
 class Workspace:
-    """A growable device byte buffer reused across calls."""
+    """A growable device byte buffer reused across calls (of one stream; a graph that
+    was captured with it needs it as it was, so it must not grow before the last
+    replay)."""
 
     def __init__(self):
         self.buf = None
@@ -896,7 +898,8 @@ def linear_int8(a: Int8Rows, w: Int8Rows, bias: torch.Tensor | None = None, acti
                 out: torch.Tensor | None = None, workspace: Workspace | None = None) -> torch.Tensor:
     """Linear layer on 8-bit rows (echo_linear_int8): a [M tokens], w [N channels]
     -> [M, N] in dtype.  activation: None or "gelu" (tanh form); or gate (fp32
-    [N]) and residual ([rows, N], picked by residual_rows): residual + gate * y."""
+    [N]) and residual ([rows, N], picked by residual_rows): residual + gate * y.
+    out overlaps no input; without residual_rows it may be the residual itself."""
     lib = _lib_handle()
     M, lda = _int8_rows(a, "a")
     N, ldw = _int8_rows(w, "w")
@@ -980,10 +983,15 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: to
                     key_mask: torch.Tensor | None = None, scale: float | None = None,
                     out: torch.Tensor | None = None, workspace: Workspace | None = None) -> torch.Tensor:
     """Attention of q [B, Lq, H, dh] to the states k, v [B, Lk, Hkv, dh]
-    (echo_cross_attention; any strides with contiguous dh): the first k_len[b]
-    (int32 [B]) states that key_mask (uint8 or bool [B, Lk]) leaves; a query
-    without any gets zeros.  scale: 1 / sqrt(dh) by default.  Returns
-    [B, Lq, H, dh]."""
+    (echo_cross_attention): the first k_len[b] (int32 [B]) states that key_mask
+    (uint8 or bool [B, Lk]) leaves; a query without any gets zeros.  bf16 with dh
+    64 or 128, fp32 with dh a multiple of 4 up to 128.  scale: 1 / sqrt(dh) by
+    default.  Returns [B, Lq, H, dh].
+
+    dh is contiguous; elements, rows and heads lie any multiple of 16 bytes apart
+    (0 too, but for out), every tensor starts at one, and rows of k and v are less
+    than 2^24 values apart; other layouts are refused.  out overlaps no input and
+    holds no row twice."""
     lib = _lib_handle()
     shape, qs = _heads_of(q, "q")
     kshape, ks = _heads_of(k, "k", q.dtype)

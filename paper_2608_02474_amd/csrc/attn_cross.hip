@@ -279,7 +279,10 @@ __global__ void __launch_bounds__(256, 2) cross_bf16(CrossArgs p) {
   // The states pass in halves of 32: while the matrix cores compute the scores
   // of one half, the vector units turn those of the half before it into
   // probabilities, which then weigh V.  LDS reads are issued
-  // X_RING MFMAs ahead.
+  // X_RING MFMAs ahead.  The probabilities enter the second product in bf16, the
+  // type its instruction takes: an output is then within 0.0022 to 0.0024 of the
+  // 64-bit one in the 2-norm, 0.0017 of it the output's own rounding.  Kept to
+  // more bits, as a second bf16 number each, they would take that product twice.
   bf16x8 pf[2];
   float psum;
   auto weigh = [&](const f32x16& sc, int c) __attribute__((always_inline)) {  // scores 2 c, 2 c + 1
