@@ -820,15 +820,17 @@ def _int8_rows(r: Int8Rows, name: str) -> tuple:
             and c.dtype == torch.int8 and s.dtype == torch.float32):
         n, width = c.shape
         ld, unit = c.stride()
-        if (unit == 1 and ld >= width >= r.cols and ld % 128 == 0 and width % 128 == 0 and 0 < r.cols <= 65536
+        if n <= 1:
+            ld = width   # no next row: whatever stride the tensor has is not one
+        if (unit == 1 and 65536 >= ld >= width >= r.cols and ld % 128 == 0 and width % 128 == 0 and 0 < r.cols <= 65536
                 and s.shape == (n,) and s.is_contiguous() and n <= _MAX_COUNT):
             return n, ld
     # not the usual case: the other checks say what is wrong, or take it
     n, width, ld = _rows_of(c, f"{name}.codes", torch.int8)
     _vector(s, f"{name}.scale", n, torch.float32)
     pitch = (r.cols + 127) // 128 * 128
-    if not 1 <= r.cols <= 65536 or width < pitch or ld % 128 or width % 128:
-        raise ValueError(f"{name}.codes must have a pitch of {pitch} bytes or a larger multiple of 128")
+    if not 1 <= r.cols <= 65536 or width < pitch or ld % 128 or width % 128 or ld > 65536:
+        raise ValueError(f"{name}.codes must have a pitch of {pitch} bytes or a larger multiple of 128 up to 65536")
     return n, ld
 
 

@@ -234,3 +234,16 @@ def test_workspace_pieces():
     ws.get(1 << 20, cpu)
     three = lay("b")
     assert calls == ["a", "b", "b"] and three[0].data_ptr() == ws.buf.data_ptr()
+
+
+def test_pitch_of_a_single_row_is_its_width():
+    """One row of codes taken from far apart ones has a stride that no next row needs;
+    of more rows it is their pitch, at most 65536."""
+    codes = torch.zeros(400, 512, dtype=torch.int8).as_subclass(_AsOnDevice)
+    scale = torch.zeros(400).as_subclass(_AsOnDevice)
+    one, far = codes[7::300][:1], codes[::200]
+    assert one.stride(0) == 300 * 512
+    assert api._int8_rows(api.Int8Rows(one, scale[:1], 400), "a") == (1, 512)
+    assert api._int8_rows(api.Int8Rows(codes[::2], scale[:200], 400), "a") == (200, 1024)
+    with pytest.raises(ValueError, match="65536"):
+        api._int8_rows(api.Int8Rows(far, scale[:2], 400), "a")
