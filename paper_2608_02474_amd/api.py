@@ -973,8 +973,6 @@ def _heads_of(t: torch.Tensor, name: str, dtype=None) -> tuple:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.dim() == 4:
         b, n, h, d = shape = t.shape
-        if max(shape) > _MAX_COUNT:
-            raise ValueError(f"{name} must have fewer than 2^31 elements, rows and heads")
         sb, sn, sh, sd = t.stride()
         if h >= 1 and d >= 1 and (sd == 1 or d == 1):
             return shape, (sb if b > 1 else 0, sn if n > 1 else 0, sh if h > 1 else 0)
@@ -1002,6 +1000,8 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_len: to
     Bk, Lk, Hkv, dk = kshape
     if kshape != vshape or Bk != B or dk != dh or H % Hkv:
         raise ValueError("k and v must be [B, Lk, Hkv, dh] with Hkv dividing q's heads")
+    if Lk > _MAX_COUNT or Lq > _MAX_COUNT or B > _MAX_COUNT or H > _MAX_COUNT or dh > _MAX_COUNT:
+        raise ValueError("fewer than 2^31 elements, queries, states and heads")
     if k_len is not None:
         _vector(k_len, "k_len", B, torch.int32)
     if key_mask is not None:
