@@ -550,6 +550,91 @@ int echo_linear_int8(const echo_linear_int8_cfg* cfg, const int8_t* a, const flo
                      const float* w_scale, const void* bias, const float* gate, const void* residual,
                      const int32_t* residual_rows, void* c, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------- rows in 4 bits */
+/*
+ * Rows held in microscaled 4-bit floating point (the element and scale formats
+ * of the OCP Microscaling Formats specification v1.0, MXFP4): codes of one sign,
+ * two exponent and one fraction bit (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives), two a byte, the even column's in the low half; for every 32
+ * columns one scale byte, value 2^(byte - 127), 255 being NaN.
+ *
+ * echo_quantize_rows_fp4: a_i as in echo_quantize_rows; for each block b of 32
+ * columns (the last one may be shorter), with m = max_{j in b} |a_ij|:
+ *   e = max(floor(log2 m) - 2, -127), scale byte e + 127 (0 for a block of zeros)
+ *   code_ij = a_ij / 2^e rounded to the nearest of the values above, halves to
+ *             the code with a fraction bit of 0, magnitudes above 6 to 6
+ * A block with an infinity or NaN, and every block of a row with r_i outside
+ * [0, x_rows), has scale 255 and codes 0.
+ * codes (16-byte aligned): rows ldq bytes apart, scales (16-byte aligned): rows
+ * lds bytes apart; ldq a multiple of 128, at least echo_fp4_pitch(D), lds a
+ * multiple of 16, at least echo_fp4_scale_pitch(D); the first so many bytes of a
+ * row are written, with zeros behind column D, others are left as they are.
+ * x, rows, shift and scale as in echo_quantize_rows.
+ *
+ * echo_dequantize_rows_fp4: x_ij = cast(2^e code_ij), x being the output here;
+ * rows, shift and scale do not apply (x_rows is not read).
+ *
+ * Requires 1 <= D <= 65536, ldq <= 65536, lds <= 65536, 0 <= M; M = 0 is a no-op.
+ */
+typedef struct {
+  int32_t M;
+  int32_t D;
+  int32_t dtype;   /* of x */
+  int32_t x_rows;  /* rows of x that `rows` may name (>= M without `rows`) */
+  int64_t ldx;     /* elements between rows of x */
+  int64_t ldq;     /* bytes between rows of codes */
+  int64_t lds;     /* bytes between rows of scales */
+  float ln_eps;
+} echo_quantize_fp4_cfg;
+
+/* bytes of a row's codes, D / 2 rounded up to a multiple of 128, and of its
+ * scales, D / 32 rounded up to a multiple of 16 (0 for D outside [1, 65536]) */
+int64_t echo_fp4_pitch(int32_t D);
+int64_t echo_fp4_scale_pitch(int32_t D);
+int echo_quantize_rows_fp4(const echo_quantize_fp4_cfg* cfg, const void* x, const int32_t* rows, const float* shift,
+                           const float* scale, uint8_t* codes, uint8_t* scales, void* stream);
+int echo_dequantize_rows_fp4(const echo_quantize_fp4_cfg* cfg, const uint8_t* codes, const uint8_t* scales, void* x,
+                             void* stream);
+
+/*
+ * Linear layer on such rows: a holds M tokens, w N channels (the weight matrix
+ * [N][K] quantized by row):
+ *   y_mn = f( sum_k a_mk w_nk + bias_n )
+ * with products exact and sums in fp32; a NaN block makes its row (channel) NaN.
+ * Where the product is split along K the parts are joined in fp32 in a fixed
+ * order: a call's result is the same every time, but a row's rounding may depend
+ * on how many rows the call has.  epilogue, bias, gate, residual, residual_rows
+ * and c as in echo_linear_int8.
+ * a, w: codes, rows lda and ldw bytes apart, a_scales, w_scales: rows ldsa and
+ * ldsw bytes apart, as echo_quantize_rows_fp4 writes them (pitches as there);
+ * behind K zeros in the codes of one of the two at least, up to the pitch of K,
+ * and no scale of 255.  a, w and their scales: 16-byte aligned; every other
+ * pointer by its element type.
+ * Requires 1 <= N <= 2^22, 1 <= K <= 65536, M >= 0 (0: no-op), and fewer than
+ * 2^24 tiles of 64 x 64 outputs.
+ */
+typedef struct {
+  int32_t M;
+  int32_t N;
+  int32_t K;
+  int32_t epilogue;   /* echo_linear_epilogue */
+  int32_t out_dtype;
+  int32_t bias_dtype;
+  int32_t residual_dtype;
+  int32_t residual_nrows;
+  int64_t lda;
+  int64_t ldsa;
+  int64_t ldw;
+  int64_t ldsw;
+  int64_t ldc;
+  int64_t ldr;
+} echo_linear_fp4_cfg;
+
+size_t echo_linear_fp4_workspace(const echo_linear_fp4_cfg* cfg);
+int echo_linear_fp4(const echo_linear_fp4_cfg* cfg, const uint8_t* a, const uint8_t* a_scales, const uint8_t* w,
+                    const uint8_t* w_scales, const void* bias, const float* gate, const void* residual,
+                    const int32_t* residual_rows, void* c, void* workspace, size_t workspace_bytes, void* stream);
+
 /* --------------------------------------------------------- cross attention */
 /*
  * Attention of Lq queries to the Lk states of an encoder (of another length),
@@ -597,6 +682,147 @@ size_t echo_cross_attention_workspace(const echo_cross_attention_cfg* cfg, int32
 int echo_cross_attention(const echo_cross_attention_cfg* cfg, const void* q, const void* k, const void* v,
                          const int32_t* k_len, const uint8_t* key_mask, void* out, void* workspace,
                          size_t workspace_bytes, void* stream);
+
+/* -------------------------------------------------------- rotary positions */
+/*
+ * Rotary positions of queries and keys [B][L][heads][dh]: the first `dims`
+ * channels of every head turn in pairs, pair j by the angle t = pos * freq[j]:
+ *   (u, v) -> magnitude * (u cos t - v sin t, u sin t + v cos t)
+ * pair j being channels (2j, 2j + 1) (ECHO_ROTARY_INTERLEAVED) or (j, j +
+ * dims / 2) (ECHO_ROTARY_HALF); channels from dims on are copied.  The angle is
+ * computed in fp64, its sine and cosine and the products in fp32, and a result is
+ * rounded once.
+ * pos: positions[b][i] (device int32, rows pos_batch elements apart, 0: the same
+ * for every element), or i where positions is NULL.  With grid_w > 0 a position
+ * is a token of a grid of frames of grid_h x grid_w: the first pairs_t pairs turn
+ * by its frame pos / (grid_h grid_w), the next pairs_r by its row, the others by
+ * its column (positions must not be negative then).
+ * q [B][L][H][dh], k [B][L][Hk][dh] (Hk = 0: none, k and k_out are not looked
+ * at), q_out and k_out with their strides, in elements, as in
+ * echo_cross_attention but of any multiple; dh values are contiguous.  An output
+ * may be its input itself (same pointer and strides) and else overlaps no input.
+ * freq: device fp64 [dims / 2].  All pointers by their element type.
+ * Requires 2 <= dims <= dh <= 512, dims even, H >= 1, H + Hk <= 65536, B * L <
+ * 2^24, magnitude finite.  B, L >= 0 (0: no-op).
+ */
+typedef enum { ECHO_ROTARY_INTERLEAVED = 0, ECHO_ROTARY_HALF = 1 } echo_rotary_layout;
+
+typedef struct {
+  int32_t B;
+  int32_t L;
+  int32_t H;
+  int32_t Hk;
+  int32_t dh;
+  int32_t dims;
+  int32_t layout;
+  int32_t dtype;
+  int32_t grid_h;      /* 0 and 0: no grid */
+  int32_t grid_w;
+  int32_t pairs_t;
+  int32_t pairs_r;
+  float magnitude;
+  int64_t pos_batch;
+  echo_strides q;
+  echo_strides k;
+  echo_strides q_out;
+  echo_strides k_out;
+} echo_rotary_cfg;
+
+int echo_rotary(const echo_rotary_cfg* cfg, const void* q, const void* k, const int32_t* positions, const double* freq,
+                void* q_out, void* k_out, void* stream);
+
+/*
+ * Host function: frequencies f_j = base^(-2j / dims), j < n = dims / 2, or with
+ * pairs_t + pairs_r > 0 those of a grid's axes, base^(-j' / n') with j' the pair's
+ * number within its axis of n' pairs (pairs_t, pairs_r and the rest), for
+ * contexts `factor` times as long as the original_length positions they were
+ * trained for:
+ *   ECHO_ROTARY_PLAIN   as they are (factor, original_length, low, high unused)
+ *   ECHO_ROTARY_LINEAR  f_j / factor
+ *   ECHO_ROTARY_BASE    base * factor^(dims / (dims - 2)) in base's place (dims > 2)
+ *   ECHO_ROTARY_RAMP    k_j f_j + (1 - k_j) f_j / factor, k_j falling from 1 to 0
+ *                       between pairs floor(p(high)) and ceil(p(low)) (within 0 ..
+ *                       dims - 1), p(r) = n ln(original_length / (2 pi r)) / ln(base)
+ *                       being the pair that turns r times in the original length;
+ *                       magnitude 1 + 0.1 ln(factor), else 1
+ *                       (YaRN, arXiv 2309.00071; low 1 and high 32 there)
+ *   ECHO_ROTARY_BANDS   the same mixture with k_j = (r_j - low) / (high - low) within
+ *                       0 .. 1, r_j = original_length f_j / (2 pi) the pair's own turns
+ * Writes dims / 2 values to freq and one to magnitude (host pointers).  A grid
+ * takes PLAIN and LINEAR.  Returns an echo_status: ECHO_EINVAL for dims odd or
+ * outside [2, 512], base <= 1, factor < 1, original_length < 1, low <= 0 or high
+ * <= low where they are used, values that are not finite, or null pointers.
+ */
+typedef enum {
+  ECHO_ROTARY_PLAIN = 0,
+  ECHO_ROTARY_LINEAR = 1,
+  ECHO_ROTARY_BASE = 2,
+  ECHO_ROTARY_RAMP = 3,
+  ECHO_ROTARY_BANDS = 4
+} echo_rotary_scaling;
+
+typedef struct {
+  int32_t dims;
+  int32_t scaling;
+  int32_t pairs_t;
+  int32_t pairs_r;
+  double base;
+  double factor;
+  double original_length;
+  double low;
+  double high;
+} echo_rotary_freq_cfg;
+
+int echo_rotary_frequencies(const echo_rotary_freq_cfg* cfg, double* freq, float* magnitude);
+
+/* ------------------------------------------- norms on both sides of a sub-layer */
+/*
+ * What lies between two sub-layers, in one pass: the norm after the one, its
+ * gate, the residual stream, and the norm before the next with its modulation.
+ *   y_i = residual_scale residual[r_i] + gate_g (N1(z_i) after_weight)
+ *   h_i = N2(y_i) before_weight (1 + scale_g) + shift_g
+ * N1 = after, N2 = before: ECHO_NORM_RMS v / sqrt(mean(v^2) + eps), ECHO_NORM_LAYER
+ * (v - mean) / sqrt(variance + eps) with the biased variance, ECHO_NORM_NONE: v
+ * (before NONE: h, before_weight, scale and shift must be NULL).  In fp32; y and h
+ * are rounded once, h from the y before its rounding.
+ * z [M][D]; residual rows r_i = residual_rows[i], or i where that is NULL; a row
+ * outside [0, residual_nrows) gives NaN in y_i and h_i.  after_weight,
+ * before_weight fp32 [D] or NULL (1); gate, scale, shift fp32 [n_groups][D], rows
+ * ldgate, ldscale, ldshift elements apart (0: one row for all) or NULL (1, 0, 0);
+ * g = groups[i] (int32 [M]; outside [0, n_groups): NaN as above), or i / (M /
+ * n_groups) where groups is NULL (n_groups then divides M).
+ * y may be the residual itself where residual_rows is NULL, h may be z itself
+ * (same type and pitch); else outputs overlap nothing.  Pointers by their
+ * element type.  Requires 1 <= D <= 16384, M >= 0 (0: no-op), n_groups >= 1,
+ * eps >= 0, residual_scale finite, pitches of at least D.
+ */
+typedef enum { ECHO_NORM_NONE = 0, ECHO_NORM_RMS = 1, ECHO_NORM_LAYER = 2 } echo_norm;
+
+typedef struct {
+  int32_t M;
+  int32_t D;
+  int32_t n_groups;
+  int32_t after;          /* echo_norm */
+  int32_t before;
+  int32_t z_dtype;
+  int32_t residual_dtype;
+  int32_t y_dtype;
+  int32_t h_dtype;
+  int32_t residual_nrows;
+  float residual_scale;
+  float eps;
+  int64_t ldz;            /* elements between rows */
+  int64_t ldr;
+  int64_t ldy;
+  int64_t ldh;
+  int64_t ldgate;
+  int64_t ldscale;
+  int64_t ldshift;
+} echo_gated_norm_cfg;
+
+int echo_gated_norm(const echo_gated_norm_cfg* cfg, const void* z, const void* residual, const int32_t* residual_rows,
+                    const float* after_weight, const float* gate, const float* before_weight, const float* scale,
+                    const float* shift, const int32_t* groups, void* y, void* h, void* stream);
 
 /* ------------------------------------------------------------ kernel timing */
 /*

@@ -20,6 +20,9 @@ ECHO_BLOCK_BATCH_INVARIANT = 1
 ECHO_ANCHOR_TOPK, ECHO_ANCHOR_UNIFORM = 0, 1
 ECHO_CODEC_RESIDUAL_INT8, ECHO_CODEC_FULL, ECHO_CODEC_NAIVE_INT8 = 0, 1, 2
 ECHO_LINEAR_NONE, ECHO_LINEAR_GELU_TANH, ECHO_LINEAR_GATE_RESIDUAL = 0, 1, 2
+ECHO_ROTARY_INTERLEAVED, ECHO_ROTARY_HALF = 0, 1
+ECHO_ROTARY_PLAIN, ECHO_ROTARY_LINEAR, ECHO_ROTARY_BASE, ECHO_ROTARY_RAMP, ECHO_ROTARY_BANDS = range(5)
+ECHO_NORM_NONE, ECHO_NORM_RMS, ECHO_NORM_LAYER = 0, 1, 2
 
 c_int32, c_int64, c_size_t, c_void_p, c_float, c_double = (
     ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_float,
@@ -104,6 +107,41 @@ class CrossAttentionCfg(ctypes.Structure):
                 ("v", Strides), ("out", Strides)]
 
 
+class QuantizeFp4Cfg(ctypes.Structure):
+    _fields_ = [("M", c_int32), ("D", c_int32), ("dtype", c_int32), ("x_rows", c_int32),
+                ("ldx", c_int64), ("ldq", c_int64), ("lds", c_int64), ("ln_eps", c_float)]
+
+
+class LinearFp4Cfg(ctypes.Structure):
+    _fields_ = [("M", c_int32), ("N", c_int32), ("K", c_int32), ("epilogue", c_int32),
+                ("out_dtype", c_int32), ("bias_dtype", c_int32), ("residual_dtype", c_int32),
+                ("residual_nrows", c_int32), ("lda", c_int64), ("ldsa", c_int64), ("ldw", c_int64),
+                ("ldsw", c_int64), ("ldc", c_int64), ("ldr", c_int64)]
+
+
+class RotaryCfg(ctypes.Structure):
+    _fields_ = [("B", c_int32), ("L", c_int32), ("H", c_int32), ("Hk", c_int32), ("dh", c_int32),
+                ("dims", c_int32), ("layout", c_int32), ("dtype", c_int32), ("grid_h", c_int32),
+                ("grid_w", c_int32), ("pairs_t", c_int32), ("pairs_r", c_int32), ("magnitude", c_float),
+                ("pos_batch", c_int64), ("q", Strides), ("k", Strides), ("q_out", Strides),
+                ("k_out", Strides)]
+
+
+class RotaryFreqCfg(ctypes.Structure):
+    _fields_ = [("dims", c_int32), ("scaling", c_int32), ("pairs_t", c_int32), ("pairs_r", c_int32),
+                ("base", c_double), ("factor", c_double), ("original_length", c_double),
+                ("low", c_double), ("high", c_double)]
+
+
+class GatedNormCfg(ctypes.Structure):
+    _fields_ = [("M", c_int32), ("D", c_int32), ("n_groups", c_int32), ("after", c_int32),
+                ("before", c_int32), ("z_dtype", c_int32), ("residual_dtype", c_int32),
+                ("y_dtype", c_int32), ("h_dtype", c_int32), ("residual_nrows", c_int32),
+                ("residual_scale", c_float), ("eps", c_float), ("ldz", c_int64), ("ldr", c_int64),
+                ("ldy", c_int64), ("ldh", c_int64), ("ldgate", c_int64), ("ldscale", c_int64),
+                ("ldshift", c_int64)]
+
+
 class KernelTime(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char_p), ("launches", c_int64), ("total_ms", c_double)]
 
@@ -158,6 +196,18 @@ _SIGNATURES = {
     "echo_linear_int8": (ctypes.c_int, [_P(LinearInt8Cfg), c_void_p, c_void_p, c_void_p, c_void_p,
                                         c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                         c_size_t, c_void_p]),
+    "echo_fp4_pitch": (c_int64, [c_int32]),
+    "echo_fp4_scale_pitch": (c_int64, [c_int32]),
+    "echo_quantize_rows_fp4": (ctypes.c_int, [_P(QuantizeFp4Cfg), c_void_p, c_void_p, c_void_p, c_void_p,
+                                              c_void_p, c_void_p, c_void_p]),
+    "echo_dequantize_rows_fp4": (ctypes.c_int, [_P(QuantizeFp4Cfg), c_void_p, c_void_p, c_void_p, c_void_p]),
+    "echo_linear_fp4_workspace": (c_size_t, [_P(LinearFp4Cfg)]),
+    "echo_linear_fp4": (ctypes.c_int, [_P(LinearFp4Cfg), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                       c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "echo_rotary": (ctypes.c_int, [_P(RotaryCfg), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                   c_void_p]),
+    "echo_rotary_frequencies": (ctypes.c_int, [_P(RotaryFreqCfg), _P(c_double), _P(c_float)]),
+    "echo_gated_norm": (ctypes.c_int, [_P(GatedNormCfg)] + [c_void_p] * 12),
     "echo_cross_attention_workspace": (c_size_t, [_P(CrossAttentionCfg), c_int32]),
     "echo_cross_attention": (ctypes.c_int, [_P(CrossAttentionCfg), c_void_p, c_void_p, c_void_p,
                                             c_void_p, c_void_p, c_void_p, c_void_p, c_size_t,

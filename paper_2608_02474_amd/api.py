@@ -16,6 +16,16 @@ and the operators of a block served in 8 bits:
   quantize_rows / dequantize_rows        rows as 8-bit codes with a scale each
   linear_int8(a, w, bias, ...)           linear layer on such rows
   cross_attention(q, k, v, ...)          attention to states of another length
+
+or in 4 bits:
+
+  quantize_rows_fp4 / dequantize_rows_fp4  rows as microscaled 4-bit floating point
+  linear_fp4(a, w, bias, ...)            linear layer on such rows
+
+and what such a block may have beside its products:
+
+  rotary(q, rot, k, positions, ...)      rotary positions of queries and keys
+  gated_norm(z, residual, ...)           norms on both sides of a sub-layer, gate, residual
 """
 from __future__ import annotations
 
@@ -26,8 +36,9 @@ import math
 import torch
 
 from . import _lib
-from ._lib import (BlockCfg, BlockWeights, CacheCfg, CrossAttentionCfg, EnergyCfg, KernelTime, LinearInt8Cfg,
-                   QuantizeCfg, RefCacheCfg, WanBlockCfg, WanBlockWeights,
+from ._lib import (BlockCfg, BlockWeights, CacheCfg, CrossAttentionCfg, EnergyCfg, GatedNormCfg, KernelTime,
+                   LinearFp4Cfg, LinearInt8Cfg, QuantizeCfg, QuantizeFp4Cfg, RefCacheCfg, RotaryCfg, RotaryFreqCfg,
+                   WanBlockCfg, WanBlockWeights,
                    RefCacheState, ScheduleCfg, ScheduleState, SelectCfg,
                    ECHO_BF16, ECHO_F32, check)
 
@@ -834,14 +845,8 @@ def _int8_rows(r: Int8Rows, name: str) -> tuple:
     return n, ld
 
 
-def quantize_rows(x: torch.Tensor, rows: torch.Tensor | None = None, shift: torch.Tensor | None = None,
-                  scale: torch.Tensor | None = None, ln_eps: float = 1e-6,
-                  out: Int8Rows | None = None) -> Int8Rows:
-    """Rows of x ([M, D], contiguous columns) as 8-bit codes with one scale each
-    (echo_quantize_rows); rows (int32) picks rows of x, shift and scale (fp32
-    [D]) put a modulated LayerNorm in front.  Quantizes a weight matrix
-    [channels, inputs] as well as tokens."""
-    lib = _lib_handle()
+def _quantize_source(x, rows, shift, scale) -> tuple:
+    """(rows of x, columns, elements between rows, rows to quantize) of checked arguments."""
     n, D, ldx = _rows_of(x, "x")
     M = n
     if rows is not None:
@@ -857,6 +862,18 @@ def quantize_rows(x: torch.Tensor, rows: torch.Tensor | None = None, shift: torc
         _vector(scale, "scale", D, torch.float32)
     if D > 65536:
         raise ValueError("rows of at most 65536 columns")
+    return n, D, ldx, M
+
+
+def quantize_rows(x: torch.Tensor, rows: torch.Tensor | None = None, shift: torch.Tensor | None = None,
+                  scale: torch.Tensor | None = None, ln_eps: float = 1e-6,
+                  out: Int8Rows | None = None) -> Int8Rows:
+    """Rows of x ([M, D], contiguous columns) as 8-bit codes with one scale each
+    (echo_quantize_rows); rows (int32) picks rows of x, shift and scale (fp32
+    [D]) put a modulated LayerNorm in front.  Quantizes a weight matrix
+    [channels, inputs] as well as tokens."""
+    lib = _lib_handle()
+    n, D, ldx, M = _quantize_source(x, rows, shift, scale)
     if out is None:
         ldq = (D + 127) // 128 * 128
         out = Int8Rows(x.new_empty((M, ldq), dtype=torch.int8), x.new_empty(M, dtype=torch.float32), D)
@@ -894,20 +911,9 @@ def dequantize_rows(r: Int8Rows, dtype=torch.bfloat16, out: torch.Tensor | None 
     return out
 
 
-def linear_int8(a: Int8Rows, w: Int8Rows, bias: torch.Tensor | None = None, activation: str | None = None,
-                gate: torch.Tensor | None = None, residual: torch.Tensor | None = None,
-                residual_rows: torch.Tensor | None = None, dtype=torch.bfloat16,
-                out: torch.Tensor | None = None, workspace: Workspace | None = None) -> torch.Tensor:
-    """Linear layer on 8-bit rows (echo_linear_int8): a [M tokens], w [N channels]
-    -> [M, N] in dtype.  activation: None or "gelu" (tanh form); or gate (fp32
-    [N]) and residual ([rows, N], picked by residual_rows): residual + gate * y.
-    out overlaps no input; without residual_rows it may be the residual itself."""
-    lib = _lib_handle()
-    M, lda = _int8_rows(a, "a")
-    N, ldw = _int8_rows(w, "w")
-    K = a.cols
-    if w.cols != K:
-        raise ValueError(f"a has {K} columns, w {w.cols}")
+def _epilogue_of(M: int, N: int, bias, activation, gate, residual, residual_rows) -> tuple:
+    """(epilogue, bias dtype, residual dtype, residual rows, elements between them) of
+    a linear layer's checked arguments."""
     epi = _lib.ECHO_LINEAR_NONE
     if activation is not None:
         if activation != "gelu":
@@ -932,6 +938,24 @@ def linear_int8(a: Int8Rows, w: Int8Rows, bias: torch.Tensor | None = None, acti
             _vector(residual_rows, "residual_rows", M, torch.int32)
         elif nres != M:
             raise ValueError(f"residual must have {M} rows")
+    return epi, bias_dt, res_dt, nres, ldr
+
+
+def linear_int8(a: Int8Rows, w: Int8Rows, bias: torch.Tensor | None = None, activation: str | None = None,
+                gate: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+                residual_rows: torch.Tensor | None = None, dtype=torch.bfloat16,
+                out: torch.Tensor | None = None, workspace: Workspace | None = None) -> torch.Tensor:
+    """Linear layer on 8-bit rows (echo_linear_int8): a [M tokens], w [N channels]
+    -> [M, N] in dtype.  activation: None or "gelu" (tanh form); or gate (fp32
+    [N]) and residual ([rows, N], picked by residual_rows): residual + gate * y.
+    out overlaps no input; without residual_rows it may be the residual itself."""
+    lib = _lib_handle()
+    M, lda = _int8_rows(a, "a")
+    N, ldw = _int8_rows(w, "w")
+    K = a.cols
+    if w.cols != K:
+        raise ValueError(f"a has {K} columns, w {w.cols}")
+    epi, bias_dt, res_dt, nres, ldr = _epilogue_of(M, N, bias, activation, gate, residual, residual_rows)
     if out is None:
         out, ldc = a.codes.new_empty((M, N), dtype=dtype), N
     else:
@@ -958,6 +982,324 @@ def _scratch(need: int, workspace: Workspace | None, like: torch.Tensor) -> torc
     if workspace is not None:
         return workspace.get(need, like.device)
     return like.new_empty(need, dtype=torch.uint8)
+
+
+# ------------------------------------------------------------- rows in 4 bits
+
+@dataclasses.dataclass
+class Fp4Rows:
+    """Rows held in 4 bits: value [i, j] = 2^(scales[i, j / 32] - 127) * code [i, j], j <
+    cols; two codes a byte (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), the even
+    column's in the low half.  A row's codes have a pitch of whole 128 bytes, its scales
+    of whole 16, with zeros behind the last column."""
+    codes: torch.Tensor        # uint8 [rows, pitch]
+    scales: torch.Tensor       # uint8 [rows, scale pitch]
+    cols: int
+
+    def __len__(self) -> int:
+        return self.codes.shape[0]
+
+
+def _fp4_rows(r: Fp4Rows, name: str) -> tuple:
+    """(rows, pitch, pitch of the scales) of checked 4-bit rows."""
+    if not isinstance(r, Fp4Rows):
+        raise TypeError(f"{name} must be Fp4Rows (see quantize_rows_fp4)")
+    n, width, ld = _rows_of(r.codes, f"{name}.codes", torch.uint8)
+    ns, swidth, lds = _rows_of(r.scales, f"{name}.scales", torch.uint8)
+    if ns != n:
+        raise ValueError(f"{name} must have as many rows of scales as of codes")
+    pitch, spitch = (r.cols + 255) // 256 * 128, (r.cols + 511) // 512 * 16
+    if not 1 <= r.cols <= 65536 or width < pitch or ld % 128 or width % 128 or ld > 65536:
+        raise ValueError(f"{name}.codes must have a pitch of {pitch} bytes or a larger multiple of 128 up to 65536")
+    if swidth < spitch or lds % 16 or swidth % 16 or lds > 65536:
+        raise ValueError(f"{name}.scales must have a pitch of {spitch} bytes or a larger multiple of 16 up to 65536")
+    return n, ld, lds
+
+
+def quantize_rows_fp4(x: torch.Tensor, rows: torch.Tensor | None = None, shift: torch.Tensor | None = None,
+                      scale: torch.Tensor | None = None, ln_eps: float = 1e-6,
+                      out: Fp4Rows | None = None) -> Fp4Rows:
+    """Rows of x ([M, D], contiguous columns) in microscaled 4-bit floating point
+    (echo_quantize_rows_fp4); rows (int32) picks rows of x, shift and scale (fp32 [D])
+    put a modulated LayerNorm in front.  Quantizes a weight matrix [channels, inputs]
+    as well as tokens."""
+    lib = _lib_handle()
+    n, D, ldx, M = _quantize_source(x, rows, shift, scale)
+    if out is None:
+        ldq, lds = (D + 255) // 256 * 128, (D + 511) // 512 * 16
+        out = Fp4Rows(x.new_empty((M, ldq), dtype=torch.uint8), x.new_empty((M, lds), dtype=torch.uint8), D)
+    else:
+        m, ldq, lds = _fp4_rows(out, "out")
+        if m != M or out.cols != D:
+            raise ValueError(f"out must hold {M} rows of {D} columns")
+    stream = _here(x.get_device(), rows, shift, scale, out.codes, out.scales)
+    cfg = QuantizeFp4Cfg(M, D, _echo_dtype(x), n, ldx, ldq, lds, ln_eps)
+    st = lib.echo_quantize_rows_fp4(ctypes.byref(cfg), x.data_ptr(), _ptr(rows), _ptr(shift), _ptr(scale),
+                                    out.codes.data_ptr(), out.scales.data_ptr(), stream)
+    if st:
+        check("echo_quantize_rows_fp4", st)
+    return out
+
+
+def dequantize_rows_fp4(r: Fp4Rows, dtype=torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values the codes stand for, [rows, cols] in dtype (echo_dequantize_rows_fp4)."""
+    lib = _lib_handle()
+    M, ldq, lds = _fp4_rows(r, "r")
+    D = r.cols
+    if out is None:
+        out, ldx = r.codes.new_empty((M, D), dtype=dtype), D
+    else:
+        m, d, ldx = _rows_of(out, "out")
+        if (m, d) != (M, D):
+            raise ValueError(f"out must be [{M}, {D}]")
+    stream = _here(r.codes.get_device(), r.scales, out)
+    cfg = QuantizeFp4Cfg(M, D, _echo_dtype(out), M, ldx, ldq, lds, 0.0)
+    st = lib.echo_dequantize_rows_fp4(ctypes.byref(cfg), r.codes.data_ptr(), r.scales.data_ptr(), out.data_ptr(),
+                                      stream)
+    if st:
+        check("echo_dequantize_rows_fp4", st)
+    return out
+
+
+def linear_fp4(a: Fp4Rows, w: Fp4Rows, bias: torch.Tensor | None = None, activation: str | None = None,
+               gate: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+               residual_rows: torch.Tensor | None = None, dtype=torch.bfloat16,
+               out: torch.Tensor | None = None, workspace: Workspace | None = None) -> torch.Tensor:
+    """Linear layer on 4-bit rows (echo_linear_fp4): a [M tokens], w [N channels] ->
+    [M, N] in dtype; the other arguments as linear_int8's.  A row's rounding may
+    depend on how many rows the call has."""
+    lib = _lib_handle()
+    M, lda, ldsa = _fp4_rows(a, "a")
+    N, ldw, ldsw = _fp4_rows(w, "w")
+    K = a.cols
+    if w.cols != K:
+        raise ValueError(f"a has {K} columns, w {w.cols}")
+    epi, bias_dt, res_dt, nres, ldr = _epilogue_of(M, N, bias, activation, gate, residual, residual_rows)
+    if out is None:
+        out, ldc = a.codes.new_empty((M, N), dtype=dtype), N
+    else:
+        m, d, ldc = _rows_of(out, "out")
+        if (m, d) != (M, N):
+            raise ValueError(f"out must be [{M}, {N}]")
+    stream = _here(a.codes.get_device(), a.scales, w.codes, w.scales, bias, gate, residual, residual_rows, out)
+    cfg = ctypes.byref(LinearFp4Cfg(M, N, K, epi, _echo_dtype(out), bias_dt, res_dt, nres, lda, ldsa, ldw, ldsw, ldc,
+                                    ldr))
+    ws = _scratch(lib.echo_linear_fp4_workspace(cfg), workspace, out)
+    st = lib.echo_linear_fp4(cfg, a.codes.data_ptr(), a.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(),
+                             _ptr(bias), _ptr(gate), _ptr(residual), _ptr(residual_rows), out.data_ptr(),
+                             _ptr(ws), 0 if ws is None else ws.numel(), stream)
+    if st:
+        check("echo_linear_fp4", st)
+    return out
+
+
+# ----------------------------------------------------------- rotary positions
+
+ROTARY_LAYOUTS = {"interleaved": _lib.ECHO_ROTARY_INTERLEAVED, "half": _lib.ECHO_ROTARY_HALF}
+ROTARY_SCALINGS = {None: _lib.ECHO_ROTARY_PLAIN, "linear": _lib.ECHO_ROTARY_LINEAR, "base": _lib.ECHO_ROTARY_BASE,
+                   "ramp": _lib.ECHO_ROTARY_RAMP, "bands": _lib.ECHO_ROTARY_BANDS}
+
+
+@dataclasses.dataclass
+class Rotary:
+    """How positions turn the heads of a model: made once, by `make` or from
+    frequencies of the caller's own, and given to every call of rotary."""
+    freq: torch.Tensor              # fp64 [pairs] on the device, radians per position
+    layout: str = "interleaved"     # pairs (2j, 2j + 1); "half": (j, j + pairs)
+    magnitude: float = 1.0          # factor of the turned channels
+    grid: tuple | None = None       # (rows, columns) of a frame: positions are tokens of a grid
+    pairs: tuple | None = None      # with a grid: pairs that turn by frame, row and column
+
+    @classmethod
+    def make(cls, dims: int, device, layout: str = "interleaved", base: float = 10000.0, scaling: str | None = None,
+             factor: float = 1.0, original_length: float = 0.0, low: float = 1.0, high: float = 32.0,
+             grid: tuple | None = None, pairs: tuple | None = None) -> "Rotary":
+        """For heads of which `dims` channels turn (echo_rotary_frequencies).  With a
+        grid and no pairs a sixth of the dims goes to rows and to columns each, as in
+        the Wan-style block."""
+        freq, magnitude, pairs = rotary_frequencies(dims, base, scaling, factor, original_length, low, high, grid, pairs)
+        return cls(torch.tensor(freq, dtype=torch.float64, device=device), layout, magnitude, grid, pairs)
+
+
+def rotary_frequencies(dims: int, base: float = 10000.0, scaling: str | None = None, factor: float = 1.0,
+                       original_length: float = 0.0, low: float = 1.0, high: float = 32.0, grid: tuple | None = None,
+                       pairs: tuple | None = None) -> tuple:
+    """(radians per position of each pair, magnitude, pairs per axis of the grid or
+    None): echo_rotary_frequencies, a host function.  scaling: None, "linear", "base",
+    "ramp" or "bands", for contexts `factor` times the original length."""
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"scaling must be one of {tuple(ROTARY_SCALINGS)}")
+    n = max(int(dims), 0) // 2
+    if grid is None:
+        if pairs is not None:
+            raise ValueError("pairs go with a grid")
+        t = r = 0
+    else:
+        if pairs is None:
+            pairs = (n - 2 * (int(dims) // 6), int(dims) // 6, int(dims) // 6)
+        t, r, c = pairs = tuple(int(v) for v in pairs)
+        if min(pairs) < 0 or t + r + c != n:
+            raise ValueError(f"pairs must be three counts that add up to {n}")
+        if t == r == 0:
+            raise ValueError("some pairs must turn by the frame or the row")
+    freq, magnitude = (ctypes.c_double * max(n, 1))(), ctypes.c_float()
+    cfg = RotaryFreqCfg(int(dims), ROTARY_SCALINGS[scaling], t, r, float(base), float(factor), float(original_length),
+                        float(low), float(high))
+    check("echo_rotary_frequencies",
+          _lib_handle().echo_rotary_frequencies(ctypes.byref(cfg), freq, ctypes.byref(magnitude)))
+    return list(freq), float(magnitude.value), pairs
+
+
+_NO_STRIDES = (0, 0, 0)
+
+
+def _rotary_out(x: torch.Tensor, shape, strides: tuple, out: torch.Tensor | None, name: str) -> tuple:
+    """(tensor, strides) of an output for x; x itself is one."""
+    if out is None:
+        b, n, h, d = shape
+        return x.new_empty(shape), (n * h * d, h * d, d)
+    oshape, os = _heads_of(out, name, x.dtype)
+    if oshape != shape or any(s == 0 for s, m in zip(os, shape) if m > 1):
+        raise ValueError(f"{name} must have the shape of its input, and no row twice")
+    return out, os
+
+
+def rotary(q: torch.Tensor, rot: Rotary, k: torch.Tensor | None = None, positions: torch.Tensor | None = None,
+           out: torch.Tensor | None = None, k_out: torch.Tensor | None = None) -> tuple:
+    """Rotary positions of q [B, L, H, dh] and, where given, k [B, L, Hk, dh]
+    (echo_rotary), in bf16 or fp32: (turned q, turned k or None).  positions: int32 [L]
+    or [B, L]; the token's number without.  dh is contiguous, the other strides are
+    any.  out and k_out may be q and k themselves and else overlap no input."""
+    lib = _lib_handle()
+    if not isinstance(rot, Rotary):
+        raise TypeError("rot must be a Rotary")
+    shape, qs = _heads_of(q, "q")
+    B, L, H, dh = shape
+    f = _dev(rot.freq, "rot.freq", torch.float64)
+    if f.dim() != 1 or rot.layout not in ROTARY_LAYOUTS:
+        raise ValueError(f"rot must have frequencies [pairs] and a layout of {tuple(ROTARY_LAYOUTS)}")
+    if max(B, L, H, dh) > _MAX_COUNT or f.numel() > 256:
+        raise ValueError("fewer than 2^31 elements, tokens and heads, and at most 256 pairs")
+    gh = gw = pt = pr = 0
+    if (rot.grid is None) != (rot.pairs is None):
+        raise ValueError("rot.grid and rot.pairs go together")
+    if rot.grid is not None:
+        gh, gw = rot.grid
+        pt, pr, pc = rot.pairs
+        if pt + pr + pc != f.numel() or not (0 < gh <= _MAX_COUNT and 0 < gw <= _MAX_COUNT) or min(rot.pairs) < 0:
+            raise ValueError(f"rot.grid must be (rows, columns), rot.pairs three counts that add up to {f.numel()}")
+    Hk, ks, kos = 0, _NO_STRIDES, _NO_STRIDES
+    if k is not None:
+        kshape, ks = _heads_of(k, "k", q.dtype)
+        Hk = kshape[2]
+        if kshape[0] != B or kshape[1] != L or kshape[3] != dh or Hk > _MAX_COUNT:
+            raise ValueError(f"k must be [{B}, {L}, heads, {dh}]")
+        k_out, kos = _rotary_out(k, kshape, ks, k_out, "k_out")
+    elif k_out is not None:
+        raise ValueError("k_out goes with k")
+    pos_batch = 0
+    if positions is not None:
+        _dev(positions, "positions", torch.int32)
+        if positions.shape == (B, L):
+            pos_batch = L
+        elif positions.shape != (L,):
+            raise ValueError(f"positions must be [{L}] or [{B}, {L}]")
+    out, os = _rotary_out(q, shape, qs, out, "out")
+    stream = _here(q.get_device(), k, f, positions, out, k_out)
+    cfg = RotaryCfg(B, L, H, Hk, dh, 2 * f.numel(), ROTARY_LAYOUTS[rot.layout], _echo_dtype(q), gh, gw, pt, pr,
+                    rot.magnitude, pos_batch, qs, ks, os, kos)
+    st = lib.echo_rotary(ctypes.byref(cfg), q.data_ptr(), _ptr(k), _ptr(positions), f.data_ptr(), out.data_ptr(),
+                         _ptr(k_out), stream)
+    if st:
+        check("echo_rotary", st)
+    return out, k_out
+
+
+# ------------------------------------------- norms on both sides of a sub-layer
+
+NORMS = {None: _lib.ECHO_NORM_NONE, "rms": _lib.ECHO_NORM_RMS, "layer": _lib.ECHO_NORM_LAYER}
+
+
+def _modulation(t: torch.Tensor | None, name: str, D: int) -> tuple:
+    """(rows, elements between them) of a modulation [D] or [groups, D]."""
+    if t is None:
+        return 1, 0
+    if isinstance(t, torch.Tensor) and t.dim() == 1:
+        _vector(t, name, D, torch.float32)
+        return 1, 0
+    n, d, ld = _rows_of(t, name, torch.float32)
+    if d != D or n < 1:
+        raise ValueError(f"{name} must be [{D}] or [groups, {D}]")
+    return n, ld if n > 1 else 0
+
+
+def gated_norm(z: torch.Tensor, residual: torch.Tensor, after: str | None = "rms",
+               after_weight: torch.Tensor | None = None, gate: torch.Tensor | None = None, residual_scale: float = 1.0,
+               residual_rows: torch.Tensor | None = None, before: str | None = "layer",
+               before_weight: torch.Tensor | None = None, scale: torch.Tensor | None = None,
+               shift: torch.Tensor | None = None, groups: torch.Tensor | None = None, eps: float = 1e-6,
+               y: torch.Tensor | None = None, h: torch.Tensor | None = None, y_dtype=None, h_dtype=None) -> tuple:
+    """What lies between two sub-layers (echo_gated_norm), for the output z [M, D] of
+    the first and the residual stream [M, D] (or rows of it, picked by residual_rows):
+      y = residual_scale residual + gate (after(z) after_weight)
+      h = before(y) before_weight (1 + scale) + shift
+    after, before: "rms", "layer" or None (no norm; before None: no h).  The weights are
+    fp32 [D]; gate, scale and shift fp32 [D] or [G, D], row i taking groups[i] (int32 [M])
+    or, without, i / (M / G).  y is of the residual's type and h of z's unless given
+    (y may be the residual, h may be z).  Returns (y, h or None)."""
+    lib = _lib_handle()
+    M, D, ldz = _rows_of(z, "z")
+    n, d, ldr = _rows_of(residual, "residual")
+    if d != D:
+        raise ValueError(f"residual must have {D} columns")
+    if after not in NORMS or before not in NORMS:
+        raise ValueError(f"after and before must be of {tuple(NORMS)}")
+    if residual_rows is not None:
+        _vector(residual_rows, "residual_rows", M, torch.int32)
+        if M > 0 and n == 0:
+            raise ValueError("residual has no rows to pick")
+    elif n != M:
+        raise ValueError(f"residual must have {M} rows")
+    for t, name in ((after_weight, "after_weight"), (before_weight, "before_weight")):
+        if t is not None:
+            _vector(t, name, D, torch.float32)
+    (g1, ldg), (g2, lds), (g3, ldt) = (_modulation(gate, "gate", D), _modulation(scale, "scale", D),
+                                       _modulation(shift, "shift", D))
+    G = max(g1, g2, g3)
+    if any(v not in (1, G) for v in (g1, g2, g3)):
+        raise ValueError("gate, scale and shift must have one row or as many as each other")
+    if groups is not None:
+        _vector(groups, "groups", M, torch.int32)
+    elif M % G:
+        raise ValueError(f"{G} groups must divide the {M} rows, or be given for each")
+    if y is None:
+        y, ldy = z.new_empty((M, D), dtype=y_dtype or residual.dtype), D
+    else:
+        m, d, ldy = _rows_of(y, "y", y_dtype)
+        if (m, d) != (M, D):
+            raise ValueError(f"y must be [{M}, {D}]")
+    ldh = h_dt = 0
+    if before is None:
+        if h is not None or before_weight is not None or scale is not None or shift is not None:
+            raise ValueError("h, before_weight, scale and shift go with a norm before the next sub-layer")
+    else:
+        if h is None:
+            h, ldh = z.new_empty((M, D), dtype=h_dtype or z.dtype), D
+        else:
+            m, d, ldh = _rows_of(h, "h", h_dtype)
+            if (m, d) != (M, D):
+                raise ValueError(f"h must be [{M}, {D}]")
+        h_dt = _echo_dtype(h)
+    stream = _here(z.get_device(), residual, residual_rows, after_weight, gate, before_weight, scale, shift, groups, y,
+                   h)
+    cfg = GatedNormCfg(M, D, G, NORMS[after], NORMS[before], _echo_dtype(z), _echo_dtype(residual), _echo_dtype(y),
+                       h_dt, n, residual_scale, eps, ldz, ldr, ldy, ldh, ldg, lds, ldt)
+    st = lib.echo_gated_norm(ctypes.byref(cfg), z.data_ptr(), residual.data_ptr(), _ptr(residual_rows),
+                             _ptr(after_weight), _ptr(gate), _ptr(before_weight), _ptr(scale), _ptr(shift),
+                             _ptr(groups), y.data_ptr(), _ptr(h), stream)
+    if st:
+        check("echo_gated_norm", st)
+    return y, h
 
 
 # ------------------------------------------------------------ cross attention

@@ -310,6 +310,55 @@ bool linear_supported(const echo_linear_int8_cfg* c) {
   return c->N <= (1 << 22) && ((int64_t(c->M) + 63) / 64) * ((int64_t(c->N) + 63) / 64) < kMaxGroups;
 }
 
+// ---- rows in 4 bits
+bool fp4_rows_ok(int64_t ld, int64_t lds, int32_t D) {
+  return ld >= echo_fp4_pitch(D) && ld <= 65536 && ld % 128 == 0 && lds >= echo_fp4_scale_pitch(D) && lds <= 65536 &&
+         lds % 16 == 0;
+}
+bool quantize_fp4_cfg_ok(const echo_quantize_fp4_cfg* c) {
+  return c != nullptr && c->M >= 0 && c->D >= 1 && c->D <= 65536 && ok_dtype(c->dtype) && c->ldx >= c->D &&
+         fp4_rows_ok(c->ldq, c->lds, c->D) && c->ln_eps >= 0.0f;
+}
+bool linear_fp4_cfg_ok(const echo_linear_fp4_cfg* c) {
+  return c != nullptr && c->M >= 0 && c->N >= 1 && c->K >= 1 && c->K <= 65536 && ok_dtype(c->out_dtype) &&
+         ok_dtype(c->bias_dtype) && ok_dtype(c->residual_dtype) &&
+         (c->epilogue == ECHO_LINEAR_NONE || c->epilogue == ECHO_LINEAR_GELU_TANH ||
+          c->epilogue == ECHO_LINEAR_GATE_RESIDUAL) &&
+         fp4_rows_ok(c->lda, c->ldsa, c->K) && fp4_rows_ok(c->ldw, c->ldsw, c->K) && c->ldc >= c->N &&
+         (c->epilogue != ECHO_LINEAR_GATE_RESIDUAL || c->ldr >= c->N);
+}
+bool linear_fp4_supported(const echo_linear_fp4_cfg* c) {
+  return c->N <= (1 << 22) && ((int64_t(c->M) + 63) / 64) * ((int64_t(c->N) + 63) / 64) < kMaxGroups;
+}
+
+// ---- rotary positions
+bool rotary_strides_ok(const echo_strides& s) { return s.batch >= 0 && s.row >= 0 && s.head >= 0; }
+bool rotary_cfg_ok(const echo_rotary_cfg* c) {
+  return c != nullptr && c->B >= 0 && c->L >= 0 && c->H >= 1 && c->Hk >= 0 && c->dims >= 2 && c->dims % 2 == 0 &&
+         c->dims <= c->dh && (c->layout == ECHO_ROTARY_INTERLEAVED || c->layout == ECHO_ROTARY_HALF) &&
+         ok_dtype(c->dtype) && c->grid_h >= 0 && c->grid_w >= 0 && (c->grid_h > 0) == (c->grid_w > 0) &&
+         c->pairs_t >= 0 && c->pairs_r >= 0 && int64_t(c->pairs_t) + c->pairs_r <= c->dims / 2 &&
+         std::isfinite(c->magnitude) && c->pos_batch >= 0 && rotary_strides_ok(c->q) && rotary_strides_ok(c->q_out) &&
+         (c->Hk == 0 || (rotary_strides_ok(c->k) && rotary_strides_ok(c->k_out)));
+}
+bool rotary_supported(const echo_rotary_cfg* c) {
+  return c->dh <= 512 && int64_t(c->H) + c->Hk <= 65536 && int64_t(c->B) * c->L < (int64_t(1) << 24);
+}
+bool same_strides(const echo_strides& a, const echo_strides& b) {
+  return a.batch == b.batch && a.row == b.row && a.head == b.head;
+}
+
+// ---- norms on both sides of a sub-layer
+bool norm_ok(int n) { return n == ECHO_NORM_NONE || n == ECHO_NORM_RMS || n == ECHO_NORM_LAYER; }
+bool gated_norm_cfg_ok(const echo_gated_norm_cfg* c) {
+  auto mod = [&](int64_t ld) { return ld == 0 || ld >= c->D; };
+  return c != nullptr && c->M >= 0 && c->D >= 1 && c->n_groups >= 1 && norm_ok(c->after) && norm_ok(c->before) &&
+         ok_dtype(c->z_dtype) && ok_dtype(c->residual_dtype) && ok_dtype(c->y_dtype) && ok_dtype(c->h_dtype) &&
+         std::isfinite(c->residual_scale) && c->eps >= 0.0f && std::isfinite(c->eps) && c->ldz >= c->D &&
+         c->ldr >= c->D && c->ldy >= c->D && (c->before == ECHO_NORM_NONE || c->ldh >= c->D) && mod(c->ldgate) &&
+         mod(c->ldscale) && mod(c->ldshift);
+}
+
 // ---- cross attention
 constexpr int32_t kMaxStates = INT32_MAX - 127;  // 2^31 - 128: two tiles of 64 short of overflow
 bool strides_ok(const echo_strides& s, int per16) {
@@ -790,7 +839,7 @@ int echo_quantize_rows(const echo_quantize_cfg* cfg, const void* x, const int32_
       (shift != nullptr && (!ok_ptr(shift) || !ok_ptr(scale))))
     return ECHO_EINVAL;
   const QuantizeArgs a{x,    cfg->ldx, rows,  cfg->x_rows, cfg->M, cfg->D, shift, scale, cfg->ln_eps,
-                       codes, cfg->ldq, row_scale};
+                       codes, cfg->ldq, row_scale, nullptr, 0};
   return device_status(launch_quantize_rows(cfg->dtype == ECHO_BF16, a, static_cast<hipStream_t>(stream)));
 }
 
@@ -799,7 +848,7 @@ int echo_dequantize_rows(const echo_quantize_cfg* cfg, const int8_t* codes, cons
   if (!quantize_cfg_ok(cfg)) return ECHO_EINVAL;
   if (cfg->M == 0) return ECHO_OK;
   if (!ok_ptr(codes) || !elem_aligned(row_scale, 4) || !elem_aligned(x, esize(cfg->dtype))) return ECHO_EINVAL;
-  const DequantizeArgs a{codes, cfg->ldq, row_scale, cfg->M, cfg->D, x, cfg->ldx};
+  const DequantizeArgs a{codes, cfg->ldq, row_scale, cfg->M, cfg->D, x, cfg->ldx, nullptr, 0};
   return device_status(launch_dequantize_rows(cfg->dtype == ECHO_BF16, a, static_cast<hipStream_t>(stream)));
 }
 
@@ -835,6 +884,182 @@ int echo_linear_int8(const echo_linear_int8_cfg* cfg, const int8_t* a, const flo
   g.res_rows = residual_rows; g.res_nrows = cfg->residual_nrows;
   g.part = static_cast<int32_t*>(workspace); g.part_bytes = workspace_bytes;
   return device_status(launch_gemm_i8(cfg->epilogue, g, static_cast<hipStream_t>(stream)));
+}
+
+int64_t echo_fp4_pitch(int32_t D) { return D < 1 || D > 65536 ? 0 : (int64_t(D) + 255) / 256 * 128; }
+int64_t echo_fp4_scale_pitch(int32_t D) { return D < 1 || D > 65536 ? 0 : (int64_t(D) + 511) / 512 * 16; }
+
+int echo_quantize_rows_fp4(const echo_quantize_fp4_cfg* cfg, const void* x, const int32_t* rows, const float* shift,
+                           const float* scale, uint8_t* codes, uint8_t* scales, void* stream) {
+  if (!quantize_fp4_cfg_ok(cfg) || (shift == nullptr) != (scale == nullptr)) return ECHO_EINVAL;
+  if (cfg->M == 0) return ECHO_OK;
+  if (!elem_aligned(x, esize(cfg->dtype)) || !ok_ptr(codes) || !ok_ptr(scales) ||
+      (rows != nullptr ? !elem_aligned(rows, 4) || cfg->x_rows < 1 : cfg->x_rows < cfg->M) ||
+      (shift != nullptr && (!ok_ptr(shift) || !ok_ptr(scale))))
+    return ECHO_EINVAL;
+  QuantizeArgs a{};
+  a.x = x; a.ldx = cfg->ldx; a.rows = rows; a.x_rows = cfg->x_rows; a.M = cfg->M; a.D = cfg->D;
+  a.shift = shift; a.scale = scale; a.ln_eps = cfg->ln_eps;
+  a.codes = reinterpret_cast<int8_t*>(codes); a.ldq = cfg->ldq;
+  a.scales = scales; a.lds = cfg->lds;
+  return device_status(launch_quantize_rows_fp4(cfg->dtype == ECHO_BF16, a, static_cast<hipStream_t>(stream)));
+}
+
+int echo_dequantize_rows_fp4(const echo_quantize_fp4_cfg* cfg, const uint8_t* codes, const uint8_t* scales, void* x,
+                             void* stream) {
+  if (!quantize_fp4_cfg_ok(cfg)) return ECHO_EINVAL;
+  if (cfg->M == 0) return ECHO_OK;
+  if (!ok_ptr(codes) || !ok_ptr(scales) || !elem_aligned(x, esize(cfg->dtype))) return ECHO_EINVAL;
+  DequantizeArgs a{};
+  a.codes = reinterpret_cast<const int8_t*>(codes); a.ldq = cfg->ldq;
+  a.scales = scales; a.lds = cfg->lds;
+  a.M = cfg->M; a.D = cfg->D; a.y = x; a.ldy = cfg->ldx;
+  return device_status(launch_dequantize_rows_fp4(cfg->dtype == ECHO_BF16, a, static_cast<hipStream_t>(stream)));
+}
+
+size_t echo_linear_fp4_workspace(const echo_linear_fp4_cfg* cfg) {
+  if (!linear_fp4_cfg_ok(cfg) || !linear_fp4_supported(cfg) || cfg->M == 0) return 0;
+  return gemm_fp4_partial_bytes(cfg->M, cfg->N, static_cast<int>(echo_fp4_pitch(cfg->K)));
+}
+
+int echo_linear_fp4(const echo_linear_fp4_cfg* cfg, const uint8_t* a, const uint8_t* a_scales, const uint8_t* w,
+                    const uint8_t* w_scales, const void* bias, const float* gate, const void* residual,
+                    const int32_t* residual_rows, void* c, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!linear_fp4_cfg_ok(cfg)) return ECHO_EINVAL;
+  if (!linear_fp4_supported(cfg)) return ECHO_EUNSUPPORTED;
+  if (cfg->M == 0) return ECHO_OK;
+  const bool gated = cfg->epilogue == ECHO_LINEAR_GATE_RESIDUAL;
+  if (!ok_ptr(a) || !ok_ptr(a_scales) || !ok_ptr(w) || !ok_ptr(w_scales) || !elem_aligned(c, esize(cfg->out_dtype)) ||
+      (bias != nullptr && !elem_aligned(bias, esize(cfg->bias_dtype))))
+    return ECHO_EINVAL;
+  if (gated ? (!elem_aligned(gate, 4) || !elem_aligned(residual, esize(cfg->residual_dtype)) ||
+               (residual_rows != nullptr ? !elem_aligned(residual_rows, 4) || cfg->residual_nrows < 1
+                                         : cfg->residual_nrows < cfg->M))
+            : (gate != nullptr || residual != nullptr || residual_rows != nullptr))
+    return ECHO_EINVAL;
+  const size_t need = echo_linear_fp4_workspace(cfg);
+  if (need > 0 && (!ok_ptr(workspace) || workspace_bytes < need)) return ECHO_EWORKSPACE;
+  GemmFp4Args g{};
+  g.A = a; g.lda = cfg->lda; g.sa = a_scales; g.ldsa = cfg->ldsa;
+  g.B = w; g.ldb = cfg->ldw; g.sb = w_scales; g.ldsb = cfg->ldsw;
+  g.M = cfg->M; g.N = cfg->N; g.K = static_cast<int>(echo_fp4_pitch(cfg->K));
+  g.bias = bias; g.bias_bf16 = cfg->bias_dtype == ECHO_BF16;
+  g.C = c; g.c_bf16 = cfg->out_dtype == ECHO_BF16; g.ldc = cfg->ldc;
+  g.gate = gate; g.res = residual; g.res_bf16 = cfg->residual_dtype == ECHO_BF16; g.ldr = cfg->ldr;
+  g.res_rows = residual_rows; g.res_nrows = cfg->residual_nrows;
+  g.part = static_cast<float*>(workspace); g.part_bytes = workspace_bytes;
+  return device_status(launch_gemm_fp4(cfg->epilogue, g, static_cast<hipStream_t>(stream)));
+}
+
+int echo_rotary(const echo_rotary_cfg* cfg, const void* q, const void* k, const int32_t* positions, const double* freq,
+                void* q_out, void* k_out, void* stream) {
+  if (!rotary_cfg_ok(cfg)) return ECHO_EINVAL;
+  if (!rotary_supported(cfg)) return ECHO_EUNSUPPORTED;
+  if (cfg->B == 0 || cfg->L == 0) return ECHO_OK;
+  const size_t es = esize(cfg->dtype);
+  const bool keys = cfg->Hk > 0;
+  if (!elem_aligned(q, es) || !elem_aligned(q_out, es) || !elem_aligned(freq, 8) ||
+      (positions != nullptr && !elem_aligned(positions, 4)) ||
+      (keys && (!elem_aligned(k, es) || !elem_aligned(k_out, es))) ||
+      (q == q_out && !same_strides(cfg->q, cfg->q_out)) ||
+      (keys && k == k_out && !same_strides(cfg->k, cfg->k_out)))
+    return ECHO_EINVAL;
+  RotaryArgs a{};
+  auto st = [](const echo_strides& s, int64_t& b, int64_t& r, int64_t& h) { b = s.batch, r = s.row, h = s.head; };
+  a.q = q; a.qo = q_out;
+  st(cfg->q, a.qb, a.qr, a.qh);
+  st(cfg->q_out, a.qob, a.qor, a.qoh);
+  if (keys) {
+    a.k = k; a.ko = k_out;
+    st(cfg->k, a.kb, a.kr, a.kh);
+    st(cfg->k_out, a.kob, a.kor, a.koh);
+  }
+  a.B = cfg->B; a.L = cfg->L; a.H = cfg->H; a.Hk = cfg->Hk; a.dh = cfg->dh; a.dims = cfg->dims;
+  a.half = cfg->layout == ECHO_ROTARY_HALF;
+  a.grid_h = cfg->grid_h; a.grid_w = cfg->grid_w; a.pairs_t = cfg->pairs_t; a.pairs_r = cfg->pairs_r;
+  a.magnitude = cfg->magnitude;
+  a.positions = positions; a.pos_batch = cfg->pos_batch; a.freq = freq;
+  return device_status(launch_rotary(cfg->dtype == ECHO_BF16, a, static_cast<hipStream_t>(stream)));
+}
+
+int echo_rotary_frequencies(const echo_rotary_freq_cfg* cfg, double* freq, float* magnitude) {
+  constexpr double kTwoPi = 6.283185307179586476925;
+  if (cfg == nullptr || freq == nullptr || magnitude == nullptr) return ECHO_EINVAL;
+  const int n = cfg->dims / 2, s = cfg->scaling;
+  const bool grid = cfg->pairs_t != 0 || cfg->pairs_r != 0, mixed = s == ECHO_ROTARY_RAMP || s == ECHO_ROTARY_BANDS;
+  if (cfg->dims < 2 || cfg->dims > 512 || cfg->dims % 2 != 0 || cfg->pairs_t < 0 || cfg->pairs_r < 0 ||
+      int64_t(cfg->pairs_t) + cfg->pairs_r > n || !std::isfinite(cfg->base) || !(cfg->base > 1.0) ||
+      s < ECHO_ROTARY_PLAIN || s > ECHO_ROTARY_BANDS || (grid && s > ECHO_ROTARY_LINEAR) ||
+      (s == ECHO_ROTARY_BASE && cfg->dims <= 2))
+    return ECHO_EINVAL;
+  if (s != ECHO_ROTARY_PLAIN && (!std::isfinite(cfg->factor) || !(cfg->factor >= 1.0))) return ECHO_EINVAL;
+  if (mixed && (!std::isfinite(cfg->original_length) || !(cfg->original_length >= 1.0) || !(cfg->low > 0.0) ||
+                !std::isfinite(cfg->high) || !(cfg->high > cfg->low)))
+    return ECHO_EINVAL;
+  const double base = s == ECHO_ROTARY_BASE ? cfg->base * std::pow(cfg->factor, cfg->dims / (cfg->dims - 2.0)) : cfg->base;
+  const auto clamp = [](double v, double lo, double hi) { return v < lo ? lo : v > hi ? hi : v; };
+  const auto pair_of = [&](double turns) {
+    return n * std::log(cfg->original_length / (kTwoPi * turns)) / std::log(base);
+  };
+  double from = 0.0, to = 0.0;
+  if (s == ECHO_ROTARY_RAMP) {
+    from = clamp(std::floor(pair_of(cfg->high)), 0.0, cfg->dims - 1.0);
+    to = clamp(std::ceil(pair_of(cfg->low)), 0.0, cfg->dims - 1.0);
+    if (!(to > from)) to = from + 0.001;
+  }
+  for (int j = 0; j < n; ++j) {
+    int at = j, of = n;
+    if (grid) {
+      const int t = cfg->pairs_t, r = cfg->pairs_r;
+      at = j < t ? j : j < t + r ? j - t : j - t - r;
+      of = j < t ? t : j < t + r ? r : n - t - r;
+    }
+    const double f = std::pow(base, -static_cast<double>(at) / of);
+    double keep = 1.0;
+    if (s == ECHO_ROTARY_LINEAR) keep = 0.0;
+    if (s == ECHO_ROTARY_RAMP) keep = 1.0 - clamp((j - from) / (to - from), 0.0, 1.0);
+    if (s == ECHO_ROTARY_BANDS)
+      keep = clamp((cfg->original_length * f / kTwoPi - cfg->low) / (cfg->high - cfg->low), 0.0, 1.0);
+    freq[j] = keep == 1.0 ? f : keep * f + (1.0 - keep) * f / cfg->factor;
+  }
+  *magnitude = s == ECHO_ROTARY_RAMP ? static_cast<float>(1.0 + 0.1 * std::log(cfg->factor)) : 1.0f;
+  return ECHO_OK;
+}
+
+int echo_gated_norm(const echo_gated_norm_cfg* cfg, const void* z, const void* residual, const int32_t* residual_rows,
+                    const float* after_weight, const float* gate, const float* before_weight, const float* scale,
+                    const float* shift, const int32_t* groups, void* y, void* h, void* stream) {
+  if (!gated_norm_cfg_ok(cfg)) return ECHO_EINVAL;
+  if (cfg->D > 16384) return ECHO_EUNSUPPORTED;
+  if (cfg->M == 0) return ECHO_OK;
+  const bool next = cfg->before != ECHO_NORM_NONE;
+  auto opt = [](const void* p) { return p == nullptr || elem_aligned(p, 4); };
+  if (!elem_aligned(z, esize(cfg->z_dtype)) || !elem_aligned(residual, esize(cfg->residual_dtype)) ||
+      !elem_aligned(y, esize(cfg->y_dtype)) || !opt(residual_rows) || !opt(after_weight) || !opt(gate) ||
+      !opt(before_weight) || !opt(scale) || !opt(shift) || !opt(groups) ||
+      (residual_rows != nullptr ? cfg->residual_nrows < 1 : cfg->residual_nrows < cfg->M) ||
+      (groups == nullptr && cfg->M % cfg->n_groups != 0))
+    return ECHO_EINVAL;
+  if (next ? !elem_aligned(h, esize(cfg->h_dtype))
+           : (h != nullptr || before_weight != nullptr || scale != nullptr || shift != nullptr))
+    return ECHO_EINVAL;
+  // an output in an input's place has to be written where that row alone was read
+  if ((y == residual && (residual_rows != nullptr || cfg->y_dtype != cfg->residual_dtype || cfg->ldy != cfg->ldr)) ||
+      (next && h == z && (cfg->h_dtype != cfg->z_dtype || cfg->ldh != cfg->ldz)))
+    return ECHO_EINVAL;
+  GatedNormArgs a{};
+  a.M = cfg->M; a.D = cfg->D; a.G = cfg->n_groups; a.after = cfg->after; a.before = cfg->before;
+  a.alpha = cfg->residual_scale; a.eps = cfg->eps;
+  a.z = z; a.z_bf16 = cfg->z_dtype == ECHO_BF16; a.ldz = cfg->ldz;
+  a.x = residual; a.x_bf16 = cfg->residual_dtype == ECHO_BF16; a.ldx = cfg->ldr;
+  a.x_rows = residual_rows; a.x_nrows = cfg->residual_nrows;
+  a.w1 = after_weight; a.w2 = before_weight;
+  a.gate = gate; a.scale = scale; a.shift = shift;
+  a.ldgate = cfg->ldgate; a.ldscale = cfg->ldscale; a.ldshift = cfg->ldshift;
+  a.groups = groups; a.rows_per_group = groups != nullptr ? 1 : cfg->M / cfg->n_groups;
+  a.y = y; a.y_bf16 = cfg->y_dtype == ECHO_BF16; a.ldy = cfg->ldy;
+  a.h = h; a.h_bf16 = cfg->h_dtype == ECHO_BF16; a.ldh = cfg->ldh;
+  return device_status(launch_gated_norm(a, static_cast<hipStream_t>(stream)));
 }
 
 size_t echo_cross_attention_workspace(const echo_cross_attention_cfg* cfg, int32_t masked) {

@@ -1,0 +1,287 @@
+// The norms on both sides of a sub-layer with its gate and residual, in one pass:
+//
+//   y_i = a x_r(i) + gate_g * (N1(z_i) * w1),   h_i = N2(y_i) * w2 * (1 + scale_g) + shift_g
+//
+// z: the sub-layer's output, x: the residual stream (its rows picked by r), g:
+// the row's modulation.  N1 and N2 are root-mean-square or layer norms (biased
+// variance, two passes over registers) in fp32, N1 may be left out.  y and h are
+// rounded once, h from the y that is not rounded.
+//
+// Apart, these are three kernels that write and read the stream between them;
+// here z and x are read and y and h written once, and the kernel is bound by
+// that.  A row lies in the registers of a wave or a workgroup; a workgroup takes
+// consecutive rows with the vectors over the channels (gate w1, w2 (1 + scale),
+// shift) in registers, and the next row's values on their way.
+#include "common.h"
+#include "kernels.h"
+#include "launch.h"
+
+namespace echo {
+
+// 8 elements of either type (the type is uniform over the launch)
+struct Any8 {
+  uint4 a, b;
+  __device__ __forceinline__ void load(const void* p, int bf, int64_t i) {
+    if (bf) {
+      a = ldg16_nt(static_cast<const bf16_t*>(p) + i);
+    } else {
+      a = ldg16_nt(static_cast<const float*>(p) + i);
+      b = ldg16_nt(static_cast<const float*>(p) + i + 4);
+    }
+  }
+  __device__ __forceinline__ void unpack(int bf, float* o) const {
+    if (bf) {
+      unpack16(a, o, static_cast<const bf16_t*>(nullptr));
+    } else {
+      unpack16(a, o, static_cast<const float*>(nullptr));
+      unpack16(b, o + 4, static_cast<const float*>(nullptr));
+    }
+  }
+};
+__device__ __forceinline__ void store8(void* p, int bf, int64_t i, const float* v) {
+  if (bf) {
+    stg16(static_cast<bf16_t*>(p) + i, pack16(v, static_cast<const bf16_t*>(nullptr)));
+  } else {
+    stg16(static_cast<float*>(p) + i, pack16(v, static_cast<const float*>(nullptr)));
+    stg16(static_cast<float*>(p) + i + 4, pack16(v + 4, static_cast<const float*>(nullptr)));
+  }
+}
+__device__ __forceinline__ float load1(const void* p, int bf, int64_t i) {
+  return bf ? bf16_to_f32(static_cast<const bf16_t*>(p)[i]) : static_cast<const float*>(p)[i];
+}
+__device__ __forceinline__ void store1(void* p, int bf, int64_t i, float v) {
+  if (bf)
+    static_cast<bf16_t*>(p)[i] = f32_to_bf16(v);
+  else
+    static_cast<float*>(p)[i] = v;
+}
+
+// A row per group of THREADS threads, NV chunks of 8 values a thread.  VEC: every
+// row of every tensor is aligned for 16-byte accesses and D % 8 == 0.
+template <int THREADS, int NV, bool VEC>
+__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) gated_norm_k(GatedNormArgs p, int rows_per_wg) {
+  constexpr int BLOCK = THREADS < 256 ? 256 : THREADS, RPB = BLOCK / THREADS, NW = THREADS / kWave;
+  constexpr bool HOLD = THREADS <= 256;  // (1024 threads have 128 registers each: the vectors are read for every row)
+  __shared__ float red[2][4][NW > 1 ? NW : 1];
+  const int t = threadIdx.x % THREADS, D = p.D;
+  int turn = 0;
+  // reduction `slot` of a row: a piece of LDS each, of two sets in turn, so that
+  // one barrier is enough
+  auto total = [&](float v, int slot) __attribute__((always_inline)) {
+    v = wave_sum(v);
+    if constexpr (NW > 1) {
+      if (t % kWave == 0) red[turn][slot][t / kWave] = v;
+      __syncthreads();
+      v = red[turn][slot][0];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) v += red[turn][slot][w];
+    }
+    return v;
+  };
+  auto in = [&](int u, int j) __attribute__((always_inline)) {
+    const int c = (t + u * THREADS) * 8;
+    return VEC ? c < D : c + j < D;
+  };
+  // v becomes its norm; what lies past the last column stays zero
+  auto norm = [&](float (&v)[NV][8], int kind, int slot) __attribute__((always_inline)) {
+    if (kind == NORM_LAYER) {
+      float s = 0.0f;
+#pragma unroll
+      for (int u = 0; u < NV; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += v[u][j];
+      const float mean = total(s, slot) / static_cast<float>(D);
+#pragma unroll
+      for (int u = 0; u < NV; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[u][j] = in(u, j) ? v[u][j] - mean : 0.0f;
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s = fmaf(v[u][j], v[u][j], s);
+    const float r = 1.0f / sqrtf(total(s, slot + 1) / static_cast<float>(D) + p.eps);
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[u][j] *= r;
+  };
+  // a vector over the channels, `none` where it is not given and past the last column
+  auto vector = [&](const float* w, int u, float none, float* o) __attribute__((always_inline)) {
+    const int c = (t + u * THREADS) * 8;
+    if (VEC) {
+      if (w != nullptr && c < D) {
+        unpack16(ldg16(w + c), o, static_cast<const float*>(nullptr));
+        unpack16(ldg16(w + c + 4), o + 4, static_cast<const float*>(nullptr));
+        return;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = none;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = w != nullptr && c + j < D ? w[c + j] : none;
+    }
+  };
+  auto gate_of = [&](int g, int u, float* o) __attribute__((always_inline)) {  // gate w1
+    float w[8];
+    vector(p.gate != nullptr ? p.gate + g * p.ldgate : nullptr, u, 1.0f, o);
+    vector(p.w1, u, 1.0f, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] *= w[j];
+  };
+  auto scale_of = [&](int g, int u, float* o) __attribute__((always_inline)) {  // w2 (1 + scale)
+    float w[8];
+    vector(p.scale != nullptr ? p.scale + g * p.ldscale : nullptr, u, 0.0f, o);
+    vector(p.w2, u, 1.0f, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = w[j] * (1.0f + o[j]);
+  };
+  auto shift_of = [&](int g, int u, float* o) __attribute__((always_inline)) {
+    vector(p.shift != nullptr ? p.shift + g * p.ldshift : nullptr, u, 0.0f, o);
+  };
+  float ga[HOLD ? NV : 1][8], sc[HOLD ? NV : 1][8], sh[HOLD ? NV : 1][8];
+  constexpr bool AHEAD = VEC && HOLD;
+  constexpr int kUnroll = VEC ? NV : 1;
+  Any8 nz[kUnroll], nx[kUnroll];
+  bool nbad = false;
+  auto source = [&](int64_t row, bool& bad) __attribute__((always_inline)) -> int64_t {
+    bad = false;
+    if (p.x_rows == nullptr) return row;
+    const int32_t r = p.x_rows[row];
+    bad = r < 0 || r >= p.x_nrows;  // no such row: NaN
+    return bad ? 0 : r;
+  };
+  auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+    const int64_t xr = source(row, nbad);
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int c = (t + u * THREADS) * 8, k = c < D ? c : 0;
+      nz[VEC ? u : 0].load(p.z, p.z_bf16, row * p.ldz + k);
+      nx[VEC ? u : 0].load(p.x, p.x_bf16, xr * p.ldx + k);
+    }
+  };
+  const int64_t base = static_cast<int64_t>(blockIdx.x) * rows_per_wg;
+  const int64_t end = base + rows_per_wg < p.M ? base + rows_per_wg : p.M;
+  int64_t row = base + threadIdx.x / THREADS;
+  int have = -1;
+  if constexpr (AHEAD)
+    if (row < end) fetch(row);
+  // (a group that reaches a barrier is the whole workgroup, so the loop is uniform for its waves)
+  for (; row < end; row += RPB) {
+    const int g = p.groups != nullptr ? p.groups[row] : static_cast<int>(row / p.rows_per_group);
+    const bool no_group = g < 0 || g >= p.G;
+    if constexpr (HOLD) {
+      if (!no_group && g != have) {
+        have = g;
+#pragma unroll
+        for (int u = 0; u < NV; ++u) gate_of(g, u, ga[u]), scale_of(g, u, sc[u]), shift_of(g, u, sh[u]);
+      }
+    }
+    const int gm = no_group ? 0 : g;
+    float v[NV][8], x[NV][8];
+    bool bad;
+    if constexpr (VEC) {
+      if constexpr (!AHEAD) fetch(row);
+      bad = nbad;
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        nz[u].unpack(p.z_bf16, v[u]);
+        nx[u].unpack(p.x_bf16, x[u]);
+        if ((t + u * THREADS) * 8 >= D) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[u][j] = x[u][j] = 0.0f;
+        }
+      }
+      if constexpr (AHEAD)
+        if (row + RPB < end) fetch(row + RPB);
+    } else {
+      const int64_t xr = source(row, bad);
+#pragma unroll
+      for (int u = 0; u < NV; ++u)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int c = (t + u * THREADS) * 8 + j;
+          v[u][j] = c < D ? load1(p.z, p.z_bf16, row * p.ldz + c) : 0.0f;
+          x[u][j] = c < D ? load1(p.x, p.x_bf16, xr * p.ldx + c) : 0.0f;
+        }
+    }
+    bad = bad || no_group;
+    if (p.after != NORM_NONE) norm(v, p.after, 0);
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      float m[8];
+      if constexpr (!HOLD) gate_of(gm, u, m);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[u][j] = fmaf(v[u][j], HOLD ? ga[HOLD ? u : 0][j] : m[j], p.alpha * x[u][j]);
+        if (bad) v[u][j] = in(u, j) ? __uint_as_float(0x7fc00000u) : 0.0f;
+      }
+    }
+    auto put = [&](void* out, int bf, int64_t ld) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        const int c = (t + u * THREADS) * 8;
+        if (VEC) {
+          if (c < D) store8(out, bf, row * ld + c, v[u]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (c + j < D) store1(out, bf, row * ld + c + j, v[u][j]);
+        }
+      }
+    };
+    put(p.y, p.y_bf16, p.ldy);
+    if (p.before != NORM_NONE) {
+      norm(v, p.before, 2);
+#pragma unroll
+      for (int u = 0; u < NV; ++u) {
+        float m[8], a[8];
+        if constexpr (!HOLD) scale_of(gm, u, m), shift_of(gm, u, a);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          v[u][j] = fmaf(v[u][j], HOLD ? sc[HOLD ? u : 0][j] : m[j], HOLD ? sh[HOLD ? u : 0][j] : a[j]);
+      }
+      put(p.h, p.h_bf16, p.ldh);
+    }
+    turn ^= 1;
+  }
+}
+
+namespace {
+
+template <int THREADS, int NV, bool VEC>
+hipError_t launch_w(const GatedNormArgs& p, hipStream_t stream) {
+  constexpr int BLOCK = THREADS < 256 ? 256 : THREADS, RPB = BLOCK / THREADS;
+  // consecutive rows of a workgroup share one read of the vectors; 8 workgroups of
+  // 256 threads a CU at least
+  const int64_t want = static_cast<int64_t>(device_cu_count()) * 8 * 256 / BLOCK;
+  int64_t per = (p.M + want - 1) / want;
+  per = (per + RPB - 1) / RPB * RPB;
+  return ECHO_LAUNCH("gated_norm", (gated_norm_k<THREADS, NV, VEC>),
+                     dim3(static_cast<unsigned>((p.M + per - 1) / per)), dim3(BLOCK), 0, stream, p,
+                     static_cast<int>(per));
+}
+template <bool VEC>
+hipError_t launch_v(const GatedNormArgs& p, hipStream_t stream) {
+  if (p.D <= 512) return launch_w<64, 1, VEC>(p, stream);
+  if (p.D <= 2048) return launch_w<256, 1, VEC>(p, stream);
+  if (p.D <= 6144) return launch_w<256, 3, VEC>(p, stream);
+  return launch_w<1024, 2, VEC>(p, stream);
+}
+
+}  // namespace
+
+hipError_t launch_gated_norm(const GatedNormArgs& p, hipStream_t stream) {
+  auto rows = [](const void* q, int bf, int64_t ld) {
+    return reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld % (bf ? 8 : 4) == 0;
+  };
+  auto vec = [](const float* q, int64_t ld) { return reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld % 4 == 0; };
+  const bool aligned = p.D % 8 == 0 && rows(p.z, p.z_bf16, p.ldz) && rows(p.x, p.x_bf16, p.ldx) &&
+                       rows(p.y, p.y_bf16, p.ldy) && (p.before == NORM_NONE || rows(p.h, p.h_bf16, p.ldh)) &&
+                       vec(p.w1, 0) && vec(p.w2, 0) && vec(p.gate, p.ldgate) && vec(p.scale, p.ldscale) &&
+                       vec(p.shift, p.ldshift);
+  return aligned ? launch_v<true>(p, stream) : launch_v<false>(p, stream);
+}
+
+}  // namespace echo

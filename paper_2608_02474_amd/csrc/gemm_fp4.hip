@@ -1,0 +1,522 @@
+// Matrix products of rows in 4 bits (quant.hip: codes of one sign, two exponent
+// and one fraction bit, a power of two for every 32 of them):
+//
+//   C[m, n] = f( sum_b 2^(ea[m, b] + eb[n, b]) sum_{k in b} A[m, k] B[n, k] + bias[n] )
+//   f: none, GELU (tanh form), or res[row(m), n] + gate[n] * (.) in fp32
+//
+// v_mfma_scale_f32_16x16x128_f8f6f4 takes 32 codes of one row per lane (16 bytes,
+// one block) and the block's scale byte from another register, multiplies and
+// adds in fp32, and makes a scale of 255 a NaN: nothing is converted on the way.
+// In bytes it is the 8-bit instruction (v_mfma_i32_16x16x64_i8: 16 bytes of a row
+// a lane, 16 cycles), so the tiles, the LDS ring and the epilogue are those of
+// gemm_int8.hip at twice the depth per byte, and the scales are added: a k-step
+// of 128 bytes has 8 of them a row.  They go through a ring of their own, 16
+// bytes a row for two k-steps (a sixteenth of the codes' bytes), and a lane picks
+// its two bytes (blocks q and 4 + q of the step, q = lane / 16) by one v_perm.
+//
+// Rows of codes have a pitch of whole 128 bytes and rows of scales of whole 16,
+// with zeros behind the last column in one operand at least, so the depth has no
+// tail.  M and N are arbitrary: rows past the end re-read the last one and are
+// not stored.
+#include <type_traits>
+
+#include "common.h"
+#include "gemm_rows.h"
+#include "kernels.h"
+#include "launch.h"
+
+namespace echo {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kFp4 = 4;  // the instruction's name for the type (cbsz, blgp)
+
+// c + a b, with byte SEL of sa and of sb the lanes' scales
+template <int SEL>
+__device__ __forceinline__ f32x4 mfma_fp4(const i32x4& a, int sa, const i32x4& b, int sb, const f32x4& c) {
+  const i32x8 a8 = {a[0], a[1], a[2], a[3], 0, 0, 0, 0}, b8 = {b[0], b[1], b[2], b[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, kFp4, kFp4, SEL, sa, SEL, sb);
+}
+
+// RBF: the residual is bf16
+template <int BM, int BN, int EPI, bool CBF, bool RBF>
+__global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_fp4_tile(GemmFp4Args p) {
+  constexpr int kStage = (BM + BN) * 128, kScales = (BM + BN) * 16;
+  constexpr int WM = BM / 2, WN = BN / 2, TI = WM / 16, TJ = WN / 16;
+  constexpr int NM = TI * TJ, NR = TI + TJ;
+  constexpr int CA = BM / 32, CB = BN / 32, NCP = CA + CB;
+  constexpr int NSC = (BM + BN) / 64;  // copies of 64 rows' scales
+  __shared__ __attribute__((aligned(1024))) char smem[2 * kStage + 2 * kScales];
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave;
+  const int wm = wave >> 1, wn = wave & 1;
+  const int l16 = lane & 15, lq = lane >> 4;
+
+  // Workgroups [0, npieces) are k-ranges of the tiles from tile_base on; the rest
+  // take the tiles before it whole, in the order of gemm_int8.hip.
+  const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN;
+  const bool split = static_cast<int>(blockIdx.x) < p.npieces;
+  int pid, ks = 0;
+  if (split) {
+    pid = p.tile_base + blockIdx.x / p.nsplit;
+    ks = blockIdx.x % p.nsplit;
+  } else {
+    constexpr int XW = BM + BN > 256 ? 32 : 64;  // tiles of an XCD that run together
+    const int g = blockIdx.x - p.npieces, xcd = g % 8, loc = g / 8;
+    const int full_waves = (static_cast<int>(gridDim.x) - p.npieces) / (8 * XW);
+    pid = loc < XW * full_waves ? (loc / XW) * 8 * XW + xcd * XW + loc % XW : g;
+  }
+  int tile_m, tile_n;
+  gemm_tile_of(pid, tm, tn, tile_m, tile_n);
+  const int m0 = tile_m * BM, n0 = tile_n * BN;
+  const int nk_all = p.K / 128, kt0 = ks * p.kps;  // kps is even: a range starts with a pair's scales
+  const int nk = split && nk_all - kt0 >= p.kps ? p.kps : nk_all - kt0;  // >= 1
+
+  // copy c of a wave fills the 8 rows 8 (wave + 4 c) .. of the (A ++ B) stage;
+  // lane i takes row i / 8, slot i % 8, which holds chunk (i % 8) ^ ((row >> 1) & 7)
+  const int chunk = ((lane % 8) ^ (((8 * wave + lane / 8) >> 1) & 7)) * 16;
+  uint32_t voff[NCP];
+#pragma unroll
+  for (int c = 0; c < NCP; ++c) {
+    const int r = 8 * (wave + 4 * (c < CA ? c : c - CA)) + lane / 8;
+    const int last = (c < CA ? p.M - m0 : p.N - n0) - 1;
+    voff[c] = static_cast<uint32_t>(r < last ? r : last) * static_cast<uint32_t>(c < CA ? p.lda : p.ldb) + chunk;
+  }
+  // scale copy c of wave w: rows 64 (w + 4 c) .. of A ++ B, a row a lane
+  constexpr int NSW = (NSC + 3) / 4;
+  uint32_t soff[NSW];
+#pragma unroll
+  for (int c = 0; c < NSW; ++c) {
+    const int s = wave + 4 * c, r = (s * 64 < BM ? s * 64 : s * 64 - BM) + lane;
+    const int last = (s * 64 < BM ? p.M - m0 : p.N - n0) - 1;
+    soff[c] = static_cast<uint32_t>(r < last ? r : last) * static_cast<uint32_t>(s * 64 < BM ? p.ldsa : p.ldsb);
+  }
+  const uint8_t* a0 = p.A + static_cast<int64_t>(m0) * p.lda + static_cast<int64_t>(kt0) * 128;
+  const uint8_t* b0 = p.B + static_cast<int64_t>(n0) * p.ldb + static_cast<int64_t>(kt0) * 128;
+  const uint8_t* sa0 = p.sa + static_cast<int64_t>(m0) * p.ldsa + static_cast<int64_t>(kt0) * 8;
+  const uint8_t* sb0 = p.sb + static_cast<int64_t>(n0) * p.ldsb + static_cast<int64_t>(kt0) * 8;
+  const uint32_t dst0 = lds_offset(smem) + wave * 1024, sdst0 = lds_offset(smem) + 2 * kStage + wave * 1024;
+  const uint8_t* src_a = a0;
+  const uint8_t* src_b = b0;
+  uint32_t dst_stage = 0;
+  auto set_fill = [&](int kt) __attribute__((always_inline)) {
+    const int kf = kt < nk ? kt : nk - 1;  // past the last k-step: re-fetched, never used
+    src_a = a0 + static_cast<int64_t>(kf) * 128;
+    src_b = b0 + static_cast<int64_t>(kf) * 128;
+    dst_stage = dst0 + (kt & 1) * kStage;
+  };
+  auto copy = [&](auto c_c) __attribute__((always_inline)) {
+    constexpr int c = decltype(c_c)::value;
+    lds_copy16_s(c < CA ? src_a : src_b, voff[c], dst_stage + c * 4096);
+  };
+  // the scales of k-steps kt and kt + 1 (kt even) into their half of the ring
+  auto copy_scales = [&](int kt) __attribute__((always_inline)) {
+    const int64_t at = (kt < nk ? kt : (nk - 1) & ~1) * 8;
+#pragma unroll
+    for (int c = 0; c < NSW; ++c) {
+      const int s = wave + 4 * c;
+      if (NSC % 4 == 0 || s < NSC)
+        lds_copy16_s((s * 64 < BM ? sa0 : sb0) + at, soff[c], sdst0 + ((kt >> 1) & 1) * kScales + c * 4096);
+    }
+  };
+
+  const int rd_a = (wm * WM + l16) * 128, rd_b = (BM + wn * WN + l16) * 128;
+  const int rd_sa = (wm * WM + l16) * 16, rd_sb = (BM + wn * WN + l16) * 16;
+  const uint32_t pick = 0x0c0c0400u + 0x0101u * lq;  // bytes lq and 4 + lq
+  const int ch0 = (lq ^ (l16 >> 1)) * 16, ch1 = ((4 + lq) ^ (l16 >> 1)) * 16;
+  i32x4 fa[2][TI], fb[2][TJ];
+  int sa[2][TI], sb[2][TJ];  // of k-steps kt & 1
+  f32x4 acc[TI][TJ];
+  auto read = [&](auto set_c, auto q_c, const char* st) __attribute__((always_inline)) {
+    constexpr int SET = decltype(set_c)::value, Q = decltype(q_c)::value;
+    const int ch = SET ? ch1 : ch0;
+    if constexpr (Q == 0)
+      fa[SET][0] = *reinterpret_cast<const i32x4*>(st + rd_a + ch);
+    else if constexpr (Q <= TJ)
+      fb[SET][Q - 1] = *reinterpret_cast<const i32x4*>(st + rd_b + (Q - 1) * 2048 + ch);
+    else
+      fa[SET][Q - TJ] = *reinterpret_cast<const i32x4*>(st + rd_a + (Q - TJ) * 2048 + ch);
+  };
+  auto read_scale = [&](auto par_c, auto q_c, const char* st) __attribute__((always_inline)) {
+    constexpr int PAR = decltype(par_c)::value, Q = decltype(q_c)::value;
+    auto two = [&](int off) __attribute__((always_inline)) {
+      const uint2 w = *reinterpret_cast<const uint2*>(st + off + PAR * 8);
+      return static_cast<int>(__builtin_amdgcn_perm(w.y, w.x, pick));
+    };
+    if constexpr (Q == 0)
+      sa[PAR][0] = two(rd_sa);
+    else if constexpr (Q <= TJ)
+      sb[PAR][Q - 1] = two(rd_sb + (Q - 1) * 256);
+    else
+      sa[PAR][Q - TJ] = two(rd_sa + (Q - TJ) * 256);
+  };
+#pragma unroll
+  for (int i = 0; i < TI; ++i)
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  auto mma = [&](auto par_c, auto set_c, auto t0_c, auto t1_c) __attribute__((always_inline)) {
+    constexpr int SET = decltype(set_c)::value, PAR = decltype(par_c)::value;
+    static_for<decltype(t0_c)::value, decltype(t1_c)::value>([&](auto t_c) __attribute__((always_inline)) {
+      constexpr int T = decltype(t_c)::value;
+      acc[T / TJ][T % TJ] =
+          mfma_fp4<SET>(fb[SET][T % TJ], sb[PAR][T % TJ], fa[SET][T / TJ], sa[PAR][T / TJ], acc[T / TJ][T % TJ]);
+    });
+  };
+  typedef std::integral_constant<int, 0> S0;
+  typedef std::integral_constant<int, 1> S1;
+  typedef std::integral_constant<int, NM / 2> Mid;
+  // A k-step: the first half's MFMAs with the second half's reads between
+  // them; half of the second half's; the wait for this wave's copies of the
+  // next k-step and the barrier; the rest, with the next k-step's first reads
+  // and the copies of the k-step after next into the stage just released.
+  auto phase0 = [&](auto par_c, const char* st) __attribute__((always_inline)) {
+    static_for<0, NR>([&](auto q_c) __attribute__((always_inline)) {
+      constexpr int Q = decltype(q_c)::value;
+      __builtin_amdgcn_sched_barrier(0);
+      read(S1{}, q_c, st);
+      mma(par_c, S0{}, std::integral_constant<int, Q * NM / NR>{}, std::integral_constant<int, (Q + 1) * NM / NR>{});
+    });
+    __builtin_amdgcn_sched_barrier(0);
+    mma(par_c, S1{}, S0{}, Mid{});
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // from k-step kt, of parity PAR, to the next one
+  auto step = [&](auto par_c, int kt) __attribute__((always_inline)) {
+    constexpr int PAR = decltype(par_c)::value;
+    typedef std::integral_constant<int, PAR ^ 1> Next;
+    const char* nxt = smem + (PAR ^ 1) * kStage;
+    const char* nsc = smem + 2 * kStage + (((kt + 1) >> 1) & 1) * kScales;
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));  // this wave's copies of k-step kt + 1
+    __syncthreads();
+    set_fill(kt + 2);
+    if constexpr (PAR == 0) copy_scales(kt + 2);
+    static_for<0, NR>([&](auto q_c) __attribute__((always_inline)) {
+      constexpr int Q = decltype(q_c)::value, M1 = NM - Mid::value;
+      __builtin_amdgcn_sched_barrier(0);
+      read(S0{}, q_c, nxt);
+      read_scale(Next{}, q_c, nsc);
+      static_for<Q * NCP / NR, (Q + 1) * NCP / NR>(copy);
+      mma(par_c, S1{}, std::integral_constant<int, Mid::value + Q * M1 / NR>{},
+          std::integral_constant<int, Mid::value + (Q + 1) * M1 / NR>{});
+    });
+    __builtin_amdgcn_sched_barrier(0);
+    phase0(Next{}, nxt);
+  };
+  copy_scales(0);
+  set_fill(0);
+  static_for<0, NCP>(copy);
+  set_fill(1);
+  static_for<0, NCP>(copy);
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm(NCP));
+  __syncthreads();
+  static_for<0, NR>([&](auto q_c) __attribute__((always_inline)) {
+    read(S0{}, q_c, smem);
+    read_scale(S0{}, q_c, smem + 2 * kStage);
+  });
+  phase0(S0{}, smem);
+  int kt = 0;
+  for (; kt + 2 < nk; kt += 2) {
+    step(S0{}, kt);
+    step(S1{}, kt + 1);
+  }
+  if (kt + 1 < nk) {
+    step(S0{}, kt);
+    mma(S1{}, S1{}, Mid{}, std::integral_constant<int, NM>{});
+  } else {
+    mma(S0{}, S1{}, Mid{}, std::integral_constant<int, NM>{});
+  }
+  __builtin_amdgcn_s_waitcnt(0);  // re-fetched k-steps still landing in LDS
+
+  // lane: channels n0 + wn WN + 16 j + 4 lq .. + 3 of token m0 + wm WM + 16 i + l16
+  if (split) {
+    float* out = p.part + static_cast<int64_t>(blockIdx.x) * BM * BN;
+#pragma unroll
+    for (int i = 0; i < TI; ++i)
+#pragma unroll
+      for (int j = 0; j < TJ; ++j)
+        *reinterpret_cast<f32x4*>(out + (wm * WM + i * 16 + l16) * BN + wn * WN + j * 16 + 4 * lq) = acc[i][j];
+    return;
+  }
+  // The epilogue of gemm_int8.hip: sixteen tokens of the wave's part at a time
+  // through the wave's own piece of LDS, whole rows a store, residuals ahead.
+  constexpr int LD = WN + 4, CPL = WN / 4, RPP = kWave / CPL, NQ = 16 / RPP;
+  static_assert(4 * 16 * LD * 4 <= 2 * kStage, "staging fits the ring");
+  __syncthreads();  // every wave's copies have landed and its last reads are done
+  float* ep = reinterpret_cast<float*>(smem) + wave * 16 * LD;
+  const bool vec = out_vec(p);
+  const int cl = lane % CPL * 4, rl = lane / CPL;
+  const int n = n0 + wn * WN + cl;
+  OutCols cols;
+  if (vec) out_cols4<EPI>(p, n < p.N ? n : p.N - 4, cols);
+  // residuals of group g, raw, two groups ahead of their use
+  constexpr bool RES = EPI == EPI_GATE_RES;
+  constexpr int NPF = 2, NS = NPF + 1;
+  ResRaw<RBF> raw[RES ? NS : 1][RES ? NQ : 1];
+  bool miss[RES ? NS : 1][RES ? NQ : 1];
+  auto fetch = [&](auto g_c) __attribute__((always_inline)) {
+    constexpr int g = decltype(g_c)::value;
+    if constexpr (RES && g < TI) {
+      if (vec) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+          const int m = m0 + wm * WM + g * 16 + rl + q * RPP;
+          const int rr = out_res_row(p, m < p.M ? m : p.M - 1);
+          miss[g % NS][q] = rr < 0;
+          raw[g % NS][q].load(p.res, static_cast<int64_t>(rr < 0 ? 0 : rr) * p.ldr + (n < p.N ? n : p.N - 4));
+        }
+      }
+    }
+  };
+  static_for<0, NPF>(fetch);
+  static_for<0, TI>([&](auto i_c) __attribute__((always_inline)) {
+    constexpr int i = decltype(i_c)::value;
+    const int mi = m0 + wm * WM + i * 16 + rl;
+    fetch(std::integral_constant<int, i + NPF>{});
+    static_for<0, TJ>([&](auto j_c) __attribute__((always_inline)) {
+      constexpr int j = decltype(j_c)::value;
+      // (as there: keeps the accumulators where they are until their turn)
+      if constexpr (BM * BN == 256 * 256) asm volatile("" : "+a"(acc[i][j]));
+      *reinterpret_cast<f32x4*>(ep + l16 * LD + j * 16 + 4 * lq) = acc[i][j];
+    });
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));  // this wave's staged rows are in LDS
+    if (vec) {
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        const f32x4 z = *reinterpret_cast<const f32x4*>(ep + (rl + q * RPP) * LD + cl);
+        float res[4];
+        if constexpr (RES) raw[i % NS][q].unpack(miss[i % NS][q], res);
+        if (mi + q * RPP < p.M && n < p.N) out_store4<EPI, CBF>(p, mi + q * RPP, n, z, cols, res);
+      }
+    } else {
+      for (int e = lane; e < 16 * WN; e += kWave) {
+        const int m = m0 + wm * WM + i * 16 + e / WN, nn = n0 + wn * WN + e % WN;
+        if (m < p.M && nn < p.N) out_store1<EPI, CBF>(p, m, nn, ep[e / WN * LD + e % WN]);
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));  // and read, before the next rows replace them
+    __builtin_amdgcn_sched_barrier(0);
+  });
+}
+
+// The k-ranges of every split tile added in order, in fp32, and the epilogue; a
+// thread takes four channels of a token.
+template <int BM, int BN, int EPI, bool CBF>
+__global__ void __launch_bounds__(256) gemm_fp4_reduce(GemmFp4Args p) {
+  const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN;
+  const int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  const int c4 = static_cast<int>(e % (BN / 4)), r = static_cast<int>((e / (BN / 4)) % BM);
+  const int t = static_cast<int>(e / (static_cast<int64_t>(BM) * (BN / 4)));
+  if (p.tile_base + t >= tm * tn) return;
+  int tile_m, tile_n;
+  gemm_tile_of(p.tile_base + t, tm, tn, tile_m, tile_n);
+  const int m = tile_m * BM + r, n = tile_n * BN + 4 * c4;
+  if (m >= p.M || n >= p.N) return;
+  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s = 0; s < p.nsplit; ++s)
+    acc += *reinterpret_cast<const f32x4*>(p.part + (static_cast<int64_t>(t) * p.nsplit + s) * BM * BN + r * BN +
+                                           4 * c4);
+  out_put4<EPI, CBF>(p, m, n, acc);
+}
+
+// ---- one to eight tokens: the read of the weights is all there is.  A wave
+// takes R channels and reads each in pieces of 1 KB, 16 contiguous bytes (a
+// block) a lane, U pieces of every channel in flight.  The matrix instruction's
+// sixteen rows are then sixteen blocks of ONE channel and its sixteen columns the
+// same blocks of one token: the sums of corresponding blocks, which are wanted,
+// lie on the diagonal of its result and the other 240 are dropped.  At a
+// sixteenth of its rate the instruction is still several times faster than the
+// memory (an MFMA of 16 cycles takes 1 KB, 256 bytes a cycle and CU, where the
+// memory delivers 11), and it needs no conversion of the codes.
+template <int MT, int R, int U, int EPI, bool CBF>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))) gemm_fp4_row(GemmFp4Args p) {
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int n0 = (blockIdx.x * 4 + wave) * R;
+  if (n0 >= p.N) return;
+  const uint8_t *w[R], *ws[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t n = n0 + r < p.N ? n0 + r : p.N - 1;
+    w[r] = p.B + n * p.ldb;
+    ws[r] = p.sb + n * p.ldsb;
+  }
+  f32x4 acc[R][MT];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[r][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int k0 = 0; k0 < p.K; k0 += 1024 * U) {
+    i32x4 wf[U][R], af[U][MT];
+    int wsc[U][R], asc[U][MT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = k0 + u * 1024 + lane * 16, kc = k < p.K ? k : 0;  // past the depth: zeros of the token
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        wf[u][r] = __builtin_bit_cast(i32x4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(w[r] + kc)));
+        wsc[u][r] = ws[r][kc / 16];
+      }
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        const int64_t m = t < p.M ? t : p.M - 1;
+        af[u][t] = *reinterpret_cast<const i32x4*>(p.A + m * p.lda + kc);
+        asc[u][t] = p.sa[m * p.ldsa + kc / 16];
+        if (k >= p.K) af[u][t] = i32x4{0, 0, 0, 0};
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[r][t] = mfma_fp4<0>(wf[u][r], wsc[u][r], af[u][t], asc[u][t], acc[r][t]);
+  }
+  // lane (q, i): rows 4 q .. 4 q + 3 of column i; the diagonal's element of column
+  // i lies in lane (i / 4, i), at i % 4
+  const int i = lane & 15;
+  const bool diag = i / 4 == lane / 16;
+  float sum[R][MT];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      const f32x4 a = acc[r][t];
+      const float v = i % 4 < 2 ? (i % 4 == 0 ? a[0] : a[1]) : (i % 4 == 2 ? a[2] : a[3]);
+      sum[r][t] = wave_sum(diag ? v : 0.0f);
+    }
+  // lane l of pass s stores output 64 s + l = r MT + t: channel n0 + r of token t
+#pragma unroll
+  for (int s = 0; s < (R * MT + 63) / 64; ++s) {
+    float mine = 0.0f;
+#pragma unroll
+    for (int e = 64 * s; e < R * MT && e < 64 * s + 64; ++e) mine = lane == e - 64 * s ? sum[e / MT][e % MT] : mine;
+    const int e = 64 * s + lane, n = n0 + e / MT, m = e % MT;
+    if (e < R * MT && n < p.N && m < p.M) out_store1<EPI, CBF>(p, m, n, mine);
+  }
+}
+
+namespace {
+
+constexpr int kRowMax = 8;  // most tokens of gemm_fp4_row
+
+enum Fp4Tile { FP4_256, FP4_128, FP4_64 };
+constexpr int kTileEdge[] = {256, 128, 64};
+
+// Estimated time of a plan, us, in the form of gemm_int8.hip's estimate.
+struct Fp4Cost {
+  int resident;
+  float start, lat, thr;  // launch and first loads; a k-step
+  float store;            // epilogue, for a workgroup on every CU
+  float join, piece;      // the second launch of a split product; 1 MB of partial sums
+  float cold;             // a k-step's loads with the weights beyond the L2s (32 MB)
+};
+constexpr Fp4Cost kFp4Cost[] = {{1, 7.28f, 1.431f, 1.431f, 7.86f, 3.42f, 0.146f, 0.0f},
+                                {2, 4.52f, 0.288f, 0.432f, 2.01f, 2.40f, 0.215f, 0.043f},
+                                {4, 3.26f, 0.225f, 0.175f, 0.57f, 2.73f, 0.228f, 0.076f}};
+
+struct Fp4Plan {
+  int tile;
+  int base, nsplit, kps;  // tiles from `base` on are split in nsplit ranges of kps k-steps
+  float us;
+};
+
+int64_t fp4_tiles(int tile, int M, int N) {
+  const int64_t e = kTileEdge[tile];
+  return ((M + e - 1) / e) * ((N + e - 1) / e);
+}
+size_t fp4_part_bytes(const Fp4Plan& p, int M, int N) {
+  const size_t e = kTileEdge[p.tile];
+  return p.nsplit < 2 ? 0 : sizeof(float) * e * e * (fp4_tiles(p.tile, M, N) - p.base) * p.nsplit;
+}
+
+float fp4_us(const Fp4Plan& p, int M, int N, int K, int ncu) {
+  const Fp4Cost& c = kFp4Cost[p.tile];
+  const int nk = K / 128;
+  auto run = [&](int64_t pieces, int steps) {
+    const int64_t n = (pieces + ncu - 1) / ncu;  // workgroups on the busiest CU
+    const float full = c.resident * c.thr > c.lat ? c.resident * c.thr : c.lat;
+    const int rest = static_cast<int>(n % c.resident);
+    const float last = rest == 0 ? 0.0f : rest * c.thr > c.lat ? rest * c.thr : c.lat;
+    return (n / c.resident * full + last) * steps + c.store * static_cast<float>(pieces) / ncu;
+  };
+  const float beyond = static_cast<float>(N) * K / 32e6f;
+  float us = c.start + c.cold * (beyond < 1.0f ? beyond : 1.0f) * nk;
+  if (p.base > 0) us += run(p.base, nk);
+  const int64_t tail = fp4_tiles(p.tile, M, N) - p.base;
+  if (tail > 0) us += run(tail * p.nsplit, p.kps) + c.join + c.piece * 1e-6f * fp4_part_bytes(p, M, N);
+  return us;
+}
+
+// Every tile whole; or the tiles beyond the last whole round of the device, or
+// all of them where they are less than a round, split along the depth: the
+// fastest by the estimate.
+Fp4Plan fp4_plan(int M, int N, int K) {
+  const int ncu = device_cu_count(), nk = K / 128;
+  constexpr size_t kMostPartial = size_t(64) << 20;
+  Fp4Plan best{-1, 0, 1, nk, 0.0f};
+  auto consider = [&](int tile, int64_t base, int ns) {
+    const int even = (nk + ns - 1) / ns, kps = ns > 1 ? (even + 1) / 2 * 2 : even;
+    Fp4Plan p{tile, static_cast<int>(base), (nk + kps - 1) / kps, kps, 0.0f};  // every range non-empty
+    if (fp4_part_bytes(p, M, N) > kMostPartial) return;
+    p.us = fp4_us(p, M, N, K, ncu);
+    if (best.tile < 0 || p.us < best.us) best = p;
+  };
+  for (int tile = FP4_256; tile <= FP4_64; ++tile) {
+    const int64_t tiles = fp4_tiles(tile, M, N), round = static_cast<int64_t>(ncu) * kFp4Cost[tile].resident;
+    consider(tile, tiles, 1);
+    for (const int ns : {2, 3, 4, 6, 8, 12, 16})
+      if (nk / ns >= 2 && tiles % round != 0 && tiles < round * 64) consider(tile, tiles / round * round, ns);
+  }
+  return best;
+}
+
+template <int E>
+hipError_t launch_tile(int epi, GemmFp4Args a, const Fp4Plan& plan, hipStream_t stream) {
+  const int tiles = static_cast<int>(fp4_tiles(plan.tile, a.M, a.N)), tail = plan.nsplit > 1 ? tiles - plan.base : 0;
+  a.tile_base = tiles - tail;
+  a.nsplit = plan.nsplit;
+  a.kps = plan.kps;
+  a.npieces = tail * plan.nsplit;
+  return with_epilogue(epi, a.c_bf16, a.res_bf16, [&](auto epi_c, auto bf_c, auto res_c) -> hipError_t {
+    constexpr int EPI = decltype(epi_c)::value;
+    constexpr bool CBF = decltype(bf_c)::value, RBF = decltype(res_c)::value;
+    hipError_t e = ECHO_LAUNCH("gemm_fp4", (gemm_fp4_tile<E, E, EPI, CBF, RBF>),
+                               dim3(static_cast<unsigned>(a.npieces + a.tile_base)), dim3(256), 0, stream, a);
+    if (e != hipSuccess || tail == 0) return e;
+    const int64_t n = static_cast<int64_t>(tail) * E * (E / 4);
+    return ECHO_LAUNCH("gemm_fp4_reduce", (gemm_fp4_reduce<E, E, EPI, CBF>),
+                       dim3(static_cast<unsigned>((n + 255) / 256)), dim3(256), 0, stream, a);
+  });
+}
+
+template <int MT, int R, int U>
+hipError_t launch_row(int epi, const GemmFp4Args& a, hipStream_t stream) {
+  const dim3 grid(static_cast<unsigned>((a.N + 4 * R - 1) / (4 * R)));
+  return with_epilogue(epi, a.c_bf16, 1, [&](auto epi_c, auto bf_c, auto) -> hipError_t {
+    return ECHO_LAUNCH("gemm_fp4_row", (gemm_fp4_row<MT, R, U, decltype(epi_c)::value, decltype(bf_c)::value>), grid,
+                       dim3(256), 0, stream, a);
+  });
+}
+
+}  // namespace
+
+size_t gemm_fp4_partial_bytes(int M, int N, int K) {
+  return M <= kRowMax ? 0 : fp4_part_bytes(fp4_plan(M, N, K), M, N);
+}
+
+hipError_t launch_gemm_fp4(int epi, const GemmFp4Args& a, hipStream_t stream) {
+  if (a.M == 1) return launch_row<1, 2, 3>(epi, a, stream);
+  if (a.M == 2) return launch_row<2, 2, 3>(epi, a, stream);
+  if (a.M <= 4) return launch_row<4, 2, 3>(epi, a, stream);
+  if (a.M <= kRowMax) return launch_row<8, 4, 1>(epi, a, stream);
+  const Fp4Plan plan = fp4_plan(a.M, a.N, a.K);
+  if (fp4_part_bytes(plan, a.M, a.N) > a.part_bytes) return hipErrorInvalidValue;
+  switch (plan.tile) {
+    case FP4_256: return launch_tile<256>(epi, a, plan, stream);
+    case FP4_128: return launch_tile<128>(epi, a, plan, stream);
+    default: return launch_tile<64>(epi, a, plan, stream);
+  }
+}
+
+}  // namespace echo

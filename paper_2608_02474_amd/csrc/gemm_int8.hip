@@ -22,122 +22,13 @@
 #include <type_traits>
 
 #include "common.h"
+#include "gemm_rows.h"
 #include "kernels.h"
 #include "launch.h"
 
 namespace echo {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ float i8_load(const void* p, int bf, int64_t i) {
-  return bf ? bf16_to_f32(static_cast<const bf16_t*>(p)[i]) : static_cast<const float*>(p)[i];
-}
-
-// z -> f(z), res being the residual and gate the channel's gate
-template <int EPI>
-__device__ __forceinline__ float i8_finish(float z, float gate, float res) {
-  if constexpr (EPI == EPI_GELU) return gelu_tanh_fast(z);
-  if constexpr (EPI == EPI_GATE_RES) return fmaf(gate, z, res);
-  return z;
-}
-
-// the residual row of output row m; -1: no such row
-__device__ __forceinline__ int i8_res_row(const GemmI8Args& p, int m) {
-  if (p.res_rows == nullptr) return m;
-  const int r = p.res_rows[m];
-  return r >= 0 && r < p.res_nrows ? r : -1;
-}
-
-// One output; za = the sum, rounded to fp32, times the token's factor.
-template <int EPI, bool CBF>
-__device__ __forceinline__ void i8_store1(const GemmI8Args& p, int m, int n, float za) {
-  const float bias = p.bias != nullptr ? i8_load(p.bias, p.bias_bf16, n) : 0.0f;
-  const float z = fmaf(za, p.sb[n], bias);
-  float res = 0.0f, gate = 0.0f;
-  if constexpr (EPI == EPI_GATE_RES) {
-    const int rr = i8_res_row(p, m);
-    gate = p.gate[n];
-    res = rr < 0 ? __uint_as_float(0x7fc00000u) : i8_load(p.res, p.res_bf16, rr * p.ldr + n);
-  }
-  const float v = i8_finish<EPI>(z, gate, res);
-  const int64_t at = m * p.ldc + n;
-  if constexpr (CBF)
-    Elem<bf16_t>::store(static_cast<bf16_t*>(p.C), at, v);
-  else
-    static_cast<float*>(p.C)[at] = v;
-}
-
-// ---- four consecutive channels at a time, where rows of C, of the residual,
-// and the vectors over the channels are aligned for that and N % 4 == 0 (vec)
-__device__ __forceinline__ bool i8_vec(const GemmI8Args& p) {
-  const uintptr_t ca = reinterpret_cast<uintptr_t>(p.C), ra = reinterpret_cast<uintptr_t>(p.res),
-                  ba = reinterpret_cast<uintptr_t>(p.bias), fa = reinterpret_cast<uintptr_t>(p.sb) |
-                                                                 reinterpret_cast<uintptr_t>(p.gate);
-  const int ce = p.c_bf16 ? 8 : 16, re = p.res_bf16 ? 8 : 16, be = p.bias_bf16 ? 8 : 16;
-  return (p.N & 3) == 0 && (p.ldc & 3) == 0 && (ca & (ce - 1)) == 0 && (p.ldr & 3) == 0 && (ra & (re - 1)) == 0 &&
-         (ba & (be - 1)) == 0 && (fa & 15) == 0;
-}
-__device__ __forceinline__ void i8_load4(const void* p, int bf, int64_t i, float* v) {
-  if (bf) {
-    const uint2 raw = *reinterpret_cast<const uint2*>(static_cast<const bf16_t*>(p) + i);
-    v[0] = __uint_as_float(raw.x << 16);
-    v[1] = __uint_as_float(raw.x & 0xffff0000u);
-    v[2] = __uint_as_float(raw.y << 16);
-    v[3] = __uint_as_float(raw.y & 0xffff0000u);
-  } else {
-    unpack16(ldg16(static_cast<const float*>(p) + i), v, static_cast<const float*>(nullptr));
-  }
-}
-// four residuals as loaded, bf16 or fp32; `miss`: NaN in their place
-template <bool BF>
-struct I8Raw {
-  uint2 v;
-  __device__ void load(const void* p, int64_t i) { v = ldg8_nt(static_cast<const bf16_t*>(p) + i); }
-  __device__ void unpack(bool miss, float* o) const {
-    const uint32_t w[2] = {miss ? 0x7fc07fc0u : v.x, miss ? 0x7fc07fc0u : v.y};
-    o[0] = __uint_as_float(w[0] << 16);
-    o[1] = __uint_as_float(w[0] & 0xffff0000u);
-    o[2] = __uint_as_float(w[1] << 16);
-    o[3] = __uint_as_float(w[1] & 0xffff0000u);
-  }
-};
-template <>
-struct I8Raw<false> {
-  uint4 v;
-  __device__ void load(const void* p, int64_t i) { v = ldg16_nt(static_cast<const float*>(p) + i); }
-  __device__ void unpack(bool miss, float* o) const {
-    unpack16(v, o, static_cast<const float*>(nullptr));
-    if (miss) o[0] = o[1] = o[2] = o[3] = __uint_as_float(0x7fc00000u);
-  }
-};
-
-// scale, bias and gate of channels n .. n + 3
-struct I8Cols {
-  float sb[4], bias[4], gate[4];
-};
-template <int EPI>
-__device__ __forceinline__ void i8_cols4(const GemmI8Args& p, int n, I8Cols& c) {
-  i8_load4(p.sb, 0, n, c.sb);
-  if (p.bias != nullptr)
-    i8_load4(p.bias, p.bias_bf16, n, c.bias);
-  else
-    c.bias[0] = c.bias[1] = c.bias[2] = c.bias[3] = 0.0f;
-  if constexpr (EPI == EPI_GATE_RES) i8_load4(p.gate, 0, n, c.gate);
-}
-template <int EPI, bool CBF>
-__device__ __forceinline__ void i8_store4(const GemmI8Args& p, int m, int n, const f32x4& za, const I8Cols& c,
-                                          const float* res) {
-  float v[4];
-#pragma unroll
-  for (int r = 0; r < 4; ++r)
-    v[r] = i8_finish<EPI>(fmaf(za[r], c.sb[r], c.bias[r]), c.gate[r], res[r]);
-  const int64_t at = m * p.ldc + n;
-  if constexpr (CBF)
-    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.C) + at) =
-        make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-  else
-    stg16(static_cast<float*>(p.C) + at, pack16(v, static_cast<const float*>(nullptr)));
-}
 
 // Four outputs of one token by themselves, vec or not (n < N).
 template <int EPI, bool CBF>
@@ -146,21 +37,7 @@ __device__ __forceinline__ void i8_put4(const GemmI8Args& p, int m, int n, const
   f32x4 za;
 #pragma unroll
   for (int r = 0; r < 4; ++r) za[r] = static_cast<float>(acc[r]) * sa;
-  if (!i8_vec(p)) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (n + r < p.N) i8_store1<EPI, CBF>(p, m, n + r, za[r]);
-    return;
-  }
-  I8Cols cols;
-  i8_cols4<EPI>(p, n, cols);
-  float res[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  if constexpr (EPI == EPI_GATE_RES) {
-    const int rr = i8_res_row(p, m);
-    i8_load4(p.res, p.res_bf16, static_cast<int64_t>(rr < 0 ? 0 : rr) * p.ldr + n, res);
-    if (rr < 0) res[0] = res[1] = res[2] = res[3] = __uint_as_float(0x7fc00000u);
-  }
-  i8_store4<EPI, CBF>(p, m, n, za, cols, res);
+  out_put4<EPI, CBF>(p, m, n, za);
 }
 
 // RBF: the residual is bf16
@@ -317,11 +194,11 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_i8_tile(Ge
   static_assert(4 * 16 * LD * 4 <= 2 * kStage, "staging fits the ring");
   __syncthreads();  // every wave's copies have landed and its last reads are done
   float* ep = reinterpret_cast<float*>(smem) + wave * 16 * LD;
-  const bool vec = i8_vec(p);
+  const bool vec = out_vec(p);
   const int cl = lane % CPL * 4, rl = lane / CPL;
   const int n = n0 + wn * WN + cl;
-  I8Cols cols;
-  if (vec) i8_cols4<EPI>(p, n < p.N ? n : p.N - 4, cols);
+  OutCols cols;
+  if (vec) out_cols4<EPI>(p, n < p.N ? n : p.N - 4, cols);
   float sa[TI];
 #pragma unroll
   for (int i = 0; i < TI; ++i) {
@@ -331,7 +208,7 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_i8_tile(Ge
   // residuals of group g, raw, two groups ahead of their use
   constexpr bool RES = EPI == EPI_GATE_RES;
   constexpr int NPF = 2, NS = NPF + 1;
-  I8Raw<RBF> raw[RES ? NS : 1][RES ? NQ : 1];
+  ResRaw<RBF> raw[RES ? NS : 1][RES ? NQ : 1];
   bool miss[RES ? NS : 1][RES ? NQ : 1];
   auto fetch = [&](auto g_c) __attribute__((always_inline)) {
     constexpr int g = decltype(g_c)::value;
@@ -340,7 +217,7 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_i8_tile(Ge
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
           const int m = m0 + wm * WM + g * 16 + rl + q * RPP;
-          const int rr = i8_res_row(p, m < p.M ? m : p.M - 1);
+          const int rr = out_res_row(p, m < p.M ? m : p.M - 1);
           miss[g % NS][q] = rr < 0;
           raw[g % NS][q].load(p.res, static_cast<int64_t>(rr < 0 ? 0 : rr) * p.ldr + (n < p.N ? n : p.N - 4));
         }
@@ -369,12 +246,12 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_i8_tile(Ge
         const f32x4 z = *reinterpret_cast<const f32x4*>(ep + (rl + q * RPP) * LD + cl);
         float res[4];
         if constexpr (RES) raw[i % NS][q].unpack(miss[i % NS][q], res);
-        if (mi + q * RPP < p.M && n < p.N) i8_store4<EPI, CBF>(p, mi + q * RPP, n, z, cols, res);
+        if (mi + q * RPP < p.M && n < p.N) out_store4<EPI, CBF>(p, mi + q * RPP, n, z, cols, res);
       }
     } else {
       for (int e = lane; e < 16 * WN; e += kWave) {
         const int m = m0 + wm * WM + i * 16 + e / WN, nn = n0 + wn * WN + e % WN;
-        if (m < p.M && nn < p.N) i8_store1<EPI, CBF>(p, m, nn, ep[e / WN * LD + e % WN]);
+        if (m < p.M && nn < p.N) out_store1<EPI, CBF>(p, m, nn, ep[e / WN * LD + e % WN]);
       }
     }
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(63));  // and read, before the next rows replace them
@@ -527,7 +404,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))
 #pragma unroll
     for (int i = 64 * s; i < R * MT && i < 64 * s + 64; ++i) mine = lane == i - 64 * s ? acc[i / MT][i % MT] : mine;
     const int i = 64 * s + lane, n = n0 + i / MT, m = i % MT;
-    if (i < R * MT && n < p.N && m < p.M) i8_store1<EPI, CBF>(p, m, n, static_cast<float>(mine) * p.sa[m]);
+    if (i < R * MT && n < p.N && m < p.M) out_store1<EPI, CBF>(p, m, n, static_cast<float>(mine) * p.sa[m]);
   }
 }
 
@@ -610,18 +487,6 @@ I8Plan i8_plan(int M, int N, int K) {
       if (nk / ns >= 2 && tiles % round != 0 && tiles < round * 64) consider(tile, tiles / round * round, ns);
   }
   return best;
-}
-
-// f(epilogue, whether C, whether the residual is bf16) as compile-time constants
-template <typename F>
-hipError_t with_epilogue(int epi, int c_bf16, int res_bf16, F&& f) {
-  auto go = [&](auto epi_c, auto res_c) -> hipError_t {
-    return c_bf16 ? f(epi_c, std::true_type{}, res_c) : f(epi_c, std::false_type{}, res_c);
-  };
-  if (epi == EPI_GELU) return go(std::integral_constant<int, EPI_GELU>{}, std::true_type{});
-  if (epi != EPI_GATE_RES) return go(std::integral_constant<int, EPI_BIAS>{}, std::true_type{});
-  return res_bf16 ? go(std::integral_constant<int, EPI_GATE_RES>{}, std::true_type{})
-                  : go(std::integral_constant<int, EPI_GATE_RES>{}, std::false_type{});
 }
 
 template <int E>

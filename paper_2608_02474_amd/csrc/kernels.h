@@ -168,6 +168,8 @@ struct QuantizeArgs {
   int8_t* codes;
   int64_t ldq;
   float* row_scale;
+  uint8_t* scales;       // in row_scale's place: rows in 4 bits, two codes a byte,
+  int64_t lds;           // a scale byte for every 32 values, lds bytes between rows
 };
 struct DequantizeArgs {
   const int8_t* codes;
@@ -176,18 +178,16 @@ struct DequantizeArgs {
   int M, D;
   void* y;
   int64_t ldy;
+  const uint8_t* scales;
+  int64_t lds;
 };
 hipError_t launch_quantize_rows(int dtype_bf16, const QuantizeArgs& p, hipStream_t stream);
 hipError_t launch_dequantize_rows(int dtype_bf16, const DequantizeArgs& p, hipStream_t stream);
+hipError_t launch_quantize_rows_fp4(int dtype_bf16, const QuantizeArgs& p, hipStream_t stream);
+hipError_t launch_dequantize_rows_fp4(int dtype_bf16, const DequantizeArgs& p, hipStream_t stream);
 
-// C[m, n] = epilogue(sa[m] sb[n] sum_k A[m, k] B[n, k] + bias[n]), see gemm_int8.hip
-struct GemmI8Args {
-  const int8_t* A;
-  int64_t lda;
-  const float* sa;
-  const int8_t* B;
-  int64_t ldb;
-  const float* sb;
+// where a product of quantized rows goes, and what its epilogue reads (gemm_rows.h)
+struct RowsOut {
   int M, N, K;             // K in bytes, a multiple of 128
   const void* bias;        // [N], optional
   int bias_bf16;
@@ -200,14 +200,86 @@ struct GemmI8Args {
   int64_t ldr;
   const int32_t* res_rows; // optional gather of residual rows
   int res_nrows;
-  int32_t* part;           // partial sums of split products
-  size_t part_bytes;
+  size_t part_bytes;       // room for partial sums of split products
   // set by the launcher: the first split tile, k-ranges of a split tile, k-steps
   // of a range, workgroups that run ranges
   int tile_base, nsplit, kps, npieces;
 };
+
+// C[m, n] = epilogue(sa[m] sb[n] sum_k A[m, k] B[n, k] + bias[n]), see gemm_int8.hip
+struct GemmI8Args : RowsOut {
+  static constexpr bool kScaled = true;
+  const int8_t* A;
+  int64_t lda;
+  const float* sa;
+  const int8_t* B;
+  int64_t ldb;
+  const float* sb;
+  int32_t* part;
+};
 size_t gemm_i8_partial_bytes(int M, int N, int K);
 hipError_t launch_gemm_i8(int epi, const GemmI8Args& a, hipStream_t stream);
+
+// C[m, n] = epilogue(sum_b sa[m, b] sb[n, b] sum_{k in b} A[m, k] B[n, k] + bias[n]), see
+// gemm_fp4.hip: codes of 4 bits, b the blocks of 32, scale bytes e + 127
+struct GemmFp4Args : RowsOut {
+  static constexpr bool kScaled = false;
+  const uint8_t* A;
+  int64_t lda;
+  const uint8_t* sa;
+  int64_t ldsa;
+  const uint8_t* B;
+  int64_t ldb;
+  const uint8_t* sb;
+  int64_t ldsb;
+  float* part;
+};
+size_t gemm_fp4_partial_bytes(int M, int N, int K);
+hipError_t launch_gemm_fp4(int epi, const GemmFp4Args& a, hipStream_t stream);
+
+// ---- rotary positions (rotary.hip)
+struct RotaryArgs {
+  const void *q, *k;
+  void *qo, *ko;
+  int64_t qb, qr, qh, kb, kr, kh, qob, qor, qoh, kob, kor, koh;  // strides of batch, row and head in elements
+  int B, L, H, Hk, dh, dims;
+  int half;                  // pairs (j, j + dims / 2); else (2j, 2j + 1)
+  int grid_h, grid_w;        // > 0: a position is frame, row and column of a grid, by which
+  int pairs_t, pairs_r;      // the first pairs_t pairs, the next pairs_r and the rest turn
+  float magnitude;
+  const int32_t* positions;  // [B][L] (pos_batch elements between elements) or null: the row
+  int64_t pos_batch;
+  const double* freq;        // [dims / 2] radians per position
+};
+hipError_t launch_rotary(int bf16, const RotaryArgs& p, hipStream_t stream);
+
+// ---- norms on both sides of a sub-layer (gated_norm.hip)
+enum NormKind { NORM_NONE = 0, NORM_RMS = 1, NORM_LAYER = 2 };
+struct GatedNormArgs {
+  int M, D, G;
+  int after, before;         // NormKind
+  float alpha, eps;
+  const void* z;
+  int z_bf16;
+  int64_t ldz;
+  const void* x;
+  int x_bf16;
+  int64_t ldx;
+  const int32_t* x_rows;     // optional: the residual of row i is x row x_rows[i]
+  int x_nrows;
+  const float *w1, *w2;      // [D], optional
+  const float *gate, *scale, *shift;  // [G][D], optional
+  int64_t ldgate, ldscale, ldshift;
+  const int32_t* groups;     // [M], optional; else row i has modulation i / rows_per_group
+  int rows_per_group;
+  void* y;
+  int y_bf16;
+  int64_t ldy;
+  void* h;                   // with `before`
+  int h_bf16;
+  int64_t ldh;
+};
+hipError_t launch_gated_norm(const GatedNormArgs& p, hipStream_t stream);
 
 // ---- attention to states of another length (attn_cross.hip)
 struct CrossArgs {
