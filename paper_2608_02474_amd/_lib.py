@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libecho.so")
@@ -142,6 +143,14 @@ class GatedNormCfg(ctypes.Structure):
                 ("ldshift", c_int64)]
 
 
+# The same structures as bytes, for the binding's calls: packing takes a fraction of the
+# time that setting a structure's fields does (26 of them: 0.5 us and 2.2).
+PACK_QUANTIZE_FP4 = struct.Struct("@4i3qf").pack
+PACK_LINEAR_FP4 = struct.Struct("@8i6q").pack
+PACK_ROTARY = struct.Struct("@12if13q").pack
+PACK_GATED_NORM = struct.Struct("@10i2f7q").pack
+
+
 class KernelTime(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char_p), ("launches", c_int64), ("total_ms", c_double)]
 
@@ -196,18 +205,19 @@ _SIGNATURES = {
     "echo_linear_int8": (ctypes.c_int, [_P(LinearInt8Cfg), c_void_p, c_void_p, c_void_p, c_void_p,
                                         c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                         c_size_t, c_void_p]),
+    # (these take their structure or its bytes)
     "echo_fp4_pitch": (c_int64, [c_int32]),
     "echo_fp4_scale_pitch": (c_int64, [c_int32]),
-    "echo_quantize_rows_fp4": (ctypes.c_int, [_P(QuantizeFp4Cfg), c_void_p, c_void_p, c_void_p, c_void_p,
+    "echo_quantize_rows_fp4": (ctypes.c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                               c_void_p, c_void_p, c_void_p]),
-    "echo_dequantize_rows_fp4": (ctypes.c_int, [_P(QuantizeFp4Cfg), c_void_p, c_void_p, c_void_p, c_void_p]),
-    "echo_linear_fp4_workspace": (c_size_t, [_P(LinearFp4Cfg)]),
-    "echo_linear_fp4": (ctypes.c_int, [_P(LinearFp4Cfg), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+    "echo_dequantize_rows_fp4": (ctypes.c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "echo_linear_fp4_workspace": (c_size_t, [c_void_p]),
+    "echo_linear_fp4": (ctypes.c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                        c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
-    "echo_rotary": (ctypes.c_int, [_P(RotaryCfg), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+    "echo_rotary": (ctypes.c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                    c_void_p]),
     "echo_rotary_frequencies": (ctypes.c_int, [_P(RotaryFreqCfg), _P(c_double), _P(c_float)]),
-    "echo_gated_norm": (ctypes.c_int, [_P(GatedNormCfg)] + [c_void_p] * 12),
+    "echo_gated_norm": (ctypes.c_int, [c_void_p] + [c_void_p] * 12),
     "echo_cross_attention_workspace": (c_size_t, [_P(CrossAttentionCfg), c_int32]),
     "echo_cross_attention": (ctypes.c_int, [_P(CrossAttentionCfg), c_void_p, c_void_p, c_void_p,
                                             c_void_p, c_void_p, c_void_p, c_void_p, c_size_t,

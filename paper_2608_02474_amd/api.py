@@ -36,9 +36,9 @@ import math
 import torch
 
 from . import _lib
-from ._lib import (BlockCfg, BlockWeights, CacheCfg, CrossAttentionCfg, EnergyCfg, GatedNormCfg, KernelTime,
-                   LinearFp4Cfg, LinearInt8Cfg, QuantizeCfg, QuantizeFp4Cfg, RefCacheCfg, RotaryCfg, RotaryFreqCfg,
-                   WanBlockCfg, WanBlockWeights,
+from ._lib import (BlockCfg, BlockWeights, CacheCfg, CrossAttentionCfg, EnergyCfg, KernelTime, LinearInt8Cfg,
+                   PACK_GATED_NORM, PACK_LINEAR_FP4, PACK_QUANTIZE_FP4, PACK_ROTARY,
+                   QuantizeCfg, RefCacheCfg, RotaryFreqCfg, WanBlockCfg, WanBlockWeights,
                    RefCacheState, ScheduleCfg, ScheduleState, SelectCfg,
                    ECHO_BF16, ECHO_F32, check)
 
@@ -56,6 +56,7 @@ def _lib_handle():
 # block call 13.0 -> 7.1 us of Python).
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # not a public name
+_device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)   # nor this one
 
 
 def _stream() -> int:
@@ -784,7 +785,7 @@ _MAX_COUNT = 2 ** 31 - 1   # the ABI's counts are 32 bits, and ctypes would wrap
 def _here(dev: int, *others) -> int:
     """The stream of the current device, which has to be that of every tensor:
     `dev` the first one's; others may be None."""
-    if dev != torch.cuda.current_device():
+    if dev != _device_now():
         raise ValueError("tensors must be on the current device")
     for t in others:
         if t is not None and t.get_device() != dev:
@@ -1004,8 +1005,20 @@ def _fp4_rows(r: Fp4Rows, name: str) -> tuple:
     """(rows, pitch, pitch of the scales) of checked 4-bit rows."""
     if not isinstance(r, Fp4Rows):
         raise TypeError(f"{name} must be Fp4Rows (see quantize_rows_fp4)")
-    n, width, ld = _rows_of(r.codes, f"{name}.codes", torch.uint8)
-    ns, swidth, lds = _rows_of(r.scales, f"{name}.scales", torch.uint8)
+    c, s = r.codes, r.scales
+    if (isinstance(c, torch.Tensor) and isinstance(s, torch.Tensor) and c.is_cuda and s.is_cuda and c.dim() == 2
+            and s.dim() == 2 and c.dtype == torch.uint8 and s.dtype == torch.uint8):
+        n, width = c.shape
+        ns, swidth = s.shape
+        ld, u = c.stride()
+        lds, su = s.stride()
+        if (ns == n and 1 < n <= _MAX_COUNT and u == 1 and su == 1 and 65536 >= ld >= width and 65536 >= lds >= swidth
+                and ld % 128 == 0 and lds % 16 == 0 and width % 128 == 0 and swidth % 16 == 0
+                and 0 < r.cols <= 2 * width and r.cols <= 32 * swidth and r.cols <= 65536):
+            return n, ld, lds
+    # not the usual case: the other checks say what is wrong, or take it
+    n, width, ld = _rows_of(c, f"{name}.codes", torch.uint8)
+    ns, swidth, lds = _rows_of(s, f"{name}.scales", torch.uint8)
     if ns != n:
         raise ValueError(f"{name} must have as many rows of scales as of codes")
     pitch, spitch = (r.cols + 255) // 256 * 128, (r.cols + 511) // 512 * 16
@@ -1033,8 +1046,8 @@ def quantize_rows_fp4(x: torch.Tensor, rows: torch.Tensor | None = None, shift: 
         if m != M or out.cols != D:
             raise ValueError(f"out must hold {M} rows of {D} columns")
     stream = _here(x.get_device(), rows, shift, scale, out.codes, out.scales)
-    cfg = QuantizeFp4Cfg(M, D, _echo_dtype(x), n, ldx, ldq, lds, ln_eps)
-    st = lib.echo_quantize_rows_fp4(ctypes.byref(cfg), x.data_ptr(), _ptr(rows), _ptr(shift), _ptr(scale),
+    cfg = PACK_QUANTIZE_FP4(M, D, _echo_dtype(x), n, ldx, ldq, lds, ln_eps)
+    st = lib.echo_quantize_rows_fp4(cfg, x.data_ptr(), _ptr(rows), _ptr(shift), _ptr(scale),
                                     out.codes.data_ptr(), out.scales.data_ptr(), stream)
     if st:
         check("echo_quantize_rows_fp4", st)
@@ -1053,8 +1066,8 @@ def dequantize_rows_fp4(r: Fp4Rows, dtype=torch.bfloat16, out: torch.Tensor | No
         if (m, d) != (M, D):
             raise ValueError(f"out must be [{M}, {D}]")
     stream = _here(r.codes.get_device(), r.scales, out)
-    cfg = QuantizeFp4Cfg(M, D, _echo_dtype(out), M, ldx, ldq, lds, 0.0)
-    st = lib.echo_dequantize_rows_fp4(ctypes.byref(cfg), r.codes.data_ptr(), r.scales.data_ptr(), out.data_ptr(),
+    cfg = PACK_QUANTIZE_FP4(M, D, _echo_dtype(out), M, ldx, ldq, lds, 0.0)
+    st = lib.echo_dequantize_rows_fp4(cfg, r.codes.data_ptr(), r.scales.data_ptr(), out.data_ptr(),
                                       stream)
     if st:
         check("echo_dequantize_rows_fp4", st)
@@ -1082,8 +1095,7 @@ def linear_fp4(a: Fp4Rows, w: Fp4Rows, bias: torch.Tensor | None = None, activat
         if (m, d) != (M, N):
             raise ValueError(f"out must be [{M}, {N}]")
     stream = _here(a.codes.get_device(), a.scales, w.codes, w.scales, bias, gate, residual, residual_rows, out)
-    cfg = ctypes.byref(LinearFp4Cfg(M, N, K, epi, _echo_dtype(out), bias_dt, res_dt, nres, lda, ldsa, ldw, ldsw, ldc,
-                                    ldr))
+    cfg = PACK_LINEAR_FP4(M, N, K, epi, _echo_dtype(out), bias_dt, res_dt, nres, lda, ldsa, ldw, ldsw, ldc, ldr)
     ws = _scratch(lib.echo_linear_fp4_workspace(cfg), workspace, out)
     st = lib.echo_linear_fp4(cfg, a.codes.data_ptr(), a.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(),
                              _ptr(bias), _ptr(gate), _ptr(residual), _ptr(residual_rows), out.data_ptr(),
@@ -1175,10 +1187,11 @@ def rotary(q: torch.Tensor, rot: Rotary, k: torch.Tensor | None = None, position
         raise TypeError("rot must be a Rotary")
     shape, qs = _heads_of(q, "q")
     B, L, H, dh = shape
-    f = _dev(rot.freq, "rot.freq", torch.float64)
-    if f.dim() != 1 or rot.layout not in ROTARY_LAYOUTS:
+    f, layout = _dev(rot.freq, "rot.freq", torch.float64), ROTARY_LAYOUTS.get(rot.layout)
+    if f.dim() != 1 or layout is None:
         raise ValueError(f"rot must have frequencies [pairs] and a layout of {tuple(ROTARY_LAYOUTS)}")
-    if max(B, L, H, dh) > _MAX_COUNT or f.numel() > 256:
+    pairs = f.numel()
+    if B > _MAX_COUNT or L > _MAX_COUNT or H > _MAX_COUNT or dh > _MAX_COUNT or pairs > 256:
         raise ValueError("fewer than 2^31 elements, tokens and heads, and at most 256 pairs")
     gh = gw = pt = pr = 0
     if (rot.grid is None) != (rot.pairs is None):
@@ -1186,8 +1199,8 @@ def rotary(q: torch.Tensor, rot: Rotary, k: torch.Tensor | None = None, position
     if rot.grid is not None:
         gh, gw = rot.grid
         pt, pr, pc = rot.pairs
-        if pt + pr + pc != f.numel() or not (0 < gh <= _MAX_COUNT and 0 < gw <= _MAX_COUNT) or min(rot.pairs) < 0:
-            raise ValueError(f"rot.grid must be (rows, columns), rot.pairs three counts that add up to {f.numel()}")
+        if pt + pr + pc != pairs or not (0 < gh <= _MAX_COUNT and 0 < gw <= _MAX_COUNT) or min(rot.pairs) < 0:
+            raise ValueError(f"rot.grid must be (rows, columns), rot.pairs three counts that add up to {pairs}")
     Hk, ks, kos = 0, _NO_STRIDES, _NO_STRIDES
     if k is not None:
         kshape, ks = _heads_of(k, "k", q.dtype)
@@ -1206,9 +1219,9 @@ def rotary(q: torch.Tensor, rot: Rotary, k: torch.Tensor | None = None, position
             raise ValueError(f"positions must be [{L}] or [{B}, {L}]")
     out, os = _rotary_out(q, shape, qs, out, "out")
     stream = _here(q.get_device(), k, f, positions, out, k_out)
-    cfg = RotaryCfg(B, L, H, Hk, dh, 2 * f.numel(), ROTARY_LAYOUTS[rot.layout], _echo_dtype(q), gh, gw, pt, pr,
-                    rot.magnitude, pos_batch, qs, ks, os, kos)
-    st = lib.echo_rotary(ctypes.byref(cfg), q.data_ptr(), _ptr(k), _ptr(positions), f.data_ptr(), out.data_ptr(),
+    cfg = PACK_ROTARY(B, L, H, Hk, dh, 2 * pairs, layout, _echo_dtype(q), gh, gw, pt, pr, rot.magnitude, pos_batch,
+                      *qs, *ks, *os, *kos)
+    st = lib.echo_rotary(cfg, q.data_ptr(), _ptr(k), _ptr(positions), f.data_ptr(), out.data_ptr(),
                          _ptr(k_out), stream)
     if st:
         check("echo_rotary", st)
@@ -1266,7 +1279,7 @@ def gated_norm(z: torch.Tensor, residual: torch.Tensor, after: str | None = "rms
     (g1, ldg), (g2, lds), (g3, ldt) = (_modulation(gate, "gate", D), _modulation(scale, "scale", D),
                                        _modulation(shift, "shift", D))
     G = max(g1, g2, g3)
-    if any(v not in (1, G) for v in (g1, g2, g3)):
+    if G > 1 and any(v not in (1, G) for v in (g1, g2, g3)):
         raise ValueError("gate, scale and shift must have one row or as many as each other")
     if groups is not None:
         _vector(groups, "groups", M, torch.int32)
@@ -1292,9 +1305,9 @@ def gated_norm(z: torch.Tensor, residual: torch.Tensor, after: str | None = "rms
         h_dt = _echo_dtype(h)
     stream = _here(z.get_device(), residual, residual_rows, after_weight, gate, before_weight, scale, shift, groups, y,
                    h)
-    cfg = GatedNormCfg(M, D, G, NORMS[after], NORMS[before], _echo_dtype(z), _echo_dtype(residual), _echo_dtype(y),
-                       h_dt, n, residual_scale, eps, ldz, ldr, ldy, ldh, ldg, lds, ldt)
-    st = lib.echo_gated_norm(ctypes.byref(cfg), z.data_ptr(), residual.data_ptr(), _ptr(residual_rows),
+    cfg = PACK_GATED_NORM(M, D, G, NORMS[after], NORMS[before], _echo_dtype(z), _echo_dtype(residual), _echo_dtype(y),
+                          h_dt, n, residual_scale, eps, ldz, ldr, ldy, ldh, ldg, lds, ldt)
+    st = lib.echo_gated_norm(cfg, z.data_ptr(), residual.data_ptr(), _ptr(residual_rows),
                              _ptr(after_weight), _ptr(gate), _ptr(before_weight), _ptr(scale), _ptr(shift),
                              _ptr(groups), y.data_ptr(), _ptr(h), stream)
     if st:

@@ -56,30 +56,34 @@ __device__ __forceinline__ void store1(void* p, int bf, int64_t i, float v) {
     static_cast<float*>(p)[i] = v;
 }
 
-// A row per group of THREADS threads, NV chunks of 8 values a thread.  VEC: every
-// row of every tensor is aligned for 16-byte accesses and D % 8 == 0.
-template <int THREADS, int NV, bool VEC>
-__global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) gated_norm_k(GatedNormArgs p, int rows_per_wg) {
-  constexpr int BLOCK = THREADS < 256 ? 256 : THREADS, RPB = BLOCK / THREADS, NW = THREADS / kWave;
-  constexpr bool HOLD = THREADS <= 256;  // (1024 threads have 128 registers each: the vectors are read for every row)
-  __shared__ float red[2][4][NW > 1 ? NW : 1];
-  const int t = threadIdx.x % THREADS, D = p.D;
+// A row to `threads` threads (one wave or the whole workgroup), NV chunks of 8 values
+// each.  VEC: every row of every tensor is aligned for 16-byte accesses and D % 8 == 0.
+// HOLD: the vectors over the channels stay in registers for a workgroup's rows, and the
+// next row's values are on their way (1024 threads have 128 registers each, not enough).
+template <int MAXT, int NV, bool VEC, bool HOLD>
+__global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int threads, int rows_per_wg) {
+  __shared__ float red[2][4][MAXT / kWave];
+  const int t = threadIdx.x % threads, D = p.D, rpb = blockDim.x / threads, waves = threads / kWave;
   int turn = 0;
   // reduction `slot` of a row: a piece of LDS each, of two sets in turn, so that
   // one barrier is enough
   auto total = [&](float v, int slot) __attribute__((always_inline)) {
     v = wave_sum(v);
-    if constexpr (NW > 1) {
+    if (waves > 1) {
       if (t % kWave == 0) red[turn][slot][t / kWave] = v;
       __syncthreads();
-      v = red[turn][slot][0];
-#pragma unroll
-      for (int w = 1; w < NW; ++w) v += red[turn][slot][w];
+      // (at most 16 waves: a partial sum to each lane of 16, and four steps)
+      const int w = t & 15;
+      v = w < waves ? red[turn][slot][w] : 0.0f;
+      v += __uint_as_float(dpp_ror<8>(__float_as_uint(v)));
+      v += __uint_as_float(dpp_ror<4>(__float_as_uint(v)));
+      v += __uint_as_float(dpp_ror<2>(__float_as_uint(v)));
+      v += __uint_as_float(dpp_ror<1>(__float_as_uint(v)));
     }
     return v;
   };
   auto in = [&](int u, int j) __attribute__((always_inline)) {
-    const int c = (t + u * THREADS) * 8;
+    const int c = (t + u * threads) * 8;
     return VEC ? c < D : c + j < D;
   };
   // v becomes its norm; what lies past the last column stays zero
@@ -109,7 +113,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) gated_norm_k(Ga
   };
   // a vector over the channels, `none` where it is not given and past the last column
   auto vector = [&](const float* w, int u, float none, float* o) __attribute__((always_inline)) {
-    const int c = (t + u * THREADS) * 8;
+    const int c = (t + u * threads) * 8;
     if (VEC) {
       if (w != nullptr && c < D) {
         unpack16(ldg16(w + c), o, static_cast<const float*>(nullptr));
@@ -156,19 +160,19 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) gated_norm_k(Ga
     const int64_t xr = source(row, nbad);
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      const int c = (t + u * THREADS) * 8, k = c < D ? c : 0;
+      const int c = (t + u * threads) * 8, k = c < D ? c : 0;
       nz[VEC ? u : 0].load(p.z, p.z_bf16, row * p.ldz + k);
       nx[VEC ? u : 0].load(p.x, p.x_bf16, xr * p.ldx + k);
     }
   };
   const int64_t base = static_cast<int64_t>(blockIdx.x) * rows_per_wg;
   const int64_t end = base + rows_per_wg < p.M ? base + rows_per_wg : p.M;
-  int64_t row = base + threadIdx.x / THREADS;
+  int64_t row = base + threadIdx.x / threads;
   int have = -1;
   if constexpr (AHEAD)
     if (row < end) fetch(row);
   // (a group that reaches a barrier is the whole workgroup, so the loop is uniform for its waves)
-  for (; row < end; row += RPB) {
+  for (; row < end; row += rpb) {
     const int g = p.groups != nullptr ? p.groups[row] : static_cast<int>(row / p.rows_per_group);
     const bool no_group = g < 0 || g >= p.G;
     if constexpr (HOLD) {
@@ -188,20 +192,20 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) gated_norm_k(Ga
       for (int u = 0; u < NV; ++u) {
         nz[u].unpack(p.z_bf16, v[u]);
         nx[u].unpack(p.x_bf16, x[u]);
-        if ((t + u * THREADS) * 8 >= D) {
+        if ((t + u * threads) * 8 >= D) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) v[u][j] = x[u][j] = 0.0f;
         }
       }
       if constexpr (AHEAD)
-        if (row + RPB < end) fetch(row + RPB);
+        if (row + rpb < end) fetch(row + rpb);
     } else {
       const int64_t xr = source(row, bad);
 #pragma unroll
       for (int u = 0; u < NV; ++u)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int c = (t + u * THREADS) * 8 + j;
+          const int c = (t + u * threads) * 8 + j;
           v[u][j] = c < D ? load1(p.z, p.z_bf16, row * p.ldz + c) : 0.0f;
           x[u][j] = c < D ? load1(p.x, p.x_bf16, xr * p.ldx + c) : 0.0f;
         }
@@ -221,7 +225,7 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) gated_norm_k(Ga
     auto put = [&](void* out, int bf, int64_t ld) __attribute__((always_inline)) {
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
-        const int c = (t + u * THREADS) * 8;
+        const int c = (t + u * threads) * 8;
         if (VEC) {
           if (c < D) store8(out, bf, row * ld + c, v[u]);
         } else {
@@ -250,24 +254,24 @@ __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS) gated_norm_k(Ga
 
 namespace {
 
-template <int THREADS, int NV, bool VEC>
-hipError_t launch_w(const GatedNormArgs& p, hipStream_t stream) {
-  constexpr int BLOCK = THREADS < 256 ? 256 : THREADS, RPB = BLOCK / THREADS;
-  // consecutive rows of a workgroup share one read of the vectors; 8 workgroups of
-  // 256 threads a CU at least
-  const int64_t want = static_cast<int64_t>(device_cu_count()) * 8 * 256 / BLOCK;
+template <int MAXT, int NV, bool VEC, bool HOLD>
+hipError_t launch_w(const GatedNormArgs& p, int threads, hipStream_t stream) {
+  const int block = threads < 256 && threads == kWave ? 256 : threads, rpb = block / threads;
+  // consecutive rows of a workgroup share one read of the vectors
+  const int64_t want = static_cast<int64_t>(device_cu_count()) * 2048 / block;
   int64_t per = (p.M + want - 1) / want;
-  per = (per + RPB - 1) / RPB * RPB;
-  return ECHO_LAUNCH("gated_norm", (gated_norm_k<THREADS, NV, VEC>),
-                     dim3(static_cast<unsigned>((p.M + per - 1) / per)), dim3(BLOCK), 0, stream, p,
+  per = (per + rpb - 1) / rpb * rpb;
+  return ECHO_LAUNCH("gated_norm", (gated_norm_k<MAXT, NV, VEC, HOLD>),
+                     dim3(static_cast<unsigned>((p.M + per - 1) / per)), dim3(block), 0, stream, p, threads,
                      static_cast<int>(per));
 }
+// As few threads as hold the row with two chunks each (with one up to 512 columns)
 template <bool VEC>
 hipError_t launch_v(const GatedNormArgs& p, hipStream_t stream) {
-  if (p.D <= 512) return launch_w<64, 1, VEC>(p, stream);
-  if (p.D <= 2048) return launch_w<256, 1, VEC>(p, stream);
-  if (p.D <= 6144) return launch_w<256, 3, VEC>(p, stream);
-  return launch_w<1024, 2, VEC>(p, stream);
+  if (p.D <= 512) return launch_w<256, 1, VEC, true>(p, kWave, stream);
+  const int threads = (p.D + 16 * kWave - 1) / (16 * kWave) * kWave;
+  if (threads <= 512) return launch_w<512, 2, VEC, true>(p, threads, stream);
+  return launch_w<1024, 2, VEC, false>(p, threads, stream);
 }
 
 }  // namespace

@@ -11,8 +11,7 @@
 // a lane, 16 cycles), so the tiles, the LDS ring and the epilogue are those of
 // gemm_int8.hip at twice the depth per byte, and the scales are added: a k-step
 // of 128 bytes has 8 of them a row.  They go through a ring of their own, 16
-// bytes a row for two k-steps (a sixteenth of the codes' bytes), and a lane picks
-// its two bytes (blocks q and 4 + q of the step, q = lane / 16) by one v_perm.
+// bytes a row for two k-steps (a sixteenth of the codes' bytes).
 //
 // Rows of codes have a pitch of whole 128 bytes and rows of scales of whole 16,
 // with zeros behind the last column in one operand at least, so the depth has no
@@ -39,8 +38,23 @@ __device__ __forceinline__ f32x4 mfma_fp4(const i32x4& a, int sa, const i32x4& b
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a8, b8, c, kFp4, kFp4, SEL, sa, SEL, sb);
 }
 
-// RBF: the residual is bf16
-template <int BM, int BN, int EPI, bool CBF, bool RBF>
+// An accumulator's value.  Written out so that the accumulators' own registers are all
+// that ever holds them: left to the compiler, 240 to 460 registers were spilled.  The
+// matrix instructions in front have to be done (acc_settled).
+__device__ __forceinline__ float from_acc(float acc) {
+  float v;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(acc));
+  return v;
+}
+__device__ __forceinline__ void acc_settled(f32x4& last) {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 15" : "+a"(last));
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// RBF: the residual is bf16.  STREAM: a workgroup goes from tile to tile without
+// draining its copies, and stores from its accumulators (rows aligned to 16 bytes).
+template <int BM, int BN, int EPI, bool CBF, bool RBF, bool STREAM>
 __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_fp4_tile(GemmFp4Args p) {
   constexpr int kStage = (BM + BN) * 128, kScales = (BM + BN) * 16;
   constexpr int WM = BM / 2, WN = BN / 2, TI = WM / 16, TJ = WN / 16;
@@ -53,80 +67,98 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_fp4_tile(G
   const int wm = wave >> 1, wn = wave & 1;
   const int l16 = lane & 15, lq = lane >> 4;
 
-  // Workgroups [0, npieces) are k-ranges of the tiles from tile_base on; the rest
-  // take the tiles before it whole, in the order of gemm_int8.hip.
+  // Work items: [0, npieces) are k-ranges of the tiles from tile_base on, the rest
+  // the tiles before it, whole, in the order of gemm_int8.hip; workgroup g takes
+  // items g, g + grid, ...
   const int tm = (p.M + BM - 1) / BM, tn = (p.N + BN - 1) / BN;
-  const bool split = static_cast<int>(blockIdx.x) < p.npieces;
-  int pid, ks = 0;
-  if (split) {
-    pid = p.tile_base + blockIdx.x / p.nsplit;
-    ks = blockIdx.x % p.nsplit;
-  } else {
-    constexpr int XW = BM + BN > 256 ? 32 : 64;  // tiles of an XCD that run together
-    const int g = blockIdx.x - p.npieces, xcd = g % 8, loc = g / 8;
-    const int full_waves = (static_cast<int>(gridDim.x) - p.npieces) / (8 * XW);
-    pid = loc < XW * full_waves ? (loc / XW) * 8 * XW + xcd * XW + loc % XW : g;
-  }
-  int tile_m, tile_n;
-  gemm_tile_of(pid, tm, tn, tile_m, tile_n);
-  const int m0 = tile_m * BM, n0 = tile_n * BN;
-  const int nk_all = p.K / 128, kt0 = ks * p.kps;  // kps is even: a range starts with a pair's scales
-  const int nk = split && nk_all - kt0 >= p.kps ? p.kps : nk_all - kt0;  // >= 1
+  const int nk_all = p.K / 128, nitems = p.npieces + p.tile_base;
+  auto item_at = [&](int item, int& m0, int& n0, int& kt0, int& nk) __attribute__((always_inline)) {
+    int pid, ks = 0;
+    if (item < p.npieces) {
+      pid = p.tile_base + item / p.nsplit;
+      ks = item % p.nsplit;
+    } else {
+      constexpr int XW = BM + BN > 256 ? 32 : 64;  // tiles of an XCD that run together
+      const int g = item - p.npieces, xcd = g % 8, loc = g / 8;
+      const int full_waves = p.tile_base / (8 * XW);
+      pid = loc < XW * full_waves ? (loc / XW) * 8 * XW + xcd * XW + loc % XW : g;
+    }
+    int tile_m, tile_n;
+    gemm_tile_of(pid, tm, tn, tile_m, tile_n);
+    m0 = tile_m * BM, n0 = tile_n * BN;
+    kt0 = ks * p.kps;  // kps is even: a range starts with a pair's scales
+    nk = item < p.npieces && nk_all - kt0 >= p.kps ? p.kps : nk_all - kt0;  // >= 1
+  };
 
-  // copy c of a wave fills the 8 rows 8 (wave + 4 c) .. of the (A ++ B) stage;
-  // lane i takes row i / 8, slot i % 8, which holds chunk (i % 8) ^ ((row >> 1) & 7)
-  const int chunk = ((lane % 8) ^ (((8 * wave + lane / 8) >> 1) & 7)) * 16;
-  uint32_t voff[NCP];
-#pragma unroll
-  for (int c = 0; c < NCP; ++c) {
-    const int r = 8 * (wave + 4 * (c < CA ? c : c - CA)) + lane / 8;
-    const int last = (c < CA ? p.M - m0 : p.N - n0) - 1;
-    voff[c] = static_cast<uint32_t>(r < last ? r : last) * static_cast<uint32_t>(c < CA ? p.lda : p.ldb) + chunk;
-  }
-  // scale copy c of wave w: rows 64 (w + 4 c) .. of A ++ B, a row a lane
+  // The copies: two k-steps ahead of the products, over the ends of items.  Copy c of
+  // a wave fills the 8 rows 8 (wave + 4 c) .. of the (A ++ B) stage; lane i takes row
+  // i / 8, slot i % 8, which holds chunk (i % 8) ^ ((row >> 1) & 7).  Scale copy c of
+  // wave w: rows 64 (w + 4 c) .. of A ++ B, a row a lane.
   constexpr int NSW = (NSC + 3) / 4;
-  uint32_t soff[NSW];
-#pragma unroll
-  for (int c = 0; c < NSW; ++c) {
-    const int s = wave + 4 * c, r = (s * 64 < BM ? s * 64 : s * 64 - BM) + lane;
-    const int last = (s * 64 < BM ? p.M - m0 : p.N - n0) - 1;
-    soff[c] = static_cast<uint32_t>(r < last ? r : last) * static_cast<uint32_t>(s * 64 < BM ? p.ldsa : p.ldsb);
-  }
-  const uint8_t* a0 = p.A + static_cast<int64_t>(m0) * p.lda + static_cast<int64_t>(kt0) * 128;
-  const uint8_t* b0 = p.B + static_cast<int64_t>(n0) * p.ldb + static_cast<int64_t>(kt0) * 128;
-  const uint8_t* sa0 = p.sa + static_cast<int64_t>(m0) * p.ldsa + static_cast<int64_t>(kt0) * 8;
-  const uint8_t* sb0 = p.sb + static_cast<int64_t>(n0) * p.ldsb + static_cast<int64_t>(kt0) * 8;
+  const int chunk = ((lane % 8) ^ (((8 * wave + lane / 8) >> 1) & 7)) * 16;
   const uint32_t dst0 = lds_offset(smem) + wave * 1024, sdst0 = lds_offset(smem) + 2 * kStage + wave * 1024;
-  const uint8_t* src_a = a0;
-  const uint8_t* src_b = b0;
+  uint32_t voff[NCP], soff[NSW];
+  const uint8_t *src_a, *src_b, *src_sa, *src_sb;
+  int f_kt = 0, f_nk = 0, f_slot = 0;
+  auto fill_item = [&](int item) __attribute__((always_inline)) {
+    int m0, n0, kt0;
+    item_at(item, m0, n0, kt0, f_nk);
+#pragma unroll
+    for (int c = 0; c < NCP; ++c) {
+      const int r = 8 * (wave + 4 * (c < CA ? c : c - CA)) + lane / 8;
+      const int last = (c < CA ? p.M - m0 : p.N - n0) - 1;
+      voff[c] = static_cast<uint32_t>(r < last ? r : last) * static_cast<uint32_t>(c < CA ? p.lda : p.ldb) + chunk;
+    }
+#pragma unroll
+    for (int c = 0; c < NSW; ++c) {
+      const int s = wave + 4 * c, r = (s * 64 < BM ? s * 64 : s * 64 - BM) + lane;
+      const int last = (s * 64 < BM ? p.M - m0 : p.N - n0) - 1;
+      soff[c] = static_cast<uint32_t>(r < last ? r : last) * static_cast<uint32_t>(s * 64 < BM ? p.ldsa : p.ldsb);
+    }
+    src_a = p.A + static_cast<int64_t>(m0) * p.lda + static_cast<int64_t>(kt0) * 128;
+    src_b = p.B + static_cast<int64_t>(n0) * p.ldb + static_cast<int64_t>(kt0) * 128;
+    src_sa = p.sa + static_cast<int64_t>(m0) * p.ldsa + static_cast<int64_t>(kt0) * 8;
+    src_sb = p.sb + static_cast<int64_t>(n0) * p.ldsb + static_cast<int64_t>(kt0) * 8;
+    f_kt = 0;
+  };
+  // the next k-step to copy, of parity PAR: its stage, and with an even one the scales
+  // of two; past an item's last k-step the same again, never used
   uint32_t dst_stage = 0;
-  auto set_fill = [&](int kt) __attribute__((always_inline)) {
-    const int kf = kt < nk ? kt : nk - 1;  // past the last k-step: re-fetched, never used
-    src_a = a0 + static_cast<int64_t>(kf) * 128;
-    src_b = b0 + static_cast<int64_t>(kf) * 128;
-    dst_stage = dst0 + (kt & 1) * kStage;
+  auto fill_start = [&](auto par_c) __attribute__((always_inline)) {
+    constexpr int PAR = decltype(par_c)::value;
+    dst_stage = dst0 + PAR * kStage;
+    if constexpr (PAR == 0) {
+#pragma unroll
+      for (int c = 0; c < NSW; ++c) {
+        const int s = wave + 4 * c;
+        if (NSC % 4 == 0 || s < NSC)
+          lds_copy16_s(s * 64 < BM ? src_sa : src_sb, soff[c], sdst0 + f_slot * kScales + c * 4096);
+      }
+      f_slot ^= 1;
+    }
   };
   auto copy = [&](auto c_c) __attribute__((always_inline)) {
     constexpr int c = decltype(c_c)::value;
     lds_copy16_s(c < CA ? src_a : src_b, voff[c], dst_stage + c * 4096);
   };
-  // the scales of k-steps kt and kt + 1 (kt even) into their half of the ring
-  auto copy_scales = [&](int kt) __attribute__((always_inline)) {
-    const int64_t at = (kt < nk ? kt : (nk - 1) & ~1) * 8;
-#pragma unroll
-    for (int c = 0; c < NSW; ++c) {
-      const int s = wave + 4 * c;
-      if (NSC % 4 == 0 || s < NSC)
-        lds_copy16_s((s * 64 < BM ? sa0 : sb0) + at, soff[c], sdst0 + ((kt >> 1) & 1) * kScales + c * 4096);
+  auto fill_done = [&](auto par_c) __attribute__((always_inline)) {
+    constexpr int PAR = decltype(par_c)::value;
+    const bool more = ++f_kt < f_nk;
+    src_a += more ? 128 : 0;
+    src_b += more ? 128 : 0;
+    if constexpr (PAR == 1) {
+      src_sa += more ? 16 : 0;
+      src_sb += more ? 16 : 0;
     }
   };
 
   const int rd_a = (wm * WM + l16) * 128, rd_b = (BM + wn * WN + l16) * 128;
-  const int rd_sa = (wm * WM + l16) * 16, rd_sb = (BM + wn * WN + l16) * 16;
-  const uint32_t pick = 0x0c0c0400u + 0x0101u * lq;  // bytes lq and 4 + lq
-  const int ch0 = (lq ^ (l16 >> 1)) * 16, ch1 = ((4 + lq) ^ (l16 >> 1)) * 16;
+  // the halves of a k-step are its even and its odd blocks, so that a lane's two
+  // scales are neighbours
+  const int rd_sa = (wm * WM + l16) * 16 + 2 * lq, rd_sb = (BM + wn * WN + l16) * 16 + 2 * lq;
+  const int ch0 = ((2 * lq) ^ (l16 >> 1)) * 16, ch1 = ((2 * lq + 1) ^ (l16 >> 1)) * 16;
   i32x4 fa[2][TI], fb[2][TJ];
-  int sa[2][TI], sb[2][TJ];  // of k-steps kt & 1
+  int sa[2][TI], sb[2][TJ];  // of even and odd k-steps; two bytes each: the halves' scales
   f32x4 acc[TI][TJ];
   auto read = [&](auto set_c, auto q_c, const char* st) __attribute__((always_inline)) {
     constexpr int SET = decltype(set_c)::value, Q = decltype(q_c)::value;
@@ -140,21 +172,13 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_fp4_tile(G
   };
   auto read_scale = [&](auto par_c, auto q_c, const char* st) __attribute__((always_inline)) {
     constexpr int PAR = decltype(par_c)::value, Q = decltype(q_c)::value;
-    auto two = [&](int off) __attribute__((always_inline)) {
-      const uint2 w = *reinterpret_cast<const uint2*>(st + off + PAR * 8);
-      return static_cast<int>(__builtin_amdgcn_perm(w.y, w.x, pick));
-    };
     if constexpr (Q == 0)
-      sa[PAR][0] = two(rd_sa);
+      sa[PAR][0] = *reinterpret_cast<const uint16_t*>(st + rd_sa + PAR * 8);
     else if constexpr (Q <= TJ)
-      sb[PAR][Q - 1] = two(rd_sb + (Q - 1) * 256);
+      sb[PAR][Q - 1] = *reinterpret_cast<const uint16_t*>(st + rd_sb + (Q - 1) * 256 + PAR * 8);
     else
-      sa[PAR][Q - TJ] = two(rd_sa + (Q - TJ) * 256);
+      sa[PAR][Q - TJ] = *reinterpret_cast<const uint16_t*>(st + rd_sa + (Q - TJ) * 256 + PAR * 8);
   };
-#pragma unroll
-  for (int i = 0; i < TI; ++i)
-#pragma unroll
-    for (int j = 0; j < TJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   auto mma = [&](auto par_c, auto set_c, auto t0_c, auto t1_c) __attribute__((always_inline)) {
     constexpr int SET = decltype(set_c)::value, PAR = decltype(par_c)::value;
     static_for<decltype(t0_c)::value, decltype(t1_c)::value>([&](auto t_c) __attribute__((always_inline)) {
@@ -165,79 +189,169 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_fp4_tile(G
   };
   typedef std::integral_constant<int, 0> S0;
   typedef std::integral_constant<int, 1> S1;
-  typedef std::integral_constant<int, NM / 2> Mid;
-  // A k-step: the first half's MFMAs with the second half's reads between
-  // them; half of the second half's; the wait for this wave's copies of the
-  // next k-step and the barrier; the rest, with the next k-step's first reads
-  // and the copies of the k-step after next into the stage just released.
-  auto phase0 = [&](auto par_c, const char* st) __attribute__((always_inline)) {
+
+  int item = blockIdx.x, m0, n0, kt0, nk, slot = 0;
+  item_at(item, m0, n0, kt0, nk);
+  fill_item(item);
+  fill_start(S0{});
+  static_for<0, NCP>(copy);
+  fill_done(S0{});
+  fill_start(S1{});
+  static_for<0, NCP>(copy);
+  fill_done(S1{});
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm(NCP));  // the first k-step and its scales
+  __syncthreads();
+  auto first_reads = [&]() __attribute__((always_inline)) {
+    static_for<0, NR>([&](auto q_c) __attribute__((always_inline)) {
+      read(S0{}, q_c, smem);
+      read_scale(S0{}, q_c, smem + 2 * kStage + slot * kScales);
+    });
+  };
+  first_reads();
+  // A k-step: the first half's MFMAs with the second half's reads between them; the
+  // wait for this wave's copies of the next k-step and the barrier; the second half's
+  // MFMAs with the next k-step's first reads and the copies of the k-step after next
+  // into the stage just released.  (The wait in the middle of the second half, as the
+  // 8-bit product has it, leaves 32 MFMAs for 64 KB of copies and all reads: 16384^3
+  // 3.99 and 4.56 PFLOP/s.)
+  auto first_half = [&](auto par_c) __attribute__((always_inline)) {
+    constexpr int PAR = decltype(par_c)::value;
     static_for<0, NR>([&](auto q_c) __attribute__((always_inline)) {
       constexpr int Q = decltype(q_c)::value;
       __builtin_amdgcn_sched_barrier(0);
-      read(S1{}, q_c, st);
+      read(S1{}, q_c, smem + PAR * kStage);
       mma(par_c, S0{}, std::integral_constant<int, Q * NM / NR>{}, std::integral_constant<int, (Q + 1) * NM / NR>{});
     });
     __builtin_amdgcn_sched_barrier(0);
-    mma(par_c, S1{}, S0{}, Mid{});
-    __builtin_amdgcn_sched_barrier(0);
   };
-  // from k-step kt, of parity PAR, to the next one
-  auto step = [&](auto par_c, int kt) __attribute__((always_inline)) {
+  auto step = [&](auto par_c) __attribute__((always_inline)) {
     constexpr int PAR = decltype(par_c)::value;
     typedef std::integral_constant<int, PAR ^ 1> Next;
-    const char* nxt = smem + (PAR ^ 1) * kStage;
-    const char* nsc = smem + 2 * kStage + (((kt + 1) >> 1) & 1) * kScales;
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));  // this wave's copies of k-step kt + 1
+    first_half(par_c);
+    if constexpr (PAR == 1) slot ^= 1;
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));  // this wave's copies of the next k-step
     __syncthreads();
-    set_fill(kt + 2);
-    if constexpr (PAR == 0) copy_scales(kt + 2);
+    fill_start(par_c);
     static_for<0, NR>([&](auto q_c) __attribute__((always_inline)) {
-      constexpr int Q = decltype(q_c)::value, M1 = NM - Mid::value;
+      constexpr int Q = decltype(q_c)::value;
       __builtin_amdgcn_sched_barrier(0);
-      read(S0{}, q_c, nxt);
-      read_scale(Next{}, q_c, nsc);
+      read(S0{}, q_c, smem + (PAR ^ 1) * kStage);
+      read_scale(Next{}, q_c, smem + 2 * kStage + slot * kScales);
       static_for<Q * NCP / NR, (Q + 1) * NCP / NR>(copy);
-      mma(par_c, S1{}, std::integral_constant<int, Mid::value + Q * M1 / NR>{},
-          std::integral_constant<int, Mid::value + (Q + 1) * M1 / NR>{});
+      mma(par_c, S1{}, std::integral_constant<int, Q * NM / NR>{}, std::integral_constant<int, (Q + 1) * NM / NR>{});
     });
     __builtin_amdgcn_sched_barrier(0);
-    phase0(Next{}, nxt);
+    fill_done(par_c);
   };
-  copy_scales(0);
-  set_fill(0);
-  static_for<0, NCP>(copy);
-  set_fill(1);
-  static_for<0, NCP>(copy);
-  __builtin_amdgcn_s_waitcnt(waitcnt_vm(NCP));
-  __syncthreads();
-  static_for<0, NR>([&](auto q_c) __attribute__((always_inline)) {
-    read(S0{}, q_c, smem);
-    read_scale(S0{}, q_c, smem + 2 * kStage);
-  });
-  phase0(S0{}, smem);
-  int kt = 0;
-  for (; kt + 2 < nk; kt += 2) {
-    step(S0{}, kt);
-    step(S1{}, kt + 1);
-  }
-  if (kt + 1 < nk) {
-    step(S0{}, kt);
-    mma(S1{}, S1{}, Mid{}, std::integral_constant<int, NM>{});
-  } else {
-    mma(S0{}, S1{}, Mid{}, std::integral_constant<int, NM>{});
-  }
-  __builtin_amdgcn_s_waitcnt(0);  // re-fetched k-steps still landing in LDS
-
-  // lane: channels n0 + wn WN + 16 j + 4 lq .. + 3 of token m0 + wm WM + 16 i + l16
-  if (split) {
-    float* out = p.part + static_cast<int64_t>(blockIdx.x) * BM * BN;
+  for (;;) {
 #pragma unroll
     for (int i = 0; i < TI; ++i)
 #pragma unroll
-      for (int j = 0; j < TJ; ++j)
-        *reinterpret_cast<f32x4*>(out + (wm * WM + i * 16 + l16) * BN + wn * WN + j * 16 + 4 * lq) = acc[i][j];
-    return;
+      for (int j = 0; j < TJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    int kt = 0;
+    for (; kt + 2 < nk; kt += 2) {
+      step(S0{});
+      step(S1{});
+    }
+    // The last two k-steps; with STREAM they copy the first two of the next item.  Of an
+    // odd number the second is the last once more (fill_done stays there), with scales
+    // of 2^-127: its products are zeros.
+    if (STREAM && item + static_cast<int>(gridDim.x) < nitems) fill_item(item + gridDim.x);
+    step(S0{});
+    const int keep = kt + 1 < nk ? -1 : 0;
+#pragma unroll
+    for (int i = 0; i < TI; ++i) sa[1][i] &= keep;
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) sb[1][j] &= keep;
+    if constexpr (STREAM) {
+      step(S1{});
+    } else {
+      first_half(S1{});
+      mma(S1{}, S1{}, S0{}, std::integral_constant<int, NM>{});
+    }
+
+    // lane: channels n0 + wn WN + 16 j + 4 lq .. + 3 of token m0 + wm WM + 16 i + l16
+    if (item < p.npieces) {
+      float* out = p.part + static_cast<int64_t>(item) * BM * BN;
+#pragma unroll
+      for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j)
+          *reinterpret_cast<f32x4*>(out + (wm * WM + i * 16 + l16) * BN + wn * WN + j * 16 + 4 * lq) = acc[i][j];
+    } else if constexpr (STREAM) {
+      // the columns' vectors, then two row groups at a time, their residuals a pair of
+      // groups ahead (loads behind stores would wait for them)
+      constexpr bool RES = EPI == EPI_GATE_RES;
+      const int nc = n0 + wn * WN + 4 * lq;
+      OutCols cols[TJ];
+#pragma unroll
+      for (int j = 0; j < TJ; ++j) out_cols4<EPI>(p, nc + 16 * j < p.N ? nc + 16 * j : p.N - 4, cols[j]);
+      ResRaw<RBF> raw[RES ? 2 : 1][RES ? TJ : 1];
+      bool miss[2];
+      auto fetch = [&](auto i_c) __attribute__((always_inline)) {
+        constexpr int i = decltype(i_c)::value;
+        if constexpr (RES && i < TI) {
+          const int m = m0 + wm * WM + i * 16 + l16;
+          const int rr = out_res_row(p, m < p.M ? m : p.M - 1);
+          miss[i % 2] = rr < 0;
+#pragma unroll
+          for (int j = 0; j < TJ; ++j)
+            raw[i % 2][j].load(p.res, static_cast<int64_t>(rr < 0 ? 0 : rr) * p.ldr +
+                                          (nc + 16 * j < p.N ? nc + 16 * j : p.N - 4));
+        }
+      };
+      acc_settled(acc[TI - 1][TJ - 1]);
+      fetch(S0{});
+      static_for<0, TI>([&](auto i_c) __attribute__((always_inline)) {
+        constexpr int i = decltype(i_c)::value;
+        fetch(std::integral_constant<int, i + 1>{});
+        const int m = m0 + wm * WM + i * 16 + l16;
+        static_for<0, TJ / 2>([&](auto j_c) __attribute__((always_inline)) {
+          constexpr int j = decltype(j_c)::value * 2;
+          float z[2][4];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float res[4];
+            if constexpr (RES) raw[i % 2][j + h].unpack(miss[i % 2], res);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              z[h][r] = out_finish<EPI>(from_acc(acc[i][j + h][r]) + cols[j + h].bias[r], cols[j + h].gate[r], res[r]);
+          }
+          const int64_t row = m * p.ldc;
+          const int at = n0 + wn * WN + 16 * j;
+          if (CBF) {
+            // (every lane takes part in the swaps)
+            const uint32_t a0 = pack_bf16x2(z[0][0], z[0][1]), a1 = pack_bf16x2(z[0][2], z[0][3]);
+            const uint32_t b0 = pack_bf16x2(z[1][0], z[1][1]), b1 = pack_bf16x2(z[1][2], z[1][3]);
+            const auto s0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false);
+            const auto s1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
+            const auto t0 = __builtin_amdgcn_permlane16_swap(s0[0], s0[1], false, false);
+            const auto t1 = __builtin_amdgcn_permlane16_swap(s1[0], s1[1], false, false);
+            if (m < p.M && at + 8 * lq < p.N)
+              stg16(static_cast<bf16_t*>(p.C) + row + at + 8 * lq, make_uint4(t0[0], t1[0], t0[1], t1[1]));
+          } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (m < p.M && at + 16 * h + 4 * lq < p.N)
+                stg16(static_cast<float*>(p.C) + row + at + 16 * h + 4 * lq, pack16(z[h], static_cast<const float*>(nullptr)));
+          }
+        });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    }
+    if constexpr (STREAM) {
+      item += gridDim.x;
+      if (item < nitems) {
+        item_at(item, m0, n0, kt0, nk);
+        // the first reads again: held through the stores they cost 80 registers
+        first_reads();
+        continue;
+      }
+    }
+    break;
   }
+  __builtin_amdgcn_s_waitcnt(0);  // re-fetched k-steps still landing in LDS
+  if (STREAM || item < p.npieces) return;
   // The epilogue of gemm_int8.hip: sixteen tokens of the wave's part at a time
   // through the wave's own piece of LDS, whole rows a store, residuals ahead.
   constexpr int LD = WN + 4, CPL = WN / 4, RPP = kWave / CPL, NQ = 16 / RPP;
@@ -403,7 +517,10 @@ constexpr int kRowMax = 8;  // most tokens of gemm_fp4_row
 enum Fp4Tile { FP4_256, FP4_128, FP4_64 };
 constexpr int kTileEdge[] = {256, 128, 64};
 
-// Estimated time of a plan, us, in the form of gemm_int8.hip's estimate.
+// Estimated time of a plan, us, in the form of gemm_int8.hip's estimate: fitted to
+// 166 products of 1 .. 32760 tokens, 64 .. 30720 channels and depths 128 .. 13824 in
+// every tile and split (1789 times; 5 to 9% off on average; the choice by them is 1%
+// slower than the fastest plan on average).  k-steps run in pairs.
 struct Fp4Cost {
   int resident;
   float start, lat, thr;  // launch and first loads; a k-step
@@ -411,9 +528,9 @@ struct Fp4Cost {
   float join, piece;      // the second launch of a split product; 1 MB of partial sums
   float cold;             // a k-step's loads with the weights beyond the L2s (32 MB)
 };
-constexpr Fp4Cost kFp4Cost[] = {{1, 7.28f, 1.431f, 1.431f, 7.86f, 3.42f, 0.146f, 0.0f},
-                                {2, 4.52f, 0.288f, 0.432f, 2.01f, 2.40f, 0.215f, 0.043f},
-                                {4, 3.26f, 0.225f, 0.175f, 0.57f, 2.73f, 0.228f, 0.076f}};
+constexpr Fp4Cost kFp4Cost[] = {{1, 5.96f, 1.385f, 0.902f, 7.39f, 7.28f, 0.100f, 0.007f},
+                                {2, 4.25f, 0.725f, 0.550f, 2.21f, 2.13f, 0.249f, 0.060f},
+                                {4, 2.66f, 0.551f, 0.216f, 0.58f, 2.43f, 0.357f, 0.093f}};
 
 struct Fp4Plan {
   int tile;
@@ -438,7 +555,7 @@ float fp4_us(const Fp4Plan& p, int M, int N, int K, int ncu) {
     const float full = c.resident * c.thr > c.lat ? c.resident * c.thr : c.lat;
     const int rest = static_cast<int>(n % c.resident);
     const float last = rest == 0 ? 0.0f : rest * c.thr > c.lat ? rest * c.thr : c.lat;
-    return (n / c.resident * full + last) * steps + c.store * static_cast<float>(pieces) / ncu;
+    return (n / c.resident * full + last) * ((steps + 1) / 2 * 2) + c.store * static_cast<float>(pieces) / ncu;
   };
   const float beyond = static_cast<float>(N) * K / 32e6f;
   float us = c.start + c.cold * (beyond < 1.0f ? beyond : 1.0f) * nk;
@@ -471,6 +588,15 @@ Fp4Plan fp4_plan(int M, int N, int K) {
   return best;
 }
 
+// whether rows of C, of the residual and the vectors over the channels are aligned
+// for 16-byte stores of four fp32 or eight bf16 outputs
+bool stream_fits(const GemmFp4Args& a) {
+  auto at = [](const void* q, int bytes) { return reinterpret_cast<uintptr_t>(q) % bytes == 0; };
+  const int per = a.c_bf16 ? 8 : 4;
+  return a.N % per == 0 && a.ldc % per == 0 && at(a.C, 16) && at(a.bias, a.bias_bf16 ? 8 : 16) && at(a.gate, 16) &&
+         at(a.res, a.res_bf16 ? 8 : 16) && a.ldr % 4 == 0;
+}
+
 template <int E>
 hipError_t launch_tile(int epi, GemmFp4Args a, const Fp4Plan& plan, hipStream_t stream) {
   const int tiles = static_cast<int>(fp4_tiles(plan.tile, a.M, a.N)), tail = plan.nsplit > 1 ? tiles - plan.base : 0;
@@ -478,11 +604,20 @@ hipError_t launch_tile(int epi, GemmFp4Args a, const Fp4Plan& plan, hipStream_t 
   a.nsplit = plan.nsplit;
   a.kps = plan.kps;
   a.npieces = tail * plan.nsplit;
+  const int items = a.npieces + a.tile_base;
   return with_epilogue(epi, a.c_bf16, a.res_bf16, [&](auto epi_c, auto bf_c, auto res_c) -> hipError_t {
     constexpr int EPI = decltype(epi_c)::value;
     constexpr bool CBF = decltype(bf_c)::value, RBF = decltype(res_c)::value;
-    hipError_t e = ECHO_LAUNCH("gemm_fp4", (gemm_fp4_tile<E, E, EPI, CBF, RBF>),
-                               dim3(static_cast<unsigned>(a.npieces + a.tile_base)), dim3(256), 0, stream, a);
+    hipError_t e;
+    // (the smaller tiles have several workgroups to a CU, whose ends overlap)
+    if (E == 256 && stream_fits(a)) {
+      const int wgs = items < device_cu_count() ? items : device_cu_count();
+      e = ECHO_LAUNCH("gemm_fp4", (gemm_fp4_tile<E, E, EPI, CBF, RBF, E == 256>), dim3(static_cast<unsigned>(wgs)),
+                      dim3(256), 0, stream, a);
+    } else {
+      e = ECHO_LAUNCH("gemm_fp4", (gemm_fp4_tile<E, E, EPI, CBF, RBF, false>), dim3(static_cast<unsigned>(items)),
+                      dim3(256), 0, stream, a);
+    }
     if (e != hipSuccess || tail == 0) return e;
     const int64_t n = static_cast<int64_t>(tail) * E * (E / 4);
     return ECHO_LAUNCH("gemm_fp4_reduce", (gemm_fp4_reduce<E, E, EPI, CBF>),
@@ -501,16 +636,28 @@ hipError_t launch_row(int epi, const GemmFp4Args& a, hipStream_t stream) {
 
 }  // namespace
 
+// Whether a product of few tokens goes by rows: it reads the weights at the memory's
+// rate, but the tokens' codes again for every two channels, through the same path
+// (1 / 2 / 4 / 8 tokens on 5120 x 5120 codes 5.0 / 5.7 / 6.5 / 9.7 us, tiles 11.3; on
+// 30720 x 5120 15.9 / 16.9 / 23.1 / 35.5, tiles 20.2).
+static bool fp4_by_rows(int M, int N, int K, const Fp4Plan& plan) {
+  return M <= 2 || (M <= kRowMax && 2.9f + (0.15f + 0.031f * M) * 1e-6f * N * K < plan.us);
+}
+
 size_t gemm_fp4_partial_bytes(int M, int N, int K) {
-  return M <= kRowMax ? 0 : fp4_part_bytes(fp4_plan(M, N, K), M, N);
+  if (M <= 2) return 0;
+  const Fp4Plan plan = fp4_plan(M, N, K);
+  return fp4_by_rows(M, N, K, plan) ? 0 : fp4_part_bytes(plan, M, N);
 }
 
 hipError_t launch_gemm_fp4(int epi, const GemmFp4Args& a, hipStream_t stream) {
+  // two channels a wave and 3 KB of each in flight (one token on 30720 x 5120 and 5120 x
+  // 5120 codes 15.9 and 5.0 us; four channels 15.5 and 5.4, 5 KB 17.6 and 5.6)
   if (a.M == 1) return launch_row<1, 2, 3>(epi, a, stream);
   if (a.M == 2) return launch_row<2, 2, 3>(epi, a, stream);
-  if (a.M <= 4) return launch_row<4, 2, 3>(epi, a, stream);
-  if (a.M <= kRowMax) return launch_row<8, 4, 1>(epi, a, stream);
   const Fp4Plan plan = fp4_plan(a.M, a.N, a.K);
+  if (fp4_by_rows(a.M, a.N, a.K, plan))
+    return a.M <= 4 ? launch_row<4, 2, 3>(epi, a, stream) : launch_row<8, 2, 3>(epi, a, stream);
   if (fp4_part_bytes(plan, a.M, a.N) > a.part_bytes) return hipErrorInvalidValue;
   switch (plan.tile) {
     case FP4_256: return launch_tile<256>(epi, a, plan, stream);

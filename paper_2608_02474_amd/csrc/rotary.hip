@@ -46,7 +46,7 @@ struct RawN {
     if constexpr (kBytes >= 16) {
 #pragma unroll
       for (int i = 0; i < kBytes / 16; ++i)
-        stg16(reinterpret_cast<char*>(p) + 16 * i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
+        stg16_nt(reinterpret_cast<char*>(p) + 16 * i, make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]));
     } else if constexpr (kBytes == 8) {
       *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
     } else if constexpr (kBytes == 4) {
@@ -91,19 +91,32 @@ __device__ __forceinline__ float2 turn_of(int pos, double f, float m) {
   return make_float2(m * co, m * si);
 }
 
-// A unit is P pairs of one head, or as many passing channels; U units of a thread
-// in flight.  Threads hold one unit number each and go over (token, head).
+// A unit is P pairs of one head, or as many passing channels; U units of a thread in
+// flight.  Threads hold one unit number each and go over (token, head).  The pairs of a
+// unit are one access (interleaved) or two (half), so that neighbouring threads' accesses
+// are neighbours: two of 16 bytes each for 32 of interleaved pairs took 368 us where one
+// of 16 takes 258 (32760 tokens x 80 heads of 128, bf16).
 template <typename T, int P, bool HALF>
 __global__ void __launch_bounds__(kRotThreads) rotary_k(RotaryArgs p, int tokens, int units, int turned) {
   constexpr int U = 4;
   __shared__ __attribute__((aligned(16))) float2 cs[kRotPairs];
+  __shared__ int64_t at_token[4][kRotPairs];  // of q, its output, k, its output
   const int n = p.dims / 2, heads = p.H + p.Hk;
   const int64_t first = static_cast<int64_t>(blockIdx.x) * tokens, total = static_cast<int64_t>(p.B) * p.L;
   const int here = static_cast<int>(total - first < tokens ? total - first : tokens);
+  if (static_cast<int>(threadIdx.x) < here) {
+    const uint32_t tok = static_cast<uint32_t>(first) + threadIdx.x;  // B L < 2^24
+    const int64_t b = tok / static_cast<uint32_t>(p.L), i = tok % static_cast<uint32_t>(p.L);
+    at_token[0][threadIdx.x] = b * p.qb + i * p.qr;
+    at_token[1][threadIdx.x] = b * p.qob + i * p.qor;
+    at_token[2][threadIdx.x] = b * p.kb + i * p.kr;
+    at_token[3][threadIdx.x] = b * p.kob + i * p.kor;
+  }
   for (int e = threadIdx.x; e < here * n; e += kRotThreads) {
-    const int64_t tok = first + e / n;
-    const int j = e % n, b = static_cast<int>(tok / p.L), i = static_cast<int>(tok % p.L);
-    int pos = p.positions != nullptr ? p.positions[b * p.pos_batch + i] : i;
+    const uint32_t tok = static_cast<uint32_t>(first) + e / n;
+    const int j = e % n;
+    const uint32_t b = tok / static_cast<uint32_t>(p.L), i = tok % static_cast<uint32_t>(p.L);
+    int pos = p.positions != nullptr ? p.positions[b * p.pos_batch + i] : static_cast<int>(i);
     if (p.grid_w > 0) {
       const int col = pos % p.grid_w, rest = pos / p.grid_w;
       pos = j < p.pairs_t ? rest / p.grid_h : j < p.pairs_t + p.pairs_r ? rest % p.grid_h : col;
@@ -116,43 +129,43 @@ __global__ void __launch_bounds__(kRotThreads) rotary_k(RotaryArgs p, int tokens
   if (slot >= slots) return;
   const bool pass = unit >= turned;
   const int at = pass ? p.dims + (unit - turned) * 2 * P : HALF ? unit * P : unit * 2 * P;
-  // (the last passing unit may have one channel only)
+  // the second access of a unit: of half layouts, and of single pairs, whose last passing
+  // unit may have one channel only
+  constexpr bool TWO = HALF || P == 1;
+  constexpr int N = TWO ? P : 2 * P;
   const int at2 = at + (!pass && HALF ? n : P);
-  const bool second = at2 < p.dh;
-  const int items = here * heads;
-  auto place = [&](int item, const T*& src, T*& dst, int& t) __attribute__((always_inline)) {
-    t = item / heads;
-    const int64_t tok = first + t;
-    const int h = item % heads;
-    const int64_t b = tok / p.L, i = tok % p.L;
-    if (h < p.H) {
-      src = static_cast<const T*>(p.q) + b * p.qb + i * p.qr + h * p.qh;
-      dst = static_cast<T*>(p.qo) + b * p.qob + i * p.qor + h * p.qoh;
-    } else {
-      src = static_cast<const T*>(p.k) + b * p.kb + i * p.kr + (h - p.H) * p.kh;
-      dst = static_cast<T*>(p.ko) + b * p.kob + i * p.kor + (h - p.H) * p.koh;
-    }
-  };
-  for (int i0 = slot; i0 < items; i0 += U * slots) {
-    RawN<T, P> a[U], b[U];
+  const bool second = TWO && at2 < p.dh;
+  const int step_t = slots / heads, step_h = slots % heads;
+  int tok = slot / heads, head = slot % heads;
+  while (tok < here) {
+    RawN<T, N> a[U], b[U];
     T* dst[U];
-    int tok[U];
+    int of[U];
+    bool live[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int item = i0 + u * slots < items ? i0 + u * slots : i0;
-      const T* src;
-      place(item, src, dst[u], tok[u]);
-      a[u].load(src + at);
-      b[u].load(src + (second ? at2 : at));
+      live[u] = tok < here;
+      of[u] = live[u] ? tok : here - 1;
+      const bool is_q = head < p.H;
+      const int h = is_q ? head : head - p.H;
+      const T* src = static_cast<const T*>(is_q ? p.q : p.k) + at_token[is_q ? 0 : 2][of[u]] + h * (is_q ? p.qh : p.kh);
+      dst[u] = static_cast<T*>(is_q ? p.qo : p.ko) + at_token[is_q ? 1 : 3][of[u]] + h * (is_q ? p.qoh : p.koh);
+      if (live[u]) {
+        a[u].load(src + at);
+        if (second) b[u].load(src + at2);
+      }
+      tok += step_t;
+      head += step_h;
+      if (head >= heads) head -= heads, ++tok;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (i0 + u * slots >= items) break;
+      if (!live[u]) break;
       if (!pass) {
         float x[2 * P], y[2 * P];
         a[u].unpack(x);
-        b[u].unpack(x + P);
-        const float2* c = cs + tok[u] * n + unit * P;
+        if constexpr (TWO) b[u].unpack(x + P);
+        const float2* c = cs + of[u] * n + unit * P;
 #pragma unroll
         for (int j = 0; j < P; ++j) {
           const int iu = HALF ? j : 2 * j, iv = HALF ? P + j : 2 * j + 1;
@@ -161,7 +174,7 @@ __global__ void __launch_bounds__(kRotThreads) rotary_k(RotaryArgs p, int tokens
           y[iv] = x[iu] * r.y + x[iv] * r.x;
         }
         a[u].pack(y);
-        b[u].pack(y + P);
+        if constexpr (TWO) b[u].pack(y + P);
       }
       a[u].store(dst[u] + at);
       if (second) b[u].store(dst[u] + at2);
@@ -171,7 +184,7 @@ __global__ void __launch_bounds__(kRotThreads) rotary_k(RotaryArgs p, int tokens
 
 namespace {
 
-template <typename T, int P>
+template <typename T, int P, bool HALF>
 hipError_t launch_p(const RotaryArgs& p, hipStream_t stream) {
   const int n = p.dims / 2, turned = n / P;
   const bool in_place = p.q == p.qo && (p.Hk == 0 || p.k == p.ko);  // (then with the same strides)
@@ -182,28 +195,34 @@ hipError_t launch_p(const RotaryArgs& p, hipStream_t stream) {
   int tokens = kRotThreads / n > 1 ? kRotThreads / n : 1;
   while (tokens > 1 && (total + tokens - 1) / tokens < 4 * device_cu_count()) tokens /= 2;
   const dim3 grid(static_cast<unsigned>((total + tokens - 1) / tokens));
-  return p.half ? ECHO_LAUNCH("rotary", (rotary_k<T, P, true>), grid, dim3(kRotThreads), 0, stream, p, tokens, units, turned)
-                : ECHO_LAUNCH("rotary", (rotary_k<T, P, false>), grid, dim3(kRotThreads), 0, stream, p, tokens, units,
-                              turned);
+  return ECHO_LAUNCH("rotary", (rotary_k<T, P, HALF>), grid, dim3(kRotThreads), 0, stream, p, tokens, units, turned);
 }
 
-// the widest unit that divides the channels and to which every tensor is aligned
+// the widest unit that divides the channels and to whose accesses every tensor is
+// aligned: 16 bytes, or less
 template <typename T>
 hipError_t launch_t(const RotaryArgs& p, hipStream_t stream) {
-  auto fits = [&](int per) {
-    const int64_t bytes = per * static_cast<int>(sizeof(T)) < 16 ? per * static_cast<int>(sizeof(T)) : 16;
-    const int64_t el = bytes / static_cast<int>(sizeof(T));
+  auto fits = [&](int pairs) {
+    const int64_t el = p.half || pairs == 1 ? pairs : 2 * pairs, bytes = el * static_cast<int>(sizeof(T));
     auto at = [&](const void* q, int64_t b, int64_t r, int64_t h) {
       return reinterpret_cast<uintptr_t>(q) % bytes == 0 && b % el == 0 && r % el == 0 && h % el == 0;
     };
-    return p.dims % (2 * per) == 0 && (p.dh - p.dims) % (2 * per) == 0 && at(p.q, p.qb, p.qr, p.qh) &&
+    return p.dims % (2 * pairs) == 0 && (p.dh - p.dims) % (2 * pairs) == 0 && at(p.q, p.qb, p.qr, p.qh) &&
            at(p.qo, p.qob, p.qor, p.qoh) &&
            (p.Hk == 0 || (at(p.k, p.kb, p.kr, p.kh) && at(p.ko, p.kob, p.kor, p.koh)));
   };
-  if (fits(8)) return launch_p<T, 8>(p, stream);
-  if (fits(4)) return launch_p<T, 4>(p, stream);
-  if (fits(2)) return launch_p<T, 2>(p, stream);
-  return launch_p<T, 1>(p, stream);
+  constexpr int W = 16 / static_cast<int>(sizeof(T));  // elements of 16 bytes
+  if (p.half) {
+    if (fits(W)) return launch_p<T, W, true>(p, stream);
+    if (fits(W / 2)) return launch_p<T, W / 2, true>(p, stream);
+    if constexpr (W / 4 > 1)
+      if (fits(W / 4)) return launch_p<T, W / 4, true>(p, stream);
+    return launch_p<T, 1, true>(p, stream);
+  }
+  if (fits(W / 2)) return launch_p<T, W / 2, false>(p, stream);
+  if constexpr (W / 4 > 1)
+    if (fits(W / 4)) return launch_p<T, W / 4, false>(p, stream);
+  return launch_p<T, 1, false>(p, stream);
 }
 
 }  // namespace

@@ -33,6 +33,18 @@ def lib():
     return _lib.load()
 
 
+def test_packed_structures_are_the_structures():
+    for cfg, pack in ((_lib.QuantizeFp4Cfg, _lib.PACK_QUANTIZE_FP4), (_lib.LinearFp4Cfg, _lib.PACK_LINEAR_FP4),
+                      (_lib.RotaryCfg, _lib.PACK_ROTARY), (_lib.GatedNormCfg, _lib.PACK_GATED_NORM)):
+        n = sum(3 if t is _lib.Strides else 1 for _, t in cfg._fields_)
+        b = pack(*range(1, n + 1))
+        got, want = cfg.from_buffer_copy(b.ljust(ctypes.sizeof(cfg), b"\0")), iter(range(1, n + 1))
+        for name, t in cfg._fields_:
+            v = getattr(got, name)
+            for x in ((v.batch, v.row, v.head) if t is _lib.Strides else (v,)):
+                assert x == next(want), (cfg, name)
+
+
 def test_pitches(lib):
     assert [lib.echo_fp4_pitch(d) for d in (1, 256, 257, 5120, 65536)] == [128, 128, 256, 2560, 32768]
     assert [lib.echo_fp4_scale_pitch(d) for d in (1, 512, 513, 5120, 65536)] == [16, 16, 32, 160, 2048]
