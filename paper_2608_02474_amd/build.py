@@ -22,7 +22,7 @@ ARCH = "gfx950"
 
 SOURCES = ["echo_abi.cpp", "energy.hip", "select.hip", "cache.hip", "block_ln.hip",
            "gemm_bf16.hip", "attn_bf16.hip", "block_f32.hip", "refcache.hip", "wan.hip",
-           "mfma_ceiling.hip", "quant.hip", "gemm_int8.hip", "gemm_fp4.hip", "rotary.hip",
+           "mfma_ceiling.hip", "quant.hip", "quant_fp4.hip", "gemm_int8.hip", "gemm_fp4.hip", "rotary.hip",
            "gated_norm.hip", "attn_cross.hip"]
 
 # Packed fp32 instructions are disabled for every device pass.

@@ -223,6 +223,14 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
+// the sum of 16 neighbouring lanes, in all of them
+__device__ __forceinline__ float sum16(float v) {
+  v += __uint_as_float(dpp_ror<8>(__float_as_uint(v)));
+  v += __uint_as_float(dpp_ror<4>(__float_as_uint(v)));
+  v += __uint_as_float(dpp_ror<2>(__float_as_uint(v)));
+  return v + __uint_as_float(dpp_ror<1>(__float_as_uint(v)));
+}
+
 // maximum and sum over lanes l and l ^ 32
 __device__ __forceinline__ float pair_max(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);

@@ -18,26 +18,6 @@
 
 namespace echo {
 
-// 8 elements of either type (the type is uniform over the launch)
-struct Any8 {
-  uint4 a, b;
-  __device__ __forceinline__ void load(const void* p, int bf, int64_t i) {
-    if (bf) {
-      a = ldg16_nt(static_cast<const bf16_t*>(p) + i);
-    } else {
-      a = ldg16_nt(static_cast<const float*>(p) + i);
-      b = ldg16_nt(static_cast<const float*>(p) + i + 4);
-    }
-  }
-  __device__ __forceinline__ void unpack(int bf, float* o) const {
-    if (bf) {
-      unpack16(a, o, static_cast<const bf16_t*>(nullptr));
-    } else {
-      unpack16(a, o, static_cast<const float*>(nullptr));
-      unpack16(b, o + 4, static_cast<const float*>(nullptr));
-    }
-  }
-};
 __device__ __forceinline__ void store8(void* p, int bf, int64_t i, const float* v) {
   if (bf) {
     stg16(static_cast<bf16_t*>(p) + i, pack16(v, static_cast<const bf16_t*>(nullptr)));
@@ -56,11 +36,10 @@ __device__ __forceinline__ void store1(void* p, int bf, int64_t i, float v) {
     static_cast<float*>(p)[i] = v;
 }
 
-// A row to `threads` threads (one wave or the whole workgroup), NV chunks of 8 values
-// each.  VEC: every row of every tensor is aligned for 16-byte accesses and D % 8 == 0.
-// HOLD: the vectors over the channels stay in registers for a workgroup's rows, and the
-// next row's values are on their way (1024 threads have 128 registers each, not enough).
-template <int MAXT, int NV, bool VEC, bool HOLD>
+// A row to `threads` threads (16 if NARROW, one wave or the whole workgroup), NV chunks
+// of 8 values each.  VEC: every row of every tensor is aligned for 16-byte accesses and D % 8 == 0.
+// HOLD: the vectors over the channels stay in registers for a workgroup's rows.
+template <int MAXT, int NV, bool VEC, bool HOLD, bool NARROW, typename TZ, typename TX>
 __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int threads, int rows_per_wg) {
   __shared__ float red[2][4][MAXT / kWave];
   const int t = threadIdx.x % threads, D = p.D, rpb = blockDim.x / threads, waves = threads / kWave;
@@ -68,17 +47,14 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
   // reduction `slot` of a row: a piece of LDS each, of two sets in turn, so that
   // one barrier is enough
   auto total = [&](float v, int slot) __attribute__((always_inline)) {
+    if constexpr (NARROW) return sum16(v);
     v = wave_sum(v);
     if (waves > 1) {
       if (t % kWave == 0) red[turn][slot][t / kWave] = v;
       __syncthreads();
       // (at most 16 waves: a partial sum to each lane of 16, and four steps)
       const int w = t & 15;
-      v = w < waves ? red[turn][slot][w] : 0.0f;
-      v += __uint_as_float(dpp_ror<8>(__float_as_uint(v)));
-      v += __uint_as_float(dpp_ror<4>(__float_as_uint(v)));
-      v += __uint_as_float(dpp_ror<2>(__float_as_uint(v)));
-      v += __uint_as_float(dpp_ror<1>(__float_as_uint(v)));
+      v = sum16(w < waves ? red[turn][slot][w] : 0.0f);
     }
     return v;
   };
@@ -145,9 +121,8 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
     vector(p.shift != nullptr ? p.shift + g * p.ldshift : nullptr, u, 0.0f, o);
   };
   float ga[HOLD ? NV : 1][8], sc[HOLD ? NV : 1][8], sh[HOLD ? NV : 1][8];
-  constexpr bool AHEAD = VEC && HOLD;
-  constexpr int kUnroll = VEC ? NV : 1;
-  Any8 nz[kUnroll], nx[kUnroll];
+  Raw8<TZ> nz[VEC ? NV : 1];
+  Raw8<TX> nx[VEC ? NV : 1];
   bool nbad = false;
   auto source = [&](int64_t row, bool& bad) __attribute__((always_inline)) -> int64_t {
     bad = false;
@@ -161,15 +136,15 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       const int c = (t + u * threads) * 8, k = c < D ? c : 0;
-      nz[VEC ? u : 0].load(p.z, p.z_bf16, row * p.ldz + k);
-      nx[VEC ? u : 0].load(p.x, p.x_bf16, xr * p.ldx + k);
+      nz[VEC ? u : 0].load_nt(static_cast<const TZ*>(p.z) + row * p.ldz + k);
+      nx[VEC ? u : 0].load_nt(static_cast<const TX*>(p.x) + xr * p.ldx + k);
     }
   };
   const int64_t base = static_cast<int64_t>(blockIdx.x) * rows_per_wg;
   const int64_t end = base + rows_per_wg < p.M ? base + rows_per_wg : p.M;
   int64_t row = base + threadIdx.x / threads;
   int have = -1;
-  if constexpr (AHEAD)
+  if constexpr (VEC)
     if (row < end) fetch(row);
   // (a group that reaches a barrier is the whole workgroup, so the loop is uniform for its waves)
   for (; row < end; row += rpb) {
@@ -183,45 +158,41 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
       }
     }
     const int gm = no_group ? 0 : g;
-    float v[NV][8], x[NV][8];
-    bool bad;
-    if constexpr (VEC) {
-      if constexpr (!AHEAD) fetch(row);
-      bad = nbad;
+    float v[NV][8];
+    int64_t xr = 0;
+    bool bad = nbad;
+    if constexpr (!VEC) xr = source(row, bad);
 #pragma unroll
-      for (int u = 0; u < NV; ++u) {
-        nz[u].unpack(p.z_bf16, v[u]);
-        nx[u].unpack(p.x_bf16, x[u]);
-        if ((t + u * threads) * 8 >= D) {
+    for (int u = 0; u < NV; ++u) {
+      if constexpr (VEC) nz[u].unpack(v[u]);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) v[u][j] = x[u][j] = 0.0f;
-        }
-      }
-      if constexpr (AHEAD)
-        if (row + rpb < end) fetch(row + rpb);
-    } else {
-      const int64_t xr = source(row, bad);
-#pragma unroll
-      for (int u = 0; u < NV; ++u)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int c = (t + u * threads) * 8 + j;
+      for (int j = 0; j < 8; ++j) {
+        const int c = (t + u * threads) * 8 + j;
+        if constexpr (VEC)
+          v[u][j] = in(u, j) ? v[u][j] : 0.0f;
+        else
           v[u][j] = c < D ? load1(p.z, p.z_bf16, row * p.ldz + c) : 0.0f;
-          x[u][j] = c < D ? load1(p.x, p.x_bf16, xr * p.ldx + c) : 0.0f;
-        }
+      }
     }
     bad = bad || no_group;
     if (p.after != NORM_NONE) norm(v, p.after, 0);
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      float m[8];
+      float m[8], x[8];
       if constexpr (!HOLD) gate_of(gm, u, m);
+      if constexpr (VEC) nx[u].unpack(x);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        v[u][j] = fmaf(v[u][j], HOLD ? ga[HOLD ? u : 0][j] : m[j], p.alpha * x[u][j]);
-        if (bad) v[u][j] = in(u, j) ? __uint_as_float(0x7fc00000u) : 0.0f;
+        const int c = (t + u * threads) * 8 + j;
+        if constexpr (!VEC) x[j] = c < D ? load1(p.x, p.x_bf16, xr * p.ldx + c) : 0.0f;
+        v[u][j] = fmaf(v[u][j], HOLD ? ga[HOLD ? u : 0][j] : m[j], p.alpha * x[j]);
+        if (bad) v[u][j] = __uint_as_float(0x7fc00000u);
+        if (!in(u, j)) v[u][j] = 0.0f;
       }
     }
+    // the next row's values, on their way through the stores and the second norm
+    if constexpr (VEC)
+      if (row + rpb < end) fetch(row + rpb);
     auto put = [&](void* out, int bf, int64_t ld) __attribute__((always_inline)) {
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
@@ -254,24 +225,32 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
 
 namespace {
 
-template <int MAXT, int NV, bool VEC, bool HOLD>
+template <int MAXT, int NV, bool VEC, bool HOLD, bool NARROW = false>
 hipError_t launch_w(const GatedNormArgs& p, int threads, hipStream_t stream) {
-  const int block = threads < 256 && threads == kWave ? 256 : threads, rpb = block / threads;
+  const int block = threads <= kWave ? 256 : threads, rpb = block / threads;
   // consecutive rows of a workgroup share one read of the vectors
   const int64_t want = static_cast<int64_t>(device_cu_count()) * 2048 / block;
   int64_t per = (p.M + want - 1) / want;
   per = (per + rpb - 1) / rpb * rpb;
-  return ECHO_LAUNCH("gated_norm", (gated_norm_k<MAXT, NV, VEC, HOLD>),
-                     dim3(static_cast<unsigned>((p.M + per - 1) / per)), dim3(block), 0, stream, p, threads,
-                     static_cast<int>(per));
+  const dim3 grid(static_cast<unsigned>((p.M + per - 1) / per));
+  auto go = [&](auto z, auto x) -> hipError_t {
+    return ECHO_LAUNCH("gated_norm", (gated_norm_k<MAXT, NV, VEC, HOLD, NARROW, decltype(z), decltype(x)>), grid, dim3(block), 0,
+                       stream, p, threads, static_cast<int>(per));
+  };
+  if (!VEC) return go(0.0f, 0.0f);  // (its loads go by the tensors' types themselves)
+  if (p.z_bf16) return p.x_bf16 ? go(bf16_t{}, bf16_t{}) : go(bf16_t{}, 0.0f);
+  return p.x_bf16 ? go(0.0f, bf16_t{}) : go(0.0f, 0.0f);
 }
-// As few threads as hold the row with two chunks each (with one up to 512 columns)
+// The fewest chunks a thread that 256 threads hold the row with (wider ones: four to
+// 512 threads), and no more threads than that takes
 template <bool VEC>
 hipError_t launch_v(const GatedNormArgs& p, hipStream_t stream) {
-  if (p.D <= 512) return launch_w<256, 1, VEC, true>(p, kWave, stream);
-  const int threads = (p.D + 16 * kWave - 1) / (16 * kWave) * kWave;
-  if (threads <= 512) return launch_w<512, 2, VEC, true>(p, threads, stream);
-  return launch_w<1024, 2, VEC, false>(p, threads, stream);
+  auto threads = [&](int chunks) { return (p.D + 8 * chunks * kWave - 1) / (8 * chunks * kWave) * kWave; };
+  if (p.D <= 128) return launch_w<256, 1, VEC, true, true>(p, 16, stream);
+  if (p.D <= 2048) return launch_w<256, 1, VEC, true>(p, threads(1), stream);
+  if (p.D <= 4096) return launch_w<256, 2, VEC, true>(p, threads(2), stream);
+  if (p.D <= 6144) return launch_w<256, 3, VEC, true>(p, threads(3), stream);
+  return launch_w<512, 4, VEC, false>(p, threads(4), stream);
 }
 
 }  // namespace

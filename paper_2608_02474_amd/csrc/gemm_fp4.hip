@@ -1,4 +1,4 @@
-// Matrix products of rows in 4 bits (quant.hip: codes of one sign, two exponent
+// Matrix products of rows in 4 bits (quant_fp4.hip: codes of one sign, two exponent
 // and one fraction bit, a power of two for every 32 of them):
 //
 //   C[m, n] = f( sum_b 2^(ea[m, b] + eb[n, b]) sum_{k in b} A[m, k] B[n, k] + bias[n] )

@@ -22,20 +22,6 @@
 //
 // One pass: a row stays in the registers of its wave (or of a workgroup, for
 // longer rows) between the maximum and the codes.
-//
-// Rows held in 4 bits (microscaled floating point, the FP4 form of the same
-// kernel): every 32 values of a row have a power of two of their own,
-//
-//   e_b = max(floor(log2 max_{j in b} |a_ij|) - 2, -127),   c_ij = rn(a_ij / 2^e_b)
-//
-// c of one sign, two exponent and one fraction bit (0, 0.5, 1, 1.5, 2, 3, 4, 6),
-// halves to the even code, magnitudes above 6 to 6; the scale is the byte e_b +
-// 127, 255 (NaN) for a block that is not finite.  The quotient is exact, so the
-// code is the value rounded once, by v_cvt_scalef32_pk_fp4_f32.  The instruction
-// takes its scale as an fp32 number, of which 2^-127 is a denormal one: such
-// blocks are multiplied by 2^64 first.  Two codes a byte, the even column's in
-// the low half.  A block's values lie in four neighbouring lanes, so its maximum
-// is two DPP moves and no row is reduced as a whole (but for LayerNorm).
 #include <type_traits>
 
 #include "common.h"
@@ -74,39 +60,11 @@ __device__ __forceinline__ uint2 codes8(const float* v, float amax, float inv, b
   return make_uint2(w[0], w[1]);
 }
 
-// The 4-bit codes of a lane's 8 values, packed, and the scale byte of the block
-// of 32 that they are a quarter of (lanes 4 n .. 4 n + 3 hold a block).
-__device__ __forceinline__ uint32_t codes8_fp4(const float* v, bool bad, uint32_t& scale) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) top = max(top, abs_bits(v[j]));
-  top = max(top, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(top), 0xb1, 0xf, 0xf, false)));
-  top = max(top, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(top), 0x4e, 0xf, 0xf, false)));
-  bad = bad || top >= 0x7f800000u;
-  const uint32_t e = top >> 23, byte = e > 2 ? e - 2 : 0;
-  scale = bad ? 255u : byte;
-  uint32_t w = 0;
-  if (byte > 0) {
-    const float s = __uint_as_float(byte << 23);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], s, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], s, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], s, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], s, 3);
-  } else {
-    constexpr float k = 0x1p64f, s = 0x1p-63f;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0] * k, v[1] * k, s, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * k, v[3] * k, s, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4] * k, v[5] * k, s, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6] * k, v[7] * k, s, 3);
-  }
-  return bad ? 0u : w;
-}
-
 // One row per group of THREADS threads, NV chunks of 8 values per thread; a
 // group goes from row to row, the next row's values on their way while one is
 // worked on (VEC).  With LN (NV <= 4) the modulation stays in registers for all
 // its rows: read again for each it was four times the bytes of a bf16 row.
-template <typename T, int THREADS, int NV, bool VEC, bool LN, bool FP4>
+template <typename T, int THREADS, int NV, bool VEC, bool LN>
 __global__ void __launch_bounds__(THREADS < 256 ? 256 : THREADS)
 quantize_rows_k(QuantizeArgs p) {
   constexpr int BLOCK = THREADS < 256 ? 256 : THREADS, RPB = BLOCK / THREADS, NW = THREADS / kWave;
@@ -133,8 +91,7 @@ quantize_rows_k(QuantizeArgs p) {
     }
     return v;
   };
-  // chunks of 8 values to write, the padding included, and (FP4) those that scales are written for
-  const int D = p.D, nch = FP4 ? (D + 255) / 256 * 32 : static_cast<int>(p.ldq / 8), nsc = (D + 511) / 512 * 64;
+  const int D = p.D, nch = static_cast<int>(p.ldq / 8);
   auto source = [&](int64_t row, bool& bad) __attribute__((always_inline)) {
     int64_t src = row;
     bad = false;
@@ -247,21 +204,6 @@ quantize_rows_k(QuantizeArgs p) {
           v[u][j] = fmaf(v[u][j] * rstd, HOLD ? sc[HOLD ? u : 0][j] : c8[j], HOLD ? sh[HOLD ? u : 0][j] : h8[j]);
       }
     }
-    if constexpr (FP4) {
-      static_assert(THREADS >= kWave, "sixteen lanes hold four neighbouring blocks");
-#pragma unroll
-      for (int u = 0; u < NV; ++u) {
-        const int c = t + u * THREADS;
-        uint32_t sc4;
-        const uint32_t w = codes8_fp4(v[u], bad, sc4);
-        if (c < nch) *reinterpret_cast<uint32_t*>(p.codes + row * p.ldq + c * 4) = w;
-        sc4 <<= (c / 4 % 4) * 8;  // the scales of sixteen lanes as one word
-        sc4 |= dpp_ror<4>(sc4);
-        sc4 |= dpp_ror<8>(sc4);
-        if (c % 16 == 0 && c < nsc) *reinterpret_cast<uint32_t*>(p.scales + row * p.lds + c / 4) = sc4;
-      }
-      continue;
-    }
     // the largest magnitude as bits: those of infinities and NaN are above every number's
     uint32_t top = 0;
 #pragma unroll
@@ -315,45 +257,18 @@ __global__ void __launch_bounds__(256) dequantize_rows_k(DequantizeArgs p, int v
   }
 }
 
-// y_ij = cast(2^e_b c_ij), exact in both types; a thread takes 8 values
-template <typename T>
-__global__ void __launch_bounds__(256) dequantize_rows_fp4_k(DequantizeArgs p, int vec) {
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  const int nch = (p.D + 7) / 8;
-  for (int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; e < static_cast<int64_t>(p.M) * nch;
-       e += static_cast<int64_t>(gridDim.x) * 256) {
-    const int64_t row = e / nch;
-    const int c = static_cast<int>(e % nch) * 8;
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(p.codes + row * p.ldq + c / 2);
-    const uint32_t b = p.scales[row * p.lds + c / 32];
-    // 2^-127 is a denormal number, 255 a NaN
-    const float s = __uint_as_float(b == 255u ? 0x7fc00000u : b == 0u ? 0x00400000u : b << 23);
-    const f32x2 u0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0), u1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1),
-                u2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2), u3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
-    const float v[8] = {s * u0[0], s * u0[1], s * u1[0], s * u1[1], s * u2[0], s * u2[1], s * u3[0], s * u3[1]};
-    T* y = static_cast<T*>(p.y) + row * p.ldy + c;
-    if (vec) {
-      constexpr int PV = Elem<T>::kPerVec;
-#pragma unroll
-      for (int h = 0; h < 8 / PV; ++h) stg16_nt(y + h * PV, pack16(v + h * PV, static_cast<const T*>(nullptr)));
-    } else {
-      for (int j = 0; j < 8 && c + j < p.D; ++j) Elem<T>::store(y, j, v[j]);
-    }
-  }
-}
-
 namespace {
 
 constexpr int kMaxGroups = 1 << 20;  // workgroups of a launch; more rows than that loop
 
-template <typename T, int THREADS, int NV, bool VEC, bool LN, bool FP4>
+template <typename T, int THREADS, int NV, bool VEC, bool LN>
 hipError_t launch_q(const QuantizeArgs& p, hipStream_t stream) {
   constexpr int BLOCK = THREADS < 256 ? 256 : THREADS, RPB = BLOCK / THREADS;
   // With LN a group takes several rows for one read of the modulation; without,
   // rows of their own start sooner (32760 x 5120 bf16: 81 us against 91 with 16
   // groups a CU; with LN 137 and 150).
   const int64_t groups = (int64_t(p.M) + RPB - 1) / RPB, most = LN ? 16 * device_cu_count() : kMaxGroups;
-  return ECHO_LAUNCH(FP4 ? "quantize_rows_fp4" : "quantize_rows", (quantize_rows_k<T, THREADS, NV, VEC, LN, FP4>),
+  return ECHO_LAUNCH("quantize_rows", (quantize_rows_k<T, THREADS, NV, VEC, LN>),
                      dim3(static_cast<unsigned>(groups < most ? groups : most)), dim3(BLOCK), 0, stream, p);
 }
 
@@ -361,60 +276,42 @@ hipError_t launch_q(const QuantizeArgs& p, hipStream_t stream) {
 // threads 81 us, to a wave 99, to 512 threads 101; 13824 wide: 1024 threads 101,
 // 256 threads 108; with LN and its registers 7800 x 1536: 256 threads 17.6, a wave
 // 20.6.)
-template <typename T, bool VEC, bool LN, bool FP4>
+template <typename T, bool VEC, bool LN>
 hipError_t launch_q_width(const QuantizeArgs& p, hipStream_t stream) {
-  const int64_t w = FP4 ? (p.D + 511) / 512 * 512 : p.ldq;  // values to write, the padding included
-  if constexpr (!FP4)
-    if (w <= 16 * 8) return launch_q<T, 16, 1, VEC, LN, FP4>(p, stream);
-  if (w <= 64 * 8) return launch_q<T, 64, 1, VEC, LN, FP4>(p, stream);
+  const int64_t w = p.ldq;  // values to write, the padding included
+  if (w <= 16 * 8) return launch_q<T, 16, 1, VEC, LN>(p, stream);
+  if (w <= 64 * 8) return launch_q<T, 64, 1, VEC, LN>(p, stream);
   if (w <= 64 * 8 * 4) {
-    if constexpr (LN) return launch_q<T, 256, 1, VEC, LN, FP4>(p, stream);
-    return launch_q<T, 64, 4, VEC, LN, FP4>(p, stream);
+    if constexpr (LN) return launch_q<T, 256, 1, VEC, LN>(p, stream);
+    return launch_q<T, 64, 4, VEC, LN>(p, stream);
   }
-  if (w <= 256 * 8 * 3) return launch_q<T, 256, 3, VEC, LN, FP4>(p, stream);
-  if (w <= 1024 * 8 * 2) return launch_q<T, 1024, 2, VEC, LN, FP4>(p, stream);
-  return launch_q<T, 1024, 8, VEC, LN, FP4>(p, stream);  // 65536 values
+  if (w <= 256 * 8 * 3) return launch_q<T, 256, 3, VEC, LN>(p, stream);
+  if (w <= 1024 * 8 * 2) return launch_q<T, 1024, 2, VEC, LN>(p, stream);
+  return launch_q<T, 1024, 8, VEC, LN>(p, stream);  // 65536 values
 }
 
-template <typename T, bool FP4>
+template <typename T>
 hipError_t launch_q_type(const QuantizeArgs& p, hipStream_t stream) {
   const bool vec = p.D % 8 == 0 && p.ldx % Elem<T>::kPerVec == 0 && reinterpret_cast<uintptr_t>(p.x) % 16 == 0;
   if (p.shift != nullptr)
-    return vec ? launch_q_width<T, true, true, FP4>(p, stream) : launch_q_width<T, false, true, FP4>(p, stream);
-  return vec ? launch_q_width<T, true, false, FP4>(p, stream) : launch_q_width<T, false, false, FP4>(p, stream);
+    return vec ? launch_q_width<T, true, true>(p, stream) : launch_q_width<T, false, true>(p, stream);
+  return vec ? launch_q_width<T, true, false>(p, stream) : launch_q_width<T, false, false>(p, stream);
 }
 
 }  // namespace
 
 hipError_t launch_quantize_rows(int dtype_bf16, const QuantizeArgs& p, hipStream_t stream) {
-  return dtype_bf16 ? launch_q_type<bf16_t, false>(p, stream) : launch_q_type<float, false>(p, stream);
+  return dtype_bf16 ? launch_q_type<bf16_t>(p, stream) : launch_q_type<float>(p, stream);
 }
-hipError_t launch_quantize_rows_fp4(int dtype_bf16, const QuantizeArgs& p, hipStream_t stream) {
-  return dtype_bf16 ? launch_q_type<bf16_t, true>(p, stream) : launch_q_type<float, true>(p, stream);
-}
-
-namespace {
-template <typename F>
-hipError_t launch_back(const DequantizeArgs& p, int per16, F&& launch) {
-  const int64_t n = static_cast<int64_t>(p.M) * ((p.D + 7) / 8);
-  const dim3 grid(static_cast<unsigned>((n + 255) / 256 < kMaxGroups ? (n + 255) / 256 : kMaxGroups));
-  return launch(grid, p.D % 8 == 0 && p.ldy % per16 == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0);
-}
-}  // namespace
 
 hipError_t launch_dequantize_rows(int dtype_bf16, const DequantizeArgs& p, hipStream_t stream) {
-  return launch_back(p, dtype_bf16 ? 8 : 4, [&](dim3 grid, int vec) {
-    return dtype_bf16
-               ? ECHO_LAUNCH("dequantize_rows", dequantize_rows_k<bf16_t>, grid, dim3(256), 0, stream, p, vec)
-               : ECHO_LAUNCH("dequantize_rows", dequantize_rows_k<float>, grid, dim3(256), 0, stream, p, vec);
-  });
-}
-hipError_t launch_dequantize_rows_fp4(int dtype_bf16, const DequantizeArgs& p, hipStream_t stream) {
-  return launch_back(p, dtype_bf16 ? 8 : 4, [&](dim3 grid, int vec) {
-    return dtype_bf16
-               ? ECHO_LAUNCH("dequantize_rows_fp4", dequantize_rows_fp4_k<bf16_t>, grid, dim3(256), 0, stream, p, vec)
-               : ECHO_LAUNCH("dequantize_rows_fp4", dequantize_rows_fp4_k<float>, grid, dim3(256), 0, stream, p, vec);
-  });
+  const int64_t n = static_cast<int64_t>(p.M) * ((p.D + 7) / 8);
+  const dim3 grid(static_cast<unsigned>((n + 255) / 256 < kMaxGroups ? (n + 255) / 256 : kMaxGroups));
+  const int per = dtype_bf16 ? 8 : 4;
+  const int vec = p.D % 8 == 0 && p.ldy % per == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
+  return dtype_bf16
+             ? ECHO_LAUNCH("dequantize_rows", dequantize_rows_k<bf16_t>, grid, dim3(256), 0, stream, p, vec)
+             : ECHO_LAUNCH("dequantize_rows", dequantize_rows_k<float>, grid, dim3(256), 0, stream, p, vec);
 }
 
 }  // namespace echo

@@ -1,0 +1,351 @@
+// Rows held in 4 bits: microscaled floating point, every 32 values of a row with a
+// power of two of their own, for the products of gemm_fp4.hip.
+//
+//   e_b = max(floor(log2 max_{j in b} |a_ij|) - 2, -127),   c_ij = rn(a_ij / 2^e_b)
+//   a_ij = x[rows(i)]_j                 or LN(x[rows(i)])_j (1 + scale_j) + shift_j
+//
+// c of one sign, two exponent and one fraction bit (0, 0.5, 1, 1.5, 2, 3, 4, 6),
+// halves to the even code, magnitudes above 6 to 6; the scale is the byte e_b +
+// 127, 255 (NaN) for a block that is not finite.  The quotient is exact, so the
+// code is the value rounded once, by v_cvt_scalef32_pk_fp4_f32.  The instruction
+// takes its scale as an fp32 number, of which 2^-127 is a denormal one: such
+// blocks are multiplied by 2^64 first.
+//
+// A lane takes 8 values, four lanes a block, whose maximum is two DPP moves, and 16
+// lanes a set of 128 values: 64 bytes of codes and one word of scales.  Without
+// LayerNorm the sets of all rows are one list, which the lanes go through with four
+// of them in flight: bound by memory.  With it a row is a group of lanes that fits it
+// (gated_norm.hip), which holds the modulation for its rows.  A row's last set
+// writes the zeros up to the row's pitches.
+#include <type_traits>
+
+#include "common.h"
+#include "kernels.h"
+#include "launch.h"
+
+namespace echo {
+
+// The 4-bit codes of a lane's 8 values, packed, and the scales of the four blocks of
+// its set of 16 lanes as one word.  bad: the row is not there.
+__device__ __forceinline__ uint32_t codes8_fp4(const float* v, bool bad, uint32_t& scales) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+  top = max(top, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(top), 0xb1, 0xf, 0xf, false)));
+  top = max(top, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(top), 0x4e, 0xf, 0xf, false)));
+  bad = bad || top >= 0x7f800000u;
+  const uint32_t e = top >> 23, byte = e > 2 ? e - 2 : 0;
+  uint32_t w = 0;
+  if (byte > 0) {
+    const float s = __uint_as_float(byte << 23);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], s, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], s, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], s, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], s, 3);
+  } else {
+    constexpr float k = 0x1p64f, s = 0x1p-63f;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0] * k, v[1] * k, s, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2] * k, v[3] * k, s, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4] * k, v[5] * k, s, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6] * k, v[7] * k, s, 3);
+  }
+  scales = (bad ? 255u : byte) << (threadIdx.x / 4 % 4 * 8);
+  scales |= dpp_ror<4>(scales);
+  scales |= dpp_ror<8>(scales);
+  return bad ? 0u : w;
+}
+
+// Set `set` of a row: lane i of its 16 has the codes w and the scales' word.
+__device__ __forceinline__ void put_set(const QuantizeArgs& p, int64_t row, int set, uint32_t w, uint32_t scales) {
+  const int i = threadIdx.x % 16, sets = (p.D + 127) / 128;
+  int8_t* codes = p.codes + row * p.ldq + set * 64;
+  uint8_t* sc = p.scales + row * p.lds + set * 4;
+  *reinterpret_cast<uint32_t*>(codes + 4 * i) = w;
+  if (i == 0) *reinterpret_cast<uint32_t*>(sc) = scales;
+  if (set == sets - 1) {  // zeros up to whole 128 bytes of codes and whole 16 of scales
+    if (sets % 2 == 1) *reinterpret_cast<uint32_t*>(codes + 64 + 4 * i) = 0;
+    if (i > 0 && i <= 3 - (sets - 1) % 4) *reinterpret_cast<uint32_t*>(sc + 4 * i) = 0;
+  }
+}
+
+__device__ __forceinline__ int64_t row_of(const QuantizeArgs& p, int64_t row, bool& bad) {
+  bad = false;
+  if (p.rows == nullptr) return row;
+  const int32_t r = p.rows[row];
+  bad = r < 0 || r >= p.x_rows;  // no such row: as a row that is not finite
+  return bad ? 0 : r;
+}
+
+// The sets of all rows: those g, g + G, ... of the list for group g of G groups of 16
+// lanes (step_row and step_set: G in rows and sets of one).
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) quantize_fp4_k(QuantizeArgs p, int64_t step_row, int step_set) {
+  constexpr int U = 4;
+  const int sets = (p.D + 127) / 128, lane = threadIdx.x % 16;
+  const int64_t g = static_cast<int64_t>(blockIdx.x) * 16 + threadIdx.x / 16;
+  int64_t row = g / sets;
+  int set = static_cast<int>(g % sets);
+  while (row < p.M) {
+    int64_t rows[U];
+    int at[U];
+    bool bad[U];
+    Raw8<T> raw[VEC ? U : 1];
+    float v[VEC ? 1 : U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      rows[u] = row;
+      at[u] = set;
+      const int c = set * 128 + lane * 8;
+      const T* x = static_cast<const T*>(p.x);
+      bad[u] = false;
+      if (row < p.M) x += row_of(p, row, bad[u]) * p.ldx;
+      if constexpr (VEC) {
+        raw[u].load_nt(x + (c < p.D ? c : 0));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[u][j] = c + j < p.D ? Elem<T>::load(x, c + j) : 0.0f;
+      }
+      row += step_row;
+      set += step_set;
+      if (set >= sets) set -= sets, ++row;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (rows[u] >= p.M) break;
+      float f[8];
+      if constexpr (VEC) {
+        raw[u].unpack(f);
+        if (at[u] * 128 + lane * 8 >= p.D) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[j] = 0.0f;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = v[u][j];
+      }
+      uint32_t scales;
+      const uint32_t w = codes8_fp4(f, bad[u], scales);
+      put_set(p, rows[u], at[u], w, scales);
+    }
+  }
+}
+
+// With LayerNorm: a row to `threads` threads (16 if NARROW, one wave or the whole
+// workgroup), NV chunks of 8 values each; a workgroup takes consecutive rows, the next
+// row's values on their way and (HOLD) the modulation in registers.
+template <typename T, int MAXT, int NV, bool VEC, bool NARROW>
+__global__ void __launch_bounds__(MAXT) quantize_fp4_ln_k(QuantizeArgs p, int threads, int rows_per_wg) {
+  constexpr bool HOLD = NV <= 4, AHEAD = VEC && NV <= 4;
+  __shared__ float red[2][2][MAXT / kWave];
+  const int t = threadIdx.x % threads, D = p.D, rpb = blockDim.x / threads, waves = threads / kWave;
+  int turn = 0;
+  // as in gated_norm.hip: a piece of LDS for each reduction, two sets in turn
+  auto total = [&](float v, int slot) __attribute__((always_inline)) {
+    if constexpr (NARROW) return sum16(v);
+    v = wave_sum(v);
+    if (waves > 1) {
+      if (t % kWave == 0) red[turn][slot][t / kWave] = v;
+      __syncthreads();
+      const int w = t & 15;
+      v = sum16(w < waves ? red[turn][slot][w] : 0.0f);
+    }
+    return v;
+  };
+  // 1 + scale and shift of chunk u; 0 and 0 past the last column, so that the values
+  // there come out as zeros
+  auto modulation = [&](int u, float* sc, float* sh) __attribute__((always_inline)) {
+    const int c = (t + u * threads) * 8;
+    if (VEC) {
+      const int k = c < D ? c : 0;
+      unpack16(ldg16(p.scale + k), sc, static_cast<const float*>(nullptr));
+      unpack16(ldg16(p.scale + k + 4), sc + 4, static_cast<const float*>(nullptr));
+      unpack16(ldg16(p.shift + k), sh, static_cast<const float*>(nullptr));
+      unpack16(ldg16(p.shift + k + 4), sh + 4, static_cast<const float*>(nullptr));
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const bool in = VEC ? c < D : c + j < D;
+      if (!VEC) {
+        sc[j] = in ? p.scale[c + j] : 0.0f;
+        sh[j] = in ? p.shift[c + j] : 0.0f;
+      }
+      sc[j] = in ? 1.0f + sc[j] : 0.0f;
+      sh[j] = in ? sh[j] : 0.0f;
+    }
+  };
+  float sc[HOLD ? NV : 1][8], sh[HOLD ? NV : 1][8];
+  if constexpr (HOLD) {
+#pragma unroll
+    for (int u = 0; u < NV; ++u) modulation(u, sc[u], sh[u]);
+  }
+  Raw8<T> next[AHEAD ? NV : 1];
+  bool next_bad = false;
+  auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+    const T* x = static_cast<const T*>(p.x) + row_of(p, row, next_bad) * p.ldx;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int c = (t + u * threads) * 8;
+      next[AHEAD ? u : 0] = Raw8<T>{};
+      if (c < D) next[AHEAD ? u : 0].load_nt(x + c);
+    }
+  };
+  const int64_t base = static_cast<int64_t>(blockIdx.x) * rows_per_wg;
+  const int64_t end = base + rows_per_wg < p.M ? base + rows_per_wg : p.M;
+  int64_t row = base + threadIdx.x / threads;
+  if constexpr (AHEAD)
+    if (row < end) fetch(row);
+  // (a group that reaches a barrier is the whole workgroup, so the loop is uniform for its waves)
+  for (; row < end; row += rpb) {
+    bool bad = next_bad;
+    float v[NV][8];
+    const T* x = nullptr;
+    if constexpr (!AHEAD) x = static_cast<const T*>(p.x) + row_of(p, row, bad) * p.ldx;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int c = (t + u * threads) * 8;
+      if constexpr (AHEAD) {
+        next[u].unpack(v[u]);
+      } else if constexpr (VEC) {
+        Raw8<T> raw{};
+        if (c < D) raw.load_nt(x + c);
+        raw.unpack(v[u]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[u][j] = c + j < D ? Elem<T>::load(x, c + j) : 0.0f;
+      }
+    }
+    if constexpr (AHEAD)
+      if (row + rpb < end) fetch(row + rpb);
+    float sum = 0.0f, sq = 0.0f;
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += v[u][j];
+    const float mean = total(sum, 0) / static_cast<float>(D);
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int c = (t + u * threads) * 8;
+      const float m = c < D ? mean : 0.0f;  // (what lies past the last column stays zero)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[u][j] -= VEC || c + j < D ? m : 0.0f;
+        sq = fmaf(v[u][j], v[u][j], sq);
+      }
+    }
+    const float rstd = 1.0f / sqrtf(total(sq, 1) / static_cast<float>(D) + p.ln_eps);
+    turn ^= 1;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+      const int set = (t + u * threads) / 16;
+      if (set * 128 >= D) continue;  // (for 16 lanes together)
+      float c8[8], h8[8];
+      if constexpr (!HOLD) modulation(u, c8, h8);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        v[u][j] = fmaf(v[u][j] * rstd, HOLD ? sc[HOLD ? u : 0][j] : c8[j], HOLD ? sh[HOLD ? u : 0][j] : h8[j]);
+      uint32_t scales;
+      const uint32_t w = codes8_fp4(v[u], bad, scales);
+      put_set(p, row, set, w, scales);
+    }
+  }
+}
+
+// y_ij = cast(2^e_b c_ij), exact in both types; a thread takes 8 values
+template <typename T>
+__global__ void __launch_bounds__(256) dequantize_fp4_k(DequantizeArgs p, int vec) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  const int nch = (p.D + 7) / 8;
+  for (int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; e < static_cast<int64_t>(p.M) * nch;
+       e += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t row = e / nch;
+    const int c = static_cast<int>(e % nch) * 8;
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(p.codes + row * p.ldq + c / 2);
+    const uint32_t b = p.scales[row * p.lds + c / 32];
+    // 2^-127 is a denormal number, 255 a NaN
+    const float s = __uint_as_float(b == 255u ? 0x7fc00000u : b == 0u ? 0x00400000u : b << 23);
+    const f32x2 u0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 0);
+    const f32x2 u1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 1);
+    const f32x2 u2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2);
+    const f32x2 u3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
+    const float v[8] = {s * u0[0], s * u0[1], s * u1[0], s * u1[1], s * u2[0], s * u2[1], s * u3[0], s * u3[1]};
+    T* y = static_cast<T*>(p.y) + row * p.ldy + c;
+    if (vec) {
+      constexpr int PV = Elem<T>::kPerVec;
+#pragma unroll
+      for (int h = 0; h < 8 / PV; ++h) stg16_nt(y + h * PV, pack16(v + h * PV, static_cast<const T*>(nullptr)));
+    } else {
+      for (int j = 0; j < 8 && c + j < p.D; ++j) Elem<T>::store(y, j, v[j]);
+    }
+  }
+}
+
+namespace {
+
+constexpr int64_t kMaxGroups = 1 << 20;  // workgroups of a launch; more rows than that loop
+
+template <typename T, bool VEC>
+hipError_t launch_plain(const QuantizeArgs& p, hipStream_t stream) {
+  const int sets = (p.D + 127) / 128;
+  const int64_t n = (static_cast<int64_t>(p.M) * sets + 63) / 64;  // four sets to 16 lanes
+  const int64_t wgs = n < kMaxGroups ? n : kMaxGroups;
+  return ECHO_LAUNCH("quantize_rows_fp4", (quantize_fp4_k<T, VEC>), dim3(static_cast<unsigned>(wgs)), dim3(256), 0,
+                     stream, p, wgs * 16 / sets, static_cast<int>(wgs * 16 % sets));
+}
+
+template <typename T, int MAXT, int NV, bool VEC, bool NARROW = false>
+hipError_t launch_ln(const QuantizeArgs& p, int threads, hipStream_t stream) {
+  const int block = threads <= kWave ? 256 : threads, rpb = block / threads;
+  // consecutive rows of a workgroup share one read of the modulation
+  const int64_t want = static_cast<int64_t>(device_cu_count()) * 4096 / block;
+  int64_t per = (p.M + want - 1) / want;
+  per = (per + rpb - 1) / rpb * rpb;
+  return ECHO_LAUNCH("quantize_rows_fp4", (quantize_fp4_ln_k<T, MAXT, NV, VEC, NARROW>),
+                     dim3(static_cast<unsigned>((p.M + per - 1) / per)), dim3(block), 0, stream, p, threads,
+                     static_cast<int>(per));
+}
+
+// What a reduction costs a wave is shared by its chunks, what it waits for by the
+// workgroups of a CU: up to 512 columns 16 lanes with up to four chunks a row, up to
+// 1024 a wave, then up to 256 threads with up to three chunks and no more threads than
+// that takes (32760 x 5120: three chunks to 256 threads 102 us, two to 320 142; 100000 x
+// 1024: two to a wave 60, one to 128 threads 73; 16000 x 8192: two to 512 threads 96, four
+// to 256 102).
+template <typename T, bool VEC>
+hipError_t launch_ln_width(const QuantizeArgs& p, hipStream_t stream) {
+  auto threads = [&](int chunks) { return (p.D + 8 * chunks * kWave - 1) / (8 * chunks * kWave) * kWave; };
+  if (p.D <= 128) return launch_ln<T, 256, 1, VEC, true>(p, 16, stream);
+  if (p.D <= 256) return launch_ln<T, 256, 2, VEC, true>(p, 16, stream);
+  if (p.D <= 512) return launch_ln<T, 256, 4, VEC, true>(p, 16, stream);
+  if (p.D <= 1024) return launch_ln<T, 256, 2, VEC>(p, kWave, stream);
+  if (p.D <= 2048) return launch_ln<T, 256, 1, VEC>(p, threads(1), stream);
+  if (p.D <= 4096) return launch_ln<T, 256, 2, VEC>(p, threads(2), stream);
+  if (p.D <= 6144) return launch_ln<T, 256, 3, VEC>(p, threads(3), stream);
+  if (p.D <= 8192) return launch_ln<T, 512, 2, VEC>(p, threads(2), stream);
+  if (p.D <= 16384) return launch_ln<T, 1024, 2, VEC>(p, threads(2), stream);
+  return launch_ln<T, 1024, 8, VEC>(p, threads(8), stream);  // 65536 values
+}
+
+template <typename T>
+hipError_t launch_type(const QuantizeArgs& p, hipStream_t stream) {
+  const bool vec = p.D % 8 == 0 && p.ldx % Elem<T>::kPerVec == 0 && reinterpret_cast<uintptr_t>(p.x) % 16 == 0;
+  if (p.shift != nullptr) return vec ? launch_ln_width<T, true>(p, stream) : launch_ln_width<T, false>(p, stream);
+  return vec ? launch_plain<T, true>(p, stream) : launch_plain<T, false>(p, stream);
+}
+
+}  // namespace
+
+hipError_t launch_quantize_rows_fp4(int dtype_bf16, const QuantizeArgs& p, hipStream_t stream) {
+  return dtype_bf16 ? launch_type<bf16_t>(p, stream) : launch_type<float>(p, stream);
+}
+
+hipError_t launch_dequantize_rows_fp4(int dtype_bf16, const DequantizeArgs& p, hipStream_t stream) {
+  const int64_t n = (static_cast<int64_t>(p.M) * ((p.D + 7) / 8) + 255) / 256;
+  const dim3 grid(static_cast<unsigned>(n < kMaxGroups ? n : kMaxGroups));
+  const int per = dtype_bf16 ? 8 : 4;
+  const int vec = p.D % 8 == 0 && p.ldy % per == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
+  return dtype_bf16
+             ? ECHO_LAUNCH("dequantize_rows_fp4", dequantize_fp4_k<bf16_t>, grid, dim3(256), 0, stream, p, vec)
+             : ECHO_LAUNCH("dequantize_rows_fp4", dequantize_fp4_k<float>, grid, dim3(256), 0, stream, p, vec);
+}
+
+}  // namespace echo

@@ -155,7 +155,8 @@ def test_quantize_picks_rows(D):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("M,D", [(1, 8), (5, 64), (4, 250), (3, 1536), (7, 5120), (2, 13824), (2, 20001)])
+@pytest.mark.parametrize("M,D", [(1, 8), (5, 64), (70, 128), (4, 250), (33, 512), (9, 700), (5, 1024), (3, 1536), (4, 3000), (7, 5120), (3, 8192),
+                                 (2, 13824), (2, 20001)])
 def test_quantize_layernorm(M, D, dtype):
     """LayerNorm in fp32 in front: sums of at most 80 terms a lane and 10 joining
     steps, so a value is within 256 steps of 2^-24 of the row's largest; its code is
@@ -244,7 +245,8 @@ def check_linear(got, a, w, bias, out_dtype, act=None, gate=None, res=None, what
 SIZES = [(1, 1, 1), (1, 16, 64), (1, 300, 5120), (2, 77, 129), (4, 33, 2049), (5, 1000, 700), (8, 64, 4100), (9, 40, 300),
          (16, 64, 128), (17, 129, 640), (32, 48, 256), (33, 100, 100), (48, 1000, 2600), (64, 512, 1024), (65, 65, 65),
          (100, 200, 300), (128, 128, 128), (130, 70, 13824), (257, 255, 200), (300, 512, 256), (500, 1030, 384),
-         (1000, 96, 4000), (1111, 2049, 130), (2100, 2304, 768), (4100, 4100, 128), (70, 300, 40000)]
+         (1000, 96, 4000), (1111, 2049, 130), (2100, 2304, 768), (4100, 4100, 128), (70, 300, 40000), (4200, 4400, 1100),
+         (3000, 6400, 1500), (5000, 5128, 300)]
 
 
 @pytest.mark.parametrize("out_dtype", [torch.bfloat16, torch.float32])
@@ -260,7 +262,8 @@ def test_linear_sizes(M, N, K, out_dtype):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 200, 300), (6, 60, 1500), (12, 96, 520), (20, 77, 130), (60, 64, 512),
-                                   (140, 260, 260), (700, 1000, 200), (4096, 4100, 128), (90, 256, 8000)])
+                                   (140, 260, 260), (700, 1000, 200), (4096, 4100, 128), (90, 256, 8000), (4200, 4400, 1100),
+                                   (5000, 5128, 300), (2600, 7000, 900)])
 @pytest.mark.parametrize("epi", ["none", "gelu", "gate_bf16", "gate_f32_rows"])
 def test_linear_epilogues(M, N, K, epi):
     g = _gen(M + N + K)
