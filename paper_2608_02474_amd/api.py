@@ -372,13 +372,14 @@ class BlockStack:
     by the saliency with unit frame weights; n_anchors is the number of
     anchor segments it marks (the k given to `anchors`).  codec:
     "residual_int8" (the default), "full" (the outputs in the activation
-    dtype) or "naive_int8"."""
+    dtype) or "naive_int8".  rotary: positions of every block's queries and keys, for
+    weights in 8 or 4 bits (block_partial)."""
 
     CODECS = {"residual_int8": 0, "full": 1, "naive_int8": 2}
 
     def __init__(self, params: list, H: int, L: int, D: int, device, dtype, scheduler: Scheduler,
                  xi: float = 1e-6, ln_eps: float = 1e-6, anchor_mask: torch.Tensor | None = None,
-                 n_anchors: int | None = None, codec: str = "residual_int8"):
+                 n_anchors: int | None = None, codec: str = "residual_int8", rotary: "Rotary | None" = None):
         if scheduler.cfg.n_full < 1:
             raise ValueError("the first step must be a full step (n_full >= 1)")
         if (anchor_mask is None) != (n_anchors is None):
@@ -398,7 +399,8 @@ class BlockStack:
         self.y_sel = torch.empty((L, D), dtype=torch.float32, **kw)
         self.all_idx = torch.arange(L, dtype=torch.int32, **kw)
         self.all_mask = torch.ones(L, dtype=torch.uint8, **kw)
-        self._w = [None if is_int8_block(p) else block_weights(p) for p in params]
+        self.rotary = rotary
+        self._w = [None if is_int8_block(p) or is_fp4_block(p) else block_weights(p) for p in params]
         self.ws, self.sel_ws, self.sel = Workspace(), Workspace(), None
         self._unit = None
         self.history = []   # (k, full, delta_t) per step; k per segment in the two-stage form
@@ -425,7 +427,7 @@ class BlockStack:
         x = x0
         for b, p in enumerate(self.params):
             ys = block_partial(p, x, idx, n, self.H, self.ln_eps, y_sel=self.y_sel,
-                               workspace=self.ws, _weights=self._w[b])
+                               workspace=self.ws, _weights=self._w[b], rotary=self.rotary)
             x = cache_update_codec(self.codec, x, idx, mask, n, ys, self.xref[b], self.y[b],
                                    store=self.store[b], codes=self.codes[b], scale=self.scale[b])
         self.history.append((k, full, delta_t))
@@ -467,15 +469,21 @@ def block_weights(params: dict) -> BlockWeights:
 def block_partial(params: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int, H: int,
                   ln_eps: float = 1e-6, y_sel: torch.Tensor | None = None,
                   workspace: Workspace | None = None, _weights: BlockWeights | None = None,
-                  batch_invariant: bool = False):
+                  batch_invariant: bool = False, rotary: "Rotary | None" = None):
     """y_sel [n_sel, D] fp32 = block output of tokens idx[:n_sel].  With
     batch_invariant, each row is bit-identical for any selection containing it.
-    With weights in 8 bits (quantize_block) the block runs on 8-bit rows; without a
-    workspace its intermediate tensors are then the call's own."""
-    if is_int8_block(params):
+    With weights in 8 or 4 bits (quantize_block) the block runs on such rows; without a
+    workspace its intermediate tensors are then the call's own.  Such a block may turn
+    its queries and keys by their tokens' positions (rotary; a token's position is its
+    number, or its place in rotary's grid), and have root-mean-square norms after its
+    sub-layers: params' after1 and after2 (fp32 [D], either or both), the weights of the
+    norms of the attention's and of the FFN's output, in front of gate and residual."""
+    if is_int8_block(params) or is_fp4_block(params):
         if batch_invariant:
-            raise ValueError("batch_invariant does not go with weights in 8 bits")
-        return _block_partial_int8(params, x, idx, n_sel, H, ln_eps, y_sel, workspace)
+            raise ValueError("batch_invariant does not go with weights in 8 bits or 4")
+        return _block_partial_rows(params, x, idx, n_sel, H, ln_eps, y_sel, workspace, rotary)
+    if rotary is not None or "after1" in params or "after2" in params:
+        raise ValueError("rotary and norms after the sub-layers go with weights in 8 or 4 bits")
     lib = _lib_handle()
     _dev(x, "x")
     _dev(idx, "idx", torch.int32)
@@ -506,44 +514,63 @@ def block_partial(params: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int, 
 MATRIX_NAMES = ("wq", "wk", "wv", "wo", "w1", "w2")
 
 
-def quantize_block(params: dict) -> dict:
+def quantize_block(params: dict, bits: int = 8) -> dict:
     """The block's parameters with its six weight matrices in 8 bits, a scale for
-    each output channel (Int8Rows); biases and modulation as they are.
-    block_partial, CachedBlock and BlockStack take them in place of params."""
-    return {**params, **{n: quantize_rows(params[n]) for n in MATRIX_NAMES}}
+    each output channel (Int8Rows), or in 4, one for every 32 inputs of a channel
+    (Fp4Rows); biases and modulation as they are.  block_partial, CachedBlock and
+    BlockStack take them in place of params."""
+    if bits not in (4, 8):
+        raise ValueError("bits must be 8 or 4")
+    quantize = quantize_rows if bits == 8 else quantize_rows_fp4
+    return {**params, **{n: quantize(params[n]) for n in MATRIX_NAMES}}
 
 
 def is_int8_block(params: dict) -> bool:
     return isinstance(params["wq"], Int8Rows)
 
 
-def _int8_block_pieces(L: int, n: int, D: int, F: int, H: int, dt) -> tuple:
-    """(shape, dtype) of what _block_partial_int8 holds between its calls, and of
+def is_fp4_block(params: dict) -> bool:
+    return isinstance(params["wq"], Fp4Rows)
+
+
+def _rows_block_pieces(fp4: bool, L: int, n: int, D: int, F: int, H: int, dt, normed: bool) -> tuple:
+    """(shape, dtype) of what _block_partial_rows holds between its calls, and of
     their scratch: products' partial sums and ranges of the attention (the sizes
     asked for here fix both; a call that needed more would take its own)."""
-    lib, f32, i8 = _lib_handle(), torch.float32, torch.int8
-    pd, pf = (D + 127) // 128 * 128, (F + 127) // 128 * 128
+    lib, f32, u8 = _lib_handle(), torch.float32, torch.uint8
     scratch = 256
     for M, N, K in ((n, D, D), (L, D, D), (n, F, D), (n, D, F)):
-        cfg = LinearInt8Cfg(M, N, K, _lib.ECHO_LINEAR_NONE, ECHO_F32, ECHO_F32, ECHO_F32, 0, pd if K == D else pf,
-                            pd if K == D else pf, N, 0)
-        scratch = max(scratch, lib.echo_linear_int8_workspace(ctypes.byref(cfg)))
+        if fp4:
+            p, q = (K + 255) // 256 * 128, (K + 511) // 512 * 16
+            cfg = PACK_LINEAR_FP4(M, N, K, _lib.ECHO_LINEAR_NONE, ECHO_F32, ECHO_F32, ECHO_F32, 0, p, q, p, q, N, 0)
+            scratch = max(scratch, lib.echo_linear_fp4_workspace(cfg))
+        else:
+            p = (K + 127) // 128 * 128
+            cfg = LinearInt8Cfg(M, N, K, _lib.ECHO_LINEAR_NONE, ECHO_F32, ECHO_F32, ECHO_F32, 0, p, p, N, 0)
+            scratch = max(scratch, lib.echo_linear_int8_workspace(ctypes.byref(cfg)))
     qs, ks = (n * D, D, D // H), (L * D, D, D // H)
     cfg = CrossAttentionCfg(1, n, L, H, H, D // H, _DTYPES[dt], (D // H) ** -0.5, qs, ks, ks, qs)
     scratch = max(scratch, lib.echo_cross_attention_workspace(ctypes.byref(cfg), 0))
-    return (((L, pd), i8), ((L,), f32), ((n, pd), i8), ((n,), f32), ((n, pf), i8), ((n,), f32),
-            ((n, D), dt), ((L, D), dt), ((L, D), dt), ((1, n, H, D // H), dt), ((n, D), f32), ((n, F), dt),
-            ((scratch,), torch.uint8))
+
+    def rows(m, k):
+        if fp4:
+            return ((m, (k + 255) // 256 * 128), u8), ((m, (k + 511) // 512 * 16), u8)
+        return ((m, (k + 127) // 128 * 128), torch.int8), ((m,), f32)
+    between = (((n, D), dt), ((n, D), dt)) if normed else ()
+    return (*rows(L, D), *rows(n, D), *rows(n, F), ((n, D), dt), ((L, D), dt), ((L, D), dt), ((1, n, H, D // H), dt),
+            ((n, D), f32), ((n, F), dt), ((scratch,), u8), *between)
 
 
-def _block_partial_int8(p: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int, H: int, ln_eps: float,
-                        y_sel: torch.Tensor | None, workspace: Workspace | None) -> torch.Tensor:
-    """block_partial on 8-bit rows: the tokens are quantized in front of every
-    product, one scale a token; attention, residuals and LayerNorms as there.
-    What it holds in between lies in the workspace, or else is allocated by the
-    calls themselves."""
+def _block_partial_rows(p: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int, H: int, ln_eps: float,
+                        y_sel: torch.Tensor | None, workspace: Workspace | None, rot: "Rotary | None") -> torch.Tensor:
+    """block_partial on 8-bit or 4-bit rows: the tokens are quantized in front of every
+    product; attention, residuals and LayerNorms as there.  What it holds in between
+    lies in the workspace, or else is allocated by the calls themselves."""
     if n_sel < 0 or H < 1:
         check("echo_block_partial", _lib.ECHO_EINVAL)
+    fp4 = is_fp4_block(p)
+    Rows, quantize, linear = ((Fp4Rows, quantize_rows_fp4, linear_fp4) if fp4 else
+                              (Int8Rows, quantize_rows, linear_int8))
     _dev(x, "x")
     L, D = x.shape
     _dev(p["mod"], "mod", torch.float32)
@@ -554,12 +581,18 @@ def _block_partial_int8(p: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int,
     for n in ("bq", "bk", "bv", "bo", "b1", "b2"):
         _dev(p[n], n, x.dtype)
     for n in MATRIX_NAMES:
-        if not isinstance(p[n], Int8Rows):
-            raise TypeError(f"{n} must be Int8Rows as wq is (see quantize_block)")
+        if not isinstance(p[n], Rows):
+            raise TypeError(f"{n} must be {Rows.__name__} as wq is (see quantize_block)")
     F = len(p["w1"])
     for n, shape in zip(MATRIX_NAMES, ((D, D), (D, D), (D, D), (D, D), (F, D), (D, F))):
         if (len(p[n]), p[n].cols) != shape:
             raise ValueError(f"{n} must be {list(shape)}")
+    after1, after2 = p.get("after1"), p.get("after2")
+    for t, n in ((after1, "after1"), (after2, "after2")):
+        if t is not None:
+            _vector(t, n, D, torch.float32)
+    if rot is not None and (not isinstance(rot, Rotary) or 2 * rot.freq.numel() > D // H):
+        raise ValueError(f"rotary must be a Rotary of at most {D // H // 2} pairs")
     if y_sel is None:
         y_sel = torch.empty((max(n_sel, 1), D), dtype=torch.float32, device=x.device)
     else:
@@ -573,27 +606,42 @@ def _block_partial_int8(p: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int,
         raise ValueError(f"idx must hold {n_sel} tokens")
     rows = idx[:n_sel]
     mod, dt, dh = p["mod"], x.dtype, D // H
-    a8 = s8 = h8 = q = k = v = o = x1 = h = scratch = None
+    a8 = s8 = h8 = q = k = v = o = x1 = h = z = c = scratch = None
     if workspace is not None:
         _echo_dtype(x)
-        ac, asc, sc, ssc, hc, hsc, q, k, v, o, x1, h, part = workspace.pieces(
-            ("int8 block", L, n_sel, D, F, H, dt), lambda: _int8_block_pieces(L, n_sel, D, F, H, dt), x.device)
+        normed = after1 is not None or after2 is not None
+        ac, asc, sc, ssc, hc, hsc, q, k, v, o, x1, h, part, *between = workspace.pieces(
+            ("rows block", fp4, L, n_sel, D, F, H, dt, normed),
+            lambda: _rows_block_pieces(fp4, L, n_sel, D, F, H, dt, normed), x.device)
         # (the selected rows' codes: of the input, then of the attention's output, then of x1)
-        a8, s8, h8 = Int8Rows(ac, asc, D), Int8Rows(sc, ssc, D), Int8Rows(hc, hsc, F)
+        a8, s8, h8 = Rows(ac, asc, D), Rows(sc, ssc, D), Rows(hc, hsc, F)
+        if normed:
+            z, c = between
         scratch = Workspace()
         scratch.buf = part
-    a = quantize_rows(x, shift=mod[0], scale=mod[1], ln_eps=ln_eps, out=a8)
-    a_sel = quantize_rows(x, rows=rows, shift=mod[0], scale=mod[1], ln_eps=ln_eps, out=s8)
-    q = linear_int8(a_sel, p["wq"], p["bq"], dtype=dt, out=q, workspace=scratch).view(1, n_sel, H, dh)
-    k = linear_int8(a, p["wk"], p["bk"], dtype=dt, out=k, workspace=scratch).view(1, L, H, dh)
-    v = linear_int8(a, p["wv"], p["bv"], dtype=dt, out=v, workspace=scratch).view(1, L, H, dh)
+    a = quantize(x, shift=mod[0], scale=mod[1], ln_eps=ln_eps, out=a8)
+    a_sel = quantize(x, rows=rows, shift=mod[0], scale=mod[1], ln_eps=ln_eps, out=s8)
+    q = linear(a_sel, p["wq"], p["bq"], dtype=dt, out=q, workspace=scratch).view(1, n_sel, H, dh)
+    k = linear(a, p["wk"], p["bk"], dtype=dt, out=k, workspace=scratch).view(1, L, H, dh)
+    v = linear(a, p["wv"], p["bv"], dtype=dt, out=v, workspace=scratch).view(1, L, H, dh)
+    if rot is not None:
+        rotary(q, rot, positions=rows, out=q)
+        rotary(k, rot, out=k)
     o = cross_attention(q, k, v, out=o, workspace=scratch).view(n_sel, D)
-    x1 = linear_int8(quantize_rows(o, out=s8), p["wo"], p["bo"], gate=mod[2], residual=x, residual_rows=rows,
-                     dtype=torch.float32, out=x1, workspace=scratch)
-    b = quantize_rows(x1, shift=mod[3], scale=mod[4], ln_eps=ln_eps, out=s8)
-    h = linear_int8(b, p["w1"], p["b1"], activation="gelu", dtype=dt, out=h, workspace=scratch)
-    return linear_int8(quantize_rows(h, out=h8), p["w2"], p["b2"], gate=mod[5], residual=x1, out=y,
-                       workspace=scratch)
+    if after1 is None:
+        x1 = linear(quantize(o, out=s8), p["wo"], p["bo"], gate=mod[2], residual=x, residual_rows=rows,
+                    dtype=torch.float32, out=x1, workspace=scratch)
+        b = quantize(x1, shift=mod[3], scale=mod[4], ln_eps=ln_eps, out=s8)
+    else:
+        z = linear(quantize(o, out=s8), p["wo"], p["bo"], dtype=dt, out=z, workspace=scratch)
+        x1, c = gated_norm(z, x, after="rms", after_weight=after1, gate=mod[2], residual_rows=rows, before="layer",
+                           scale=mod[4], shift=mod[3], eps=ln_eps, y=x1, h=c, y_dtype=torch.float32)
+        b = quantize(c, out=s8)
+    h = linear(b, p["w1"], p["b1"], activation="gelu", dtype=dt, out=h, workspace=scratch)
+    if after2 is None:
+        return linear(quantize(h, out=h8), p["w2"], p["b2"], gate=mod[5], residual=x1, out=y, workspace=scratch)
+    z = linear(quantize(h, out=h8), p["w2"], p["b2"], dtype=dt, out=z, workspace=scratch)
+    return gated_norm(z, x1, after="rms", after_weight=after2, gate=mod[5], before=None, eps=ln_eps, y=y)[0]
 
 
 # ----------------------------------------------------------- Wan-style block
@@ -607,8 +655,8 @@ def wan_block_partial(params: dict, x: torch.Tensor, ctx: torch.Tensor, idx: tor
     ints); grid (T, gh, gw).  Returns y_sel [sum(n_sel), D] fp32 in idx order.
     params: the block weights plus wqc, wkc, wvc, woc, bqc, bkc, bvc, boc (in
     x's dtype) and gq, gk, gqc, gkc, g3, b3 (fp32 [D])."""
-    if is_int8_block(params):
-        raise ValueError("the Wan-style block takes no weights in 8 bits")
+    if is_int8_block(params) or is_fp4_block(params):
+        raise ValueError("the Wan-style block takes no weights in 8 bits or 4")
     lib = _lib_handle()
     _dev(x, "x")
     _dev(ctx, "ctx", x.dtype)
@@ -1419,11 +1467,12 @@ class CachedBlock:
 
     init(x)                 recompute every token and fill the cache (first step)
     step(x, w, ratio|k)     saliency -> top-K -> partial block -> cache update
-    Returns the block output y [L, D] in the activation dtype.
+    Returns the block output y [L, D] in the activation dtype.  rotary: positions of
+    queries and keys, for weights in 8 or 4 bits (block_partial).
     """
 
     def __init__(self, params: dict, H: int, L: int, D: int, device, dtype,
-                 ln_eps: float = 1e-6, xi: float = 1e-6):
+                 ln_eps: float = 1e-6, xi: float = 1e-6, rotary: "Rotary | None" = None):
         self.params = params
         self.H, self.L, self.D = H, L, D
         self.ln_eps, self.xi = ln_eps, xi
@@ -1437,11 +1486,13 @@ class CachedBlock:
         self.ws = Workspace()
         self.sel_ws = Workspace()
         self.sel = None
-        self._w = None if is_int8_block(params) else block_weights(params)
+        self.rotary = rotary
+        self._w = None if is_int8_block(params) or is_fp4_block(params) else block_weights(params)
 
     def init(self, x: torch.Tensor) -> torch.Tensor:
         ys = block_partial(self.params, x, self.all_idx, self.L, self.H, self.ln_eps,
-                           y_sel=self.y_sel, workspace=self.ws, _weights=self._w)
+                           y_sel=self.y_sel, workspace=self.ws, _weights=self._w,
+                           rotary=self.rotary)
         return cache_update(x, self.all_idx, self.all_mask, self.L, ys, self.xref, self.codes,
                             self.scale, self.y)
 
@@ -1452,6 +1503,7 @@ class CachedBlock:
         self.sel = select(x, self.xref, frame_weight, N, k=k, xi=self.xi, out=self.sel,
                           workspace=self.sel_ws)
         ys = block_partial(self.params, x, self.sel.idx, k, self.H, self.ln_eps,
-                           y_sel=self.y_sel, workspace=self.ws, _weights=self._w)
+                           y_sel=self.y_sel, workspace=self.ws, _weights=self._w,
+                           rotary=self.rotary)
         return cache_update(x, self.sel.idx, self.sel.mask, k, ys, self.xref, self.codes,
                             self.scale, self.y)

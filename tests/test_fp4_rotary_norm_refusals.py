@@ -234,3 +234,36 @@ def test_binding_rejects_host_tensors_shapes_and_types():
                dict(residual=f(5, 64)), dict(residual=f(6, 63))):
         with pytest.raises((ValueError, TypeError)):
             api.gated_norm(z, kw.pop("residual", f(6, 64)), **kw)
+
+
+def test_block_on_4_bit_rows_refuses_before_any_launch():
+    """Codes of the other kind among the matrices, norms of another shape, positions of
+    more channels than a head has; what goes with such rows alone, and what does not."""
+    D, F, L = 256, 512, 6
+    u8 = torch.uint8
+    w = lambda n, k: api.Fp4Rows(on(n, (k + 255) // 256 * 128, dtype=u8), on(n, (k + 511) // 512 * 16, dtype=u8), k)  # noqa: E731
+    w8 = api.Int8Rows(on(D, D, dtype=torch.int8), on(D, dtype=torch.float32), D)
+    p = {"wq": w(D, D), "wk": w(D, D), "wv": w(D, D), "wo": w(D, D), "w1": w(F, D), "w2": w(D, F),
+         "bq": on(D), "bk": on(D), "bv": on(D), "bo": on(D), "b1": on(F), "b2": on(D), "mod": on(6, D, dtype=torch.float32)}
+    x, idx, y = on(L, D), on(L, dtype=torch.int32), on(L, D, dtype=torch.float32)
+    f = lambda *s: on(*s, dtype=torch.float32)  # noqa: E731
+    assert api.is_fp4_block(p) and not api.is_int8_block(p)
+    for kw in (dict(y_sel=on(L, D)), dict(y_sel=y[:3]), dict(idx=idx[:3]), dict(wk=w8), dict(wk=on(D, D)), dict(w1=w(F, F)), dict(w2=w(D, D)),
+               dict(after1=f(D - 1)), dict(after2=f(1, D)), dict(after2=on(D)), dict(mod=f(5, D)),
+               dict(rotary=api.Rotary(on(D, dtype=torch.float64))), dict(rotary=1.0)):
+        q = {**p, **{n: t for n, t in kw.items() if n in p or n.startswith("after")}}
+        with pytest.raises((ValueError, TypeError), match=next(iter(kw))):
+            api.block_partial(q, x, kw.get("idx", idx), 4, 2, y_sel=kw.get("y_sel", y), rotary=kw.get("rotary"))
+    with pytest.raises(ValueError, match="batch_invariant"):
+        api.block_partial(p, x, idx, 4, 2, batch_invariant=True)
+    with pytest.raises(ValueError, match="4"):
+        api.wan_block_partial(p, None, None, None, [0], 1, (1, 1, 1))
+    for n_sel, H in ((-1, 2), (2, 0)):
+        with pytest.raises(RuntimeError, match="echo_block_partial"):
+            api.block_partial(p, x, idx, n_sel, H)
+    with pytest.raises(ValueError, match="bits"):
+        api.quantize_block({}, bits=2)
+    bf = {n: on(2, 2) for n in p}
+    for kw in (dict(rotary=api.Rotary(on(1, dtype=torch.float64))), dict()):
+        with pytest.raises(ValueError, match="8 or 4 bits"):
+            api.block_partial(bf if kw else {**bf, "after1": f(2)}, x, idx, 4, 2, **kw)

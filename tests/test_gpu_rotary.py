@@ -115,6 +115,22 @@ def test_grid(grid, pairs, dh, layout, dtype):
     check(y.cpu(), x, angle, layout, 1.0, "in order")
 
 
+@pytest.mark.parametrize("grid", [(21, 30, 52), (5, 3, 4)])
+def test_as_the_wan_style_block_turns(grid):
+    """The positions of the Wan-style block, by its own oracle."""
+    from oracle import wan_block as OW
+    H, dh = 3, 128
+    n = grid[0] * grid[1] * grid[2]
+    g = _gen(7)
+    rows = torch.randint(0, n, (60,), generator=g, dtype=torch.int32)
+    x = torch.randn(1, 60, H, dh, generator=g)
+    rot = api.Rotary.make(dh, device(), grid=grid[1:])
+    got, _ = api.rotary(x.to(device()), rot, positions=rows.to(device()))
+    want = torch.from_numpy(OW.apply_rope(x[0].reshape(60, H * dh).double().numpy(), rows.numpy(), grid, H)).view(60, H, dh)
+    err = 12 * U32 * x[0].abs().reshape(60, H, dh // 2, 2).sum(-1, keepdim=True).expand(-1, -1, -1, 2).reshape(60, H, dh)
+    assert ((got.cpu().double()[0] - want).abs() <= err.double() + 1e-30).all()
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("dims", [128, 64, 36])
 def test_in_place_strides_and_surroundings(dims, dtype):
