@@ -542,8 +542,9 @@ def _rows_block_pieces(fp4: bool, L: int, n: int, D: int, F: int, H: int, dt, no
     for M, N, K in ((n, D, D), (L, D, D), (n, F, D), (n, D, F)):
         if fp4:
             p, q = (K + 255) // 256 * 128, (K + 511) // 512 * 16
-            cfg = PACK_LINEAR_FP4(M, N, K, _lib.ECHO_LINEAR_NONE, ECHO_F32, ECHO_F32, ECHO_F32, 0, p, q, p, q, N, 0)
-            scratch = max(scratch, lib.echo_linear_fp4_workspace(cfg))
+            for epi in (_lib.ECHO_LINEAR_NONE, _lib.ECHO_LINEAR_GELU_TANH, _lib.ECHO_LINEAR_GATE_RESIDUAL):
+                cfg = PACK_LINEAR_FP4(M, N, K, epi, ECHO_F32, ECHO_F32, ECHO_F32, 0, p, q, p, q, N, N)
+                scratch = max(scratch, lib.echo_linear_fp4_workspace(cfg))
         else:
             p = (K + 127) // 128 * 128
             cfg = LinearInt8Cfg(M, N, K, _lib.ECHO_LINEAR_NONE, ECHO_F32, ECHO_F32, ECHO_F32, 0, p, p, N, 0)

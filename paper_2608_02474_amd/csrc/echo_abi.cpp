@@ -919,7 +919,7 @@ int echo_dequantize_rows_fp4(const echo_quantize_fp4_cfg* cfg, const uint8_t* co
 
 size_t echo_linear_fp4_workspace(const echo_linear_fp4_cfg* cfg) {
   if (!linear_fp4_cfg_ok(cfg) || !linear_fp4_supported(cfg) || cfg->M == 0) return 0;
-  return gemm_fp4_partial_bytes(cfg->M, cfg->N, static_cast<int>(echo_fp4_pitch(cfg->K)));
+  return gemm_fp4_partial_bytes(cfg->M, cfg->N, static_cast<int>(echo_fp4_pitch(cfg->K)), cfg->epilogue);
 }
 
 int echo_linear_fp4(const echo_linear_fp4_cfg* cfg, const uint8_t* a, const uint8_t* a_scales, const uint8_t* w,

@@ -61,7 +61,8 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_fp4_tile(G
   constexpr int NM = TI * TJ, NR = TI + TJ;
   constexpr int CA = BM / 32, CB = BN / 32, NCP = CA + CB;
   constexpr int NSC = (BM + BN) / 64;  // copies of 64 rows' scales
-  __shared__ __attribute__((aligned(1024))) char smem[2 * kStage + 2 * kScales];
+  constexpr int kCols = STREAM ? 4 * WN * 8 : 0;  // the waves' bias and gate
+  __shared__ __attribute__((aligned(1024))) char smem[2 * kStage + 2 * kScales + kCols];
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave), lane = tid % kWave;
   const int wm = wave >> 1, wn = wave & 1;
@@ -279,32 +280,43 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_fp4_tile(G
         for (int j = 0; j < TJ; ++j)
           *reinterpret_cast<f32x4*>(out + (wm * WM + i * 16 + l16) * BN + wn * WN + j * 16 + 4 * lq) = acc[i][j];
     } else if constexpr (STREAM) {
-      // the columns' vectors, then two row groups at a time, their residuals a pair of
-      // groups ahead (loads behind stores would wait for them)
+      // The columns' vectors, then the row groups in batches, the residuals of a batch on
+      // their way before the stores of the one before it: memory operations end in order,
+      // so a load behind a store waits for it (a row group a batch: 513 us for 13104 x 5120
+      // x 13824 with a bf16 residual, three 491).
       constexpr bool RES = EPI == EPI_GATE_RES;
+      constexpr int BATCH = RBF ? 3 : 2, NB = (TI + BATCH - 1) / BATCH;
       const int nc = n0 + wn * WN + 4 * lq;
-      OutCols cols[TJ];
+      // (the columns' vectors in the wave's own piece of LDS: 64 registers otherwise)
+      float* const bias = reinterpret_cast<float*>(smem + 2 * kStage + 2 * kScales) + wave * 2 * WN;
+      float* const gate = bias + WN;
+      for (int c = lane; c < WN; c += kWave) {
+        const int n = n0 + wn * WN + c < p.N ? n0 + wn * WN + c : p.N - 1;
+        bias[c] = p.bias != nullptr ? out_load(p.bias, p.bias_bf16, n) : 0.0f;
+        if constexpr (RES) gate[c] = p.gate[n];
+      }
+      ResRaw<RBF> raw[RES ? 2 * BATCH : 1][RES ? TJ : 1];
+      bool miss[2 * BATCH];
+      auto fetch = [&](auto b_c) __attribute__((always_inline)) {
+        constexpr int b = decltype(b_c)::value;
+        if constexpr (RES && b < NB) {
 #pragma unroll
-      for (int j = 0; j < TJ; ++j) out_cols4<EPI>(p, nc + 16 * j < p.N ? nc + 16 * j : p.N - 4, cols[j]);
-      ResRaw<RBF> raw[RES ? 2 : 1][RES ? TJ : 1];
-      bool miss[2];
-      auto fetch = [&](auto i_c) __attribute__((always_inline)) {
-        constexpr int i = decltype(i_c)::value;
-        if constexpr (RES && i < TI) {
-          const int m = m0 + wm * WM + i * 16 + l16;
-          const int rr = out_res_row(p, m < p.M ? m : p.M - 1);
-          miss[i % 2] = rr < 0;
+          for (int i = b * BATCH; i < (b + 1) * BATCH && i < TI; ++i) {
+            const int at = i % (2 * BATCH), m = m0 + wm * WM + i * 16 + l16;
+            const int rr = out_res_row(p, m < p.M ? m : p.M - 1);
+            miss[at] = rr < 0;
 #pragma unroll
-          for (int j = 0; j < TJ; ++j)
-            raw[i % 2][j].load(p.res, static_cast<int64_t>(rr < 0 ? 0 : rr) * p.ldr +
-                                          (nc + 16 * j < p.N ? nc + 16 * j : p.N - 4));
+            for (int j = 0; j < TJ; ++j)
+              raw[at][j].load(p.res, static_cast<int64_t>(rr < 0 ? 0 : rr) * p.ldr +
+                                         (nc + 16 * j < p.N ? nc + 16 * j : p.N - 4));
+          }
         }
       };
       acc_settled(acc[TI - 1][TJ - 1]);
       fetch(S0{});
       static_for<0, TI>([&](auto i_c) __attribute__((always_inline)) {
-        constexpr int i = decltype(i_c)::value;
-        fetch(std::integral_constant<int, i + 1>{});
+        constexpr int i = decltype(i_c)::value, at_i = i % (2 * BATCH);
+        if constexpr (i % BATCH == 0) fetch(std::integral_constant<int, i / BATCH + 1>{});
         const int m = m0 + wm * WM + i * 16 + l16;
         static_for<0, TJ / 2>([&](auto j_c) __attribute__((always_inline)) {
           constexpr int j = decltype(j_c)::value * 2;
@@ -312,10 +324,13 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_fp4_tile(G
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             float res[4];
-            if constexpr (RES) raw[i % 2][j + h].unpack(miss[i % 2], res);
+            if constexpr (RES) raw[at_i][j + h].unpack(miss[at_i], res);
+            const f32x4 cb = *reinterpret_cast<const f32x4*>(bias + 16 * (j + h) + 4 * lq);
+            f32x4 cg = {};
+            if constexpr (RES) cg = *reinterpret_cast<const f32x4*>(gate + 16 * (j + h) + 4 * lq);
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-              z[h][r] = out_finish<EPI>(from_acc(acc[i][j + h][r]) + cols[j + h].bias[r], cols[j + h].gate[r], res[r]);
+              z[h][r] = out_finish<EPI>(from_acc(acc[i][j + h][r]) + cb[r], cg[r], res[r]);
           }
           const int64_t row = m * p.ldc;
           const int at = n0 + wn * WN + 16 * j;
@@ -520,17 +535,18 @@ constexpr int kTileEdge[] = {256, 128, 64};
 // Estimated time of a plan, us, in the form of gemm_int8.hip's estimate: fitted to
 // 166 products of 1 .. 32760 tokens, 64 .. 30720 channels and depths 128 .. 13824 in
 // every tile and split (1789 times; 5 to 9% off on average; the choice by them is 1%
-// slower than the fastest plan on average).  k-steps run in pairs.
+// slower than the fastest plan on average, 2 and 3% with GELU or gate and residual).
+// k-steps run in pairs.
 struct Fp4Cost {
   int resident;
   float start, lat, thr;  // launch and first loads; a k-step
-  float store;            // epilogue, for a workgroup on every CU
+  float store[3];         // each epilogue, for a workgroup on every CU
   float join, piece;      // the second launch of a split product; 1 MB of partial sums
   float cold;             // a k-step's loads with the weights beyond the L2s (32 MB)
 };
-constexpr Fp4Cost kFp4Cost[] = {{1, 5.96f, 1.385f, 0.902f, 7.39f, 7.28f, 0.100f, 0.007f},
-                                {2, 4.25f, 0.725f, 0.550f, 2.21f, 2.13f, 0.249f, 0.060f},
-                                {4, 2.66f, 0.551f, 0.216f, 0.58f, 2.43f, 0.357f, 0.093f}};
+constexpr Fp4Cost kFp4Cost[] = {{1, 5.96f, 1.385f, 0.902f, {11.58f, 15.70f, 29.66f}, 7.28f, 0.100f, 0.007f},
+                                {2, 4.25f, 0.725f, 0.550f, {2.77f, 3.31f, 4.72f}, 2.13f, 0.249f, 0.060f},
+                                {4, 2.66f, 0.551f, 0.216f, {0.67f, 0.75f, 1.26f}, 2.43f, 0.357f, 0.093f}};
 
 struct Fp4Plan {
   int tile;
@@ -547,7 +563,7 @@ size_t fp4_part_bytes(const Fp4Plan& p, int M, int N) {
   return p.nsplit < 2 ? 0 : sizeof(float) * e * e * (fp4_tiles(p.tile, M, N) - p.base) * p.nsplit;
 }
 
-float fp4_us(const Fp4Plan& p, int M, int N, int K, int ncu) {
+float fp4_us(const Fp4Plan& p, int M, int N, int K, int epi, int ncu) {
   const Fp4Cost& c = kFp4Cost[p.tile];
   const int nk = K / 128;
   auto run = [&](int64_t pieces, int steps) {
@@ -555,7 +571,7 @@ float fp4_us(const Fp4Plan& p, int M, int N, int K, int ncu) {
     const float full = c.resident * c.thr > c.lat ? c.resident * c.thr : c.lat;
     const int rest = static_cast<int>(n % c.resident);
     const float last = rest == 0 ? 0.0f : rest * c.thr > c.lat ? rest * c.thr : c.lat;
-    return (n / c.resident * full + last) * ((steps + 1) / 2 * 2) + c.store * static_cast<float>(pieces) / ncu;
+    return (n / c.resident * full + last) * ((steps + 1) / 2 * 2) + c.store[epi] * static_cast<float>(pieces) / ncu;
   };
   const float beyond = static_cast<float>(N) * K / 32e6f;
   float us = c.start + c.cold * (beyond < 1.0f ? beyond : 1.0f) * nk;
@@ -568,7 +584,7 @@ float fp4_us(const Fp4Plan& p, int M, int N, int K, int ncu) {
 // Every tile whole; or the tiles beyond the last whole round of the device, or
 // all of them where they are less than a round, split along the depth: the
 // fastest by the estimate.
-Fp4Plan fp4_plan(int M, int N, int K) {
+Fp4Plan fp4_plan(int M, int N, int K, int epi) {
   const int ncu = device_cu_count(), nk = K / 128;
   constexpr size_t kMostPartial = size_t(64) << 20;
   Fp4Plan best{-1, 0, 1, nk, 0.0f};
@@ -576,7 +592,7 @@ Fp4Plan fp4_plan(int M, int N, int K) {
     const int even = (nk + ns - 1) / ns, kps = ns > 1 ? (even + 1) / 2 * 2 : even;
     Fp4Plan p{tile, static_cast<int>(base), (nk + kps - 1) / kps, kps, 0.0f};  // every range non-empty
     if (fp4_part_bytes(p, M, N) > kMostPartial) return;
-    p.us = fp4_us(p, M, N, K, ncu);
+    p.us = fp4_us(p, M, N, K, epi, ncu);
     if (best.tile < 0 || p.us < best.us) best = p;
   };
   for (int tile = FP4_256; tile <= FP4_64; ++tile) {
@@ -644,9 +660,9 @@ static bool fp4_by_rows(int M, int N, int K, const Fp4Plan& plan) {
   return M <= 2 || (M <= kRowMax && 2.9f + (0.15f + 0.031f * M) * 1e-6f * N * K < plan.us);
 }
 
-size_t gemm_fp4_partial_bytes(int M, int N, int K) {
+size_t gemm_fp4_partial_bytes(int M, int N, int K, int epi) {
   if (M <= 2) return 0;
-  const Fp4Plan plan = fp4_plan(M, N, K);
+  const Fp4Plan plan = fp4_plan(M, N, K, epi);
   return fp4_by_rows(M, N, K, plan) ? 0 : fp4_part_bytes(plan, M, N);
 }
 
@@ -655,7 +671,7 @@ hipError_t launch_gemm_fp4(int epi, const GemmFp4Args& a, hipStream_t stream) {
   // 5120 codes 15.9 and 5.0 us; four channels 15.5 and 5.4, 5 KB 17.6 and 5.6)
   if (a.M == 1) return launch_row<1, 2, 3>(epi, a, stream);
   if (a.M == 2) return launch_row<2, 2, 3>(epi, a, stream);
-  const Fp4Plan plan = fp4_plan(a.M, a.N, a.K);
+  const Fp4Plan plan = fp4_plan(a.M, a.N, a.K, epi);
   if (fp4_by_rows(a.M, a.N, a.K, plan))
     return a.M <= 4 ? launch_row<4, 2, 3>(epi, a, stream) : launch_row<8, 2, 3>(epi, a, stream);
   if (fp4_part_bytes(plan, a.M, a.N) > a.part_bytes) return hipErrorInvalidValue;

@@ -234,7 +234,7 @@ struct GemmFp4Args : RowsOut {
   int64_t ldsb;
   float* part;
 };
-size_t gemm_fp4_partial_bytes(int M, int N, int K);
+size_t gemm_fp4_partial_bytes(int M, int N, int K, int epi);
 hipError_t launch_gemm_fp4(int epi, const GemmFp4Args& a, hipStream_t stream);
 
 // ---- rotary positions (rotary.hip)
