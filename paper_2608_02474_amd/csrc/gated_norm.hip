@@ -9,9 +9,13 @@
 //
 // Apart, these are three kernels that write and read the stream between them;
 // here z and x are read and y and h written once, and the kernel is bound by
-// that.  A row lies in the registers of a wave or a workgroup; a workgroup takes
-// consecutive rows with the vectors over the channels (gate w1, w2 (1 + scale),
-// shift) in registers, and the next row's values on their way.
+// that: 26208 x 5120 with x and y in fp32 (1.6 GB) 335 us, 4.8 TB/s where a copy
+// moves 5.1.  A row lies in the registers of 16 lanes, a wave or a workgroup; a
+// workgroup takes consecutive rows with the vectors over the channels (gate w1,
+// w2 (1 + scale), shift) in registers, and the next row's values on their way
+// behind the first norm (during it too, they took the registers of a second
+// workgroup on the CU).  Rows of more than 6144 columns do neither (9000 x 13824:
+// 402 us, 453 with the next row on its way).
 #include "common.h"
 #include "kernels.h"
 #include "launch.h"
@@ -38,7 +42,8 @@ __device__ __forceinline__ void store1(void* p, int bf, int64_t i, float v) {
 
 // A row to `threads` threads (16 if NARROW, one wave or the whole workgroup), NV chunks
 // of 8 values each.  VEC: every row of every tensor is aligned for 16-byte accesses and D % 8 == 0.
-// HOLD: the vectors over the channels stay in registers for a workgroup's rows.
+// HOLD: the vectors over the channels stay in registers for a workgroup's rows, and the
+// next row is fetched ahead.
 template <int MAXT, int NV, bool VEC, bool HOLD, bool NARROW, typename TZ, typename TX>
 __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int threads, int rows_per_wg) {
   __shared__ float red[2][4][MAXT / kWave];
@@ -144,7 +149,7 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
   const int64_t end = base + rows_per_wg < p.M ? base + rows_per_wg : p.M;
   int64_t row = base + threadIdx.x / threads;
   int have = -1;
-  if constexpr (VEC)
+  if constexpr (VEC && HOLD)
     if (row < end) fetch(row);
   // (a group that reaches a barrier is the whole workgroup, so the loop is uniform for its waves)
   for (; row < end; row += rpb) {
@@ -158,6 +163,7 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
       }
     }
     const int gm = no_group ? 0 : g;
+    if constexpr (VEC && !HOLD) fetch(row);
     float v[NV][8];
     int64_t xr = 0;
     bool bad = nbad;
@@ -191,7 +197,7 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
       }
     }
     // the next row's values, on their way through the stores and the second norm
-    if constexpr (VEC)
+    if constexpr (VEC && HOLD)
       if (row + rpb < end) fetch(row + rpb);
     auto put = [&](void* out, int bf, int64_t ld) __attribute__((always_inline)) {
 #pragma unroll
@@ -242,7 +248,9 @@ hipError_t launch_w(const GatedNormArgs& p, int threads, hipStream_t stream) {
   return p.x_bf16 ? go(0.0f, bf16_t{}) : go(0.0f, 0.0f);
 }
 // The fewest chunks a thread that 256 threads hold the row with (wider ones: four to
-// 512 threads), and no more threads than that takes
+// 512 threads), and no more threads than that takes (26208 x 5120: three chunks to 256
+// threads 335 us, two to 320 390; 400000 x 64: 16 lanes to a row 67, a wave 193; 16000 x
+// 8192: four to 256 361, two to 512 345, but 9000 x 13824 402 and 452)
 template <bool VEC>
 hipError_t launch_v(const GatedNormArgs& p, hipStream_t stream) {
   auto threads = [&](int chunks) { return (p.D + 8 * chunks * kWave - 1) / (8 * chunks * kWave) * kWave; };

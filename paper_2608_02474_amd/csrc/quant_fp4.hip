@@ -132,10 +132,11 @@ __global__ void __launch_bounds__(256) quantize_fp4_k(QuantizeArgs p, int64_t st
 
 // With LayerNorm: a row to `threads` threads (16 if NARROW, one wave or the whole
 // workgroup), NV chunks of 8 values each; a workgroup takes consecutive rows, the next
-// row's values on their way and (HOLD) the modulation in registers.
+// row's values on their way and the modulation in registers (HOLD: where they leave room
+// for a second workgroup on the CU; of wider rows both are read when they are due).
 template <typename T, int MAXT, int NV, bool VEC, bool NARROW>
 __global__ void __launch_bounds__(MAXT) quantize_fp4_ln_k(QuantizeArgs p, int threads, int rows_per_wg) {
-  constexpr bool HOLD = NV <= 4, AHEAD = VEC && NV <= 4;
+  constexpr bool HOLD = MAXT <= 256 || NV <= 2, AHEAD = VEC && HOLD;
   __shared__ float red[2][2][MAXT / kWave];
   const int t = threadIdx.x % threads, D = p.D, rpb = blockDim.x / threads, waves = threads / kWave;
   int turn = 0;
@@ -309,7 +310,8 @@ hipError_t launch_ln(const QuantizeArgs& p, int threads, hipStream_t stream) {
 // 1024 a wave, then up to 256 threads with up to three chunks and no more threads than
 // that takes (32760 x 5120: three chunks to 256 threads 102 us, two to 320 142; 100000 x
 // 1024: two to a wave 60, one to 128 threads 73; 16000 x 8192: two to 512 threads 96, four
-// to 256 102).
+// to 256 102; 13104 x 13824: four to 448 threads 149, two to 896 172, 181 if they hold the
+// modulation).
 template <typename T, bool VEC>
 hipError_t launch_ln_width(const QuantizeArgs& p, hipStream_t stream) {
   auto threads = [&](int chunks) { return (p.D + 8 * chunks * kWave - 1) / (8 * chunks * kWave) * kWave; };
@@ -321,7 +323,7 @@ hipError_t launch_ln_width(const QuantizeArgs& p, hipStream_t stream) {
   if (p.D <= 4096) return launch_ln<T, 256, 2, VEC>(p, threads(2), stream);
   if (p.D <= 6144) return launch_ln<T, 256, 3, VEC>(p, threads(3), stream);
   if (p.D <= 8192) return launch_ln<T, 512, 2, VEC>(p, threads(2), stream);
-  if (p.D <= 16384) return launch_ln<T, 1024, 2, VEC>(p, threads(2), stream);
+  if (p.D <= 16384) return launch_ln<T, 512, 4, VEC>(p, threads(4), stream);
   return launch_ln<T, 1024, 8, VEC>(p, threads(8), stream);  // 65536 values
 }
 
