@@ -569,7 +569,8 @@ int echo_linear_int8(const echo_linear_int8_cfg* cfg, const int8_t* a, const flo
  * lds bytes apart; ldq a multiple of 128, at least echo_fp4_pitch(D), lds a
  * multiple of 16, at least echo_fp4_scale_pitch(D); the first so many bytes of a
  * row are written, with zeros behind column D, others are left as they are.
- * x, rows, shift and scale as in echo_quantize_rows.
+ * x, rows, shift and scale as in echo_quantize_rows, but shift and scale may be
+ * at any element.
  *
  * echo_dequantize_rows_fp4: x_ij = cast(2^e code_ij), x being the output here;
  * rows, shift and scale do not apply (x_rows is not read).

@@ -143,6 +143,78 @@ template <> struct Raw8<float> {
   }
 };
 
+// The same at any element's alignment (vector accesses of any alignment are the
+// hardware's own), and chunk c of a row of D elements: what lies past its end is
+// zero and is not touched.  VEC: rows are aligned to 16 bytes and D % 8 == 0.
+typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T>
+__device__ __forceinline__ void load8_any(Raw8<T>& r, const T* p) {
+  typedef std::conditional_t<sizeof(T) == 2, u32x4_at2, u32x4_at4> any4;
+  const any4* q = reinterpret_cast<const any4*>(p);
+  const any4 a = q[0];
+  if constexpr (sizeof(T) == 2) {
+    r.v = make_uint4(a.x, a.y, a.z, a.w);
+  } else {
+    const any4 b = q[1];
+    r.v0 = make_uint4(a.x, a.y, a.z, a.w);
+    r.v1 = make_uint4(b.x, b.y, b.z, b.w);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8_any(T* p, const Raw8<T>& r) {
+  typedef std::conditional_t<sizeof(T) == 2, u32x4_at2, u32x4_at4> any4;
+  any4* q = reinterpret_cast<any4*>(p);
+  if constexpr (sizeof(T) == 2) {
+    q[0] = any4{r.v.x, r.v.y, r.v.z, r.v.w};
+  } else {
+    q[0] = any4{r.v0.x, r.v0.y, r.v0.z, r.v0.w};
+    q[1] = any4{r.v1.x, r.v1.y, r.v1.z, r.v1.w};
+  }
+}
+template <typename T>
+__device__ __forceinline__ void pack8(Raw8<T>& r, const float* v) {
+  if constexpr (sizeof(T) == 2) {
+    r.v = pack16(v, static_cast<const T*>(nullptr));
+  } else {
+    r.v0 = pack16(v, static_cast<const T*>(nullptr));
+    r.v1 = pack16(v + 4, static_cast<const T*>(nullptr));
+  }
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void load_chunk(Raw8<T>& r, const T* row, int c, int D) {
+  r = Raw8<T>{};
+  if constexpr (VEC) {
+    if (c < D) r.load_nt(row + c);
+  } else if (c + 8 <= D) {
+    load8_any(r, row + c);  // (neighbours share lines here, so no streaming access)
+  } else if (c < D) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < D ? Elem<T>::load(row, c + j) : 0.0f;
+    pack8(r, v);
+  }
+}
+template <bool VEC, bool STREAM, typename T>
+__device__ __forceinline__ void store_chunk(T* row, int c, int D, const float* v) {
+  Raw8<T> r;
+  pack8(r, v);
+  if constexpr (VEC) {
+    if (c < D) {
+      if constexpr (STREAM)
+        r.store_nt(row + c);
+      else
+        r.store(row + c);
+    }
+  } else if (c + 8 <= D) {
+    store8_any(row + c, r);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (c + j < D) Elem<T>::store(row, c + j, v[j]);
+  }
+}
+
 // GELU with the tanh approximation, using 0.5 z (1 + tanh u) = z / (1 + e^{-2u})
 // with u = sqrt(2/pi) (z + 0.044715 z^3): e^{-2u} = 2^{z (k1 + k2 z^2)}, k1 =
 // -2 sqrt(2/pi) log2(e), k2 = 0.044715 k1, so the argument is one FMA and two

@@ -895,7 +895,7 @@ int echo_quantize_rows_fp4(const echo_quantize_fp4_cfg* cfg, const void* x, cons
   if (cfg->M == 0) return ECHO_OK;
   if (!elem_aligned(x, esize(cfg->dtype)) || !ok_ptr(codes) || !ok_ptr(scales) ||
       (rows != nullptr ? !elem_aligned(rows, 4) || cfg->x_rows < 1 : cfg->x_rows < cfg->M) ||
-      (shift != nullptr && (!ok_ptr(shift) || !ok_ptr(scale))))
+      (shift != nullptr && (!elem_aligned(shift, 4) || !elem_aligned(scale, 4))))
     return ECHO_EINVAL;
   QuantizeArgs a{};
   a.x = x; a.ldx = cfg->ldx; a.rows = rows; a.x_rows = cfg->x_rows; a.M = cfg->M; a.D = cfg->D;

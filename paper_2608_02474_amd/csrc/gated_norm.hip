@@ -14,34 +14,17 @@
 // workgroup takes consecutive rows with the vectors over the channels (gate w1,
 // w2 (1 + scale), shift) in registers, and the next row's values on their way
 // behind the first norm (during it too, they took the registers of a second
-// workgroup on the CU).  Rows of more than 6144 columns do neither (9000 x 13824:
-// 402 us, 453 with the next row on its way).
+// workgroup on the CU).  Rows of more than 8192 columns do neither (they would
+// leave 1024 threads no registers).  Unaligned rows take vector accesses at any
+// element (7341 columns: 206 us where single elements took 769).
 #include "common.h"
 #include "kernels.h"
 #include "launch.h"
 
 namespace echo {
 
-__device__ __forceinline__ void store8(void* p, int bf, int64_t i, const float* v) {
-  if (bf) {
-    stg16(static_cast<bf16_t*>(p) + i, pack16(v, static_cast<const bf16_t*>(nullptr)));
-  } else {
-    stg16(static_cast<float*>(p) + i, pack16(v, static_cast<const float*>(nullptr)));
-    stg16(static_cast<float*>(p) + i + 4, pack16(v + 4, static_cast<const float*>(nullptr)));
-  }
-}
-__device__ __forceinline__ float load1(const void* p, int bf, int64_t i) {
-  return bf ? bf16_to_f32(static_cast<const bf16_t*>(p)[i]) : static_cast<const float*>(p)[i];
-}
-__device__ __forceinline__ void store1(void* p, int bf, int64_t i, float v) {
-  if (bf)
-    static_cast<bf16_t*>(p)[i] = f32_to_bf16(v);
-  else
-    static_cast<float*>(p)[i] = v;
-}
-
 // A row to `threads` threads (16 if NARROW, one wave or the whole workgroup), NV chunks
-// of 8 values each.  VEC: every row of every tensor is aligned for 16-byte accesses and D % 8 == 0.
+// of 8 values each.  VEC: every row of every tensor is aligned to 16 bytes and D % 8 == 0.
 // HOLD: the vectors over the channels stay in registers for a workgroup's rows, and the
 // next row is fetched ahead.
 template <int MAXT, int NV, bool VEC, bool HOLD, bool NARROW, typename TZ, typename TX>
@@ -92,20 +75,19 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[u][j] *= r;
   };
-  // a vector over the channels, `none` where it is not given and past the last column
+  // a vector over the channels, `none` where it is not given (past the last column 0)
   auto vector = [&](const float* w, int u, float none, float* o) __attribute__((always_inline)) {
     const int c = (t + u * threads) * 8;
-    if (VEC) {
-      if (w != nullptr && c < D) {
-        unpack16(ldg16(w + c), o, static_cast<const float*>(nullptr));
-        unpack16(ldg16(w + c + 4), o + 4, static_cast<const float*>(nullptr));
-        return;
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = none;
+    if (w != nullptr && (!VEC || c < D)) {
+      Raw8<float> r;
+      if constexpr (VEC)
+        r.load(w + c);
+      else
+        load_chunk<false>(r, w, c, D);
+      r.unpack(o);
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = w != nullptr && c + j < D ? w[c + j] : none;
+      for (int j = 0; j < 8; ++j) o[j] = none;
     }
   };
   auto gate_of = [&](int g, int u, float* o) __attribute__((always_inline)) {  // gate w1
@@ -126,8 +108,8 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
     vector(p.shift != nullptr ? p.shift + g * p.ldshift : nullptr, u, 0.0f, o);
   };
   float ga[HOLD ? NV : 1][8], sc[HOLD ? NV : 1][8], sh[HOLD ? NV : 1][8];
-  Raw8<TZ> nz[VEC ? NV : 1];
-  Raw8<TX> nx[VEC ? NV : 1];
+  Raw8<TZ> nz[NV];
+  Raw8<TX> nx[NV];
   bool nbad = false;
   auto source = [&](int64_t row, bool& bad) __attribute__((always_inline)) -> int64_t {
     bad = false;
@@ -140,16 +122,23 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
     const int64_t xr = source(row, nbad);
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      const int c = (t + u * threads) * 8, k = c < D ? c : 0;
-      nz[VEC ? u : 0].load_nt(static_cast<const TZ*>(p.z) + row * p.ldz + k);
-      nx[VEC ? u : 0].load_nt(static_cast<const TX*>(p.x) + xr * p.ldx + k);
+      const int c = (t + u * threads) * 8;
+      const TZ* z = static_cast<const TZ*>(p.z) + row * p.ldz;
+      const TX* x = static_cast<const TX*>(p.x) + xr * p.ldx;
+      if constexpr (VEC) {
+        nz[u].load_nt(z + (c < D ? c : 0));
+        nx[u].load_nt(x + (c < D ? c : 0));
+      } else {
+        load_chunk<false>(nz[u], z, c, D);
+        load_chunk<false>(nx[u], x, c, D);
+      }
     }
   };
   const int64_t base = static_cast<int64_t>(blockIdx.x) * rows_per_wg;
   const int64_t end = base + rows_per_wg < p.M ? base + rows_per_wg : p.M;
   int64_t row = base + threadIdx.x / threads;
   int have = -1;
-  if constexpr (VEC && HOLD)
+  if constexpr (HOLD)
     if (row < end) fetch(row);
   // (a group that reaches a barrier is the whole workgroup, so the loop is uniform for its waves)
   for (; row < end; row += rpb) {
@@ -163,21 +152,15 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
       }
     }
     const int gm = no_group ? 0 : g;
-    if constexpr (VEC && !HOLD) fetch(row);
+    if constexpr (!HOLD) fetch(row);
     float v[NV][8];
-    int64_t xr = 0;
     bool bad = nbad;
-    if constexpr (!VEC) xr = source(row, bad);
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      if constexpr (VEC) nz[u].unpack(v[u]);
+      nz[u].unpack(v[u]);
+      if constexpr (VEC) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int c = (t + u * threads) * 8 + j;
-        if constexpr (VEC)
-          v[u][j] = in(u, j) ? v[u][j] : 0.0f;
-        else
-          v[u][j] = c < D ? load1(p.z, p.z_bf16, row * p.ldz + c) : 0.0f;
+        for (int j = 0; j < 8; ++j) v[u][j] = in(u, j) ? v[u][j] : 0.0f;
       }
     }
     bad = bad || no_group;
@@ -186,30 +169,25 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
     for (int u = 0; u < NV; ++u) {
       float m[8], x[8];
       if constexpr (!HOLD) gate_of(gm, u, m);
-      if constexpr (VEC) nx[u].unpack(x);
+      nx[u].unpack(x);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int c = (t + u * threads) * 8 + j;
-        if constexpr (!VEC) x[j] = c < D ? load1(p.x, p.x_bf16, xr * p.ldx + c) : 0.0f;
         v[u][j] = fmaf(v[u][j], HOLD ? ga[HOLD ? u : 0][j] : m[j], p.alpha * x[j]);
         if (bad) v[u][j] = __uint_as_float(0x7fc00000u);
         if (!in(u, j)) v[u][j] = 0.0f;
       }
     }
     // the next row's values, on their way through the stores and the second norm
-    if constexpr (VEC && HOLD)
+    if constexpr (HOLD)
       if (row + rpb < end) fetch(row + rpb);
     auto put = [&](void* out, int bf, int64_t ld) __attribute__((always_inline)) {
 #pragma unroll
       for (int u = 0; u < NV; ++u) {
         const int c = (t + u * threads) * 8;
-        if (VEC) {
-          if (c < D) store8(out, bf, row * ld + c, v[u]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (c + j < D) store1(out, bf, row * ld + c + j, v[u][j]);
-        }
+        if (bf)
+          store_chunk<VEC, false>(static_cast<bf16_t*>(out) + row * ld, c, D, v[u]);
+        else
+          store_chunk<VEC, false>(static_cast<float*>(out) + row * ld, c, D, v[u]);
       }
     };
     put(p.y, p.y_bf16, p.ldy);
@@ -235,7 +213,8 @@ template <int MAXT, int NV, bool VEC, bool HOLD, bool NARROW = false>
 hipError_t launch_w(const GatedNormArgs& p, int threads, hipStream_t stream) {
   const int block = threads <= kWave ? 256 : threads, rpb = block / threads;
   // consecutive rows of a workgroup share one read of the vectors
-  const int64_t want = static_cast<int64_t>(device_cu_count()) * 2048 / block;
+  // (a whole number of workgroups to a CU: 9000 x 13824 takes 431 us with 7/3 of them)
+  const int64_t want = static_cast<int64_t>(device_cu_count()) * (2048 / block);
   int64_t per = (p.M + want - 1) / want;
   per = (per + rpb - 1) / rpb * rpb;
   const dim3 grid(static_cast<unsigned>((p.M + per - 1) / per));
@@ -243,22 +222,26 @@ hipError_t launch_w(const GatedNormArgs& p, int threads, hipStream_t stream) {
     return ECHO_LAUNCH("gated_norm", (gated_norm_k<MAXT, NV, VEC, HOLD, NARROW, decltype(z), decltype(x)>), grid, dim3(block), 0,
                        stream, p, threads, static_cast<int>(per));
   };
-  if (!VEC) return go(0.0f, 0.0f);  // (its loads go by the tensors' types themselves)
   if (p.z_bf16) return p.x_bf16 ? go(bf16_t{}, bf16_t{}) : go(bf16_t{}, 0.0f);
   return p.x_bf16 ? go(0.0f, bf16_t{}) : go(0.0f, 0.0f);
 }
-// The fewest chunks a thread that 256 threads hold the row with (wider ones: four to
-// 512 threads), and no more threads than that takes (26208 x 5120: three chunks to 256
-// threads 335 us, two to 320 390; 400000 x 64: 16 lanes to a row 67, a wave 193; 16000 x
-// 8192: four to 256 361, two to 512 345, but 9000 x 13824 402 and 452)
+// The fewest chunks a thread that 256 threads hold the row with, and no more threads
+// than that takes (26208 x 5120: three chunks to 256 threads 335 us, two to 320 390;
+// 400000 x 64: 16 lanes to a row 67, a wave 193).  Wider rows, and unaligned ones whose
+// bounds would take the registers of a second chunk, go to up to 1024 threads with one
+// chunk, two from 8192 columns on (16000 x 8192: 327, four to 256 threads 354; 9000 x
+// 13824: 359, four to 448 threads 395; 7524 x 7341: 206, four to 256 threads 617).
 template <bool VEC>
 hipError_t launch_v(const GatedNormArgs& p, hipStream_t stream) {
   auto threads = [&](int chunks) { return (p.D + 8 * chunks * kWave - 1) / (8 * chunks * kWave) * kWave; };
   if (p.D <= 128) return launch_w<256, 1, VEC, true, true>(p, 16, stream);
   if (p.D <= 2048) return launch_w<256, 1, VEC, true>(p, threads(1), stream);
-  if (p.D <= 4096) return launch_w<256, 2, VEC, true>(p, threads(2), stream);
-  if (p.D <= 6144) return launch_w<256, 3, VEC, true>(p, threads(3), stream);
-  return launch_w<512, 4, VEC, false>(p, threads(4), stream);
+  if constexpr (VEC) {  // (the bounds of unaligned rows take the registers that would hold the vectors)
+    if (p.D <= 4096) return launch_w<256, 2, VEC, true>(p, threads(2), stream);
+    if (p.D <= 6144) return launch_w<256, 3, VEC, true>(p, threads(3), stream);
+  }
+  if (p.D <= 8192) return launch_w<1024, 1, VEC, true>(p, threads(1), stream);
+  return launch_w<1024, 2, VEC, false>(p, threads(2), stream);
 }
 
 }  // namespace

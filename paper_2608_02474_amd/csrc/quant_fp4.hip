@@ -89,8 +89,7 @@ __global__ void __launch_bounds__(256) quantize_fp4_k(QuantizeArgs p, int64_t st
     int64_t rows[U];
     int at[U];
     bool bad[U];
-    Raw8<T> raw[VEC ? U : 1];
-    float v[VEC ? 1 : U][8];
+    Raw8<T> raw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       rows[u] = row;
@@ -99,12 +98,7 @@ __global__ void __launch_bounds__(256) quantize_fp4_k(QuantizeArgs p, int64_t st
       const T* x = static_cast<const T*>(p.x);
       bad[u] = false;
       if (row < p.M) x += row_of(p, row, bad[u]) * p.ldx;
-      if constexpr (VEC) {
-        raw[u].load_nt(x + (c < p.D ? c : 0));
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[u][j] = c + j < p.D ? Elem<T>::load(x, c + j) : 0.0f;
-      }
+      load_chunk<VEC>(raw[u], x, c, p.D);
       row += step_row;
       set += step_set;
       if (set >= sets) set -= sets, ++row;
@@ -113,16 +107,7 @@ __global__ void __launch_bounds__(256) quantize_fp4_k(QuantizeArgs p, int64_t st
     for (int u = 0; u < U; ++u) {
       if (rows[u] >= p.M) break;
       float f[8];
-      if constexpr (VEC) {
-        raw[u].unpack(f);
-        if (at[u] * 128 + lane * 8 >= p.D) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = 0.0f;
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = v[u][j];
-      }
+      raw[u].unpack(f);
       uint32_t scales;
       const uint32_t w = codes8_fp4(f, bad[u], scales);
       put_set(p, rows[u], at[u], w, scales);
@@ -136,7 +121,7 @@ __global__ void __launch_bounds__(256) quantize_fp4_k(QuantizeArgs p, int64_t st
 // for a second workgroup on the CU; of wider rows both are read when they are due).
 template <typename T, int MAXT, int NV, bool VEC, bool NARROW>
 __global__ void __launch_bounds__(MAXT) quantize_fp4_ln_k(QuantizeArgs p, int threads, int rows_per_wg) {
-  constexpr bool HOLD = MAXT <= 256 || NV <= 2, AHEAD = VEC && HOLD;
+  constexpr bool HOLD = MAXT <= 256 || NV <= 2, AHEAD = HOLD;
   __shared__ float red[2][2][MAXT / kWave];
   const int t = threadIdx.x % threads, D = p.D, rpb = blockDim.x / threads, waves = threads / kWave;
   int turn = 0;
@@ -156,20 +141,19 @@ __global__ void __launch_bounds__(MAXT) quantize_fp4_ln_k(QuantizeArgs p, int th
   // there come out as zeros
   auto modulation = [&](int u, float* sc, float* sh) __attribute__((always_inline)) {
     const int c = (t + u * threads) * 8;
-    if (VEC) {
-      const int k = c < D ? c : 0;
-      unpack16(ldg16(p.scale + k), sc, static_cast<const float*>(nullptr));
-      unpack16(ldg16(p.scale + k + 4), sc + 4, static_cast<const float*>(nullptr));
-      unpack16(ldg16(p.shift + k), sh, static_cast<const float*>(nullptr));
-      unpack16(ldg16(p.shift + k + 4), sh + 4, static_cast<const float*>(nullptr));
+    Raw8<float> rs, rh;
+    if constexpr (VEC) {
+      rs.load(p.scale + (c < D ? c : 0));
+      rh.load(p.shift + (c < D ? c : 0));
+    } else {
+      load_chunk<false>(rs, p.scale, c, D);
+      load_chunk<false>(rh, p.shift, c, D);
     }
+    rs.unpack(sc);
+    rh.unpack(sh);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const bool in = VEC ? c < D : c + j < D;
-      if (!VEC) {
-        sc[j] = in ? p.scale[c + j] : 0.0f;
-        sh[j] = in ? p.shift[c + j] : 0.0f;
-      }
       sc[j] = in ? 1.0f + sc[j] : 0.0f;
       sh[j] = in ? sh[j] : 0.0f;
     }
@@ -185,9 +169,7 @@ __global__ void __launch_bounds__(MAXT) quantize_fp4_ln_k(QuantizeArgs p, int th
     const T* x = static_cast<const T*>(p.x) + row_of(p, row, next_bad) * p.ldx;
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      const int c = (t + u * threads) * 8;
-      next[AHEAD ? u : 0] = Raw8<T>{};
-      if (c < D) next[AHEAD ? u : 0].load_nt(x + c);
+      load_chunk<VEC>(next[AHEAD ? u : 0], x, (t + u * threads) * 8, D);
     }
   };
   const int64_t base = static_cast<int64_t>(blockIdx.x) * rows_per_wg;
@@ -203,16 +185,12 @@ __global__ void __launch_bounds__(MAXT) quantize_fp4_ln_k(QuantizeArgs p, int th
     if constexpr (!AHEAD) x = static_cast<const T*>(p.x) + row_of(p, row, bad) * p.ldx;
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      const int c = (t + u * threads) * 8;
       if constexpr (AHEAD) {
         next[u].unpack(v[u]);
-      } else if constexpr (VEC) {
-        Raw8<T> raw{};
-        if (c < D) raw.load_nt(x + c);
-        raw.unpack(v[u]);
       } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[u][j] = c + j < D ? Elem<T>::load(x, c + j) : 0.0f;
+        Raw8<T> raw;
+        load_chunk<VEC>(raw, x, (t + u * threads) * 8, D);
+        raw.unpack(v[u]);
       }
     }
     if constexpr (AHEAD)
@@ -252,8 +230,8 @@ __global__ void __launch_bounds__(MAXT) quantize_fp4_ln_k(QuantizeArgs p, int th
 }
 
 // y_ij = cast(2^e_b c_ij), exact in both types; a thread takes 8 values
-template <typename T>
-__global__ void __launch_bounds__(256) dequantize_fp4_k(DequantizeArgs p, int vec) {
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) dequantize_fp4_k(DequantizeArgs p) {
   typedef float f32x2 __attribute__((ext_vector_type(2)));
   const int nch = (p.D + 7) / 8;
   for (int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; e < static_cast<int64_t>(p.M) * nch;
@@ -269,14 +247,7 @@ __global__ void __launch_bounds__(256) dequantize_fp4_k(DequantizeArgs p, int ve
     const f32x2 u2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 2);
     const f32x2 u3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, 1.0f, 3);
     const float v[8] = {s * u0[0], s * u0[1], s * u1[0], s * u1[1], s * u2[0], s * u2[1], s * u3[0], s * u3[1]};
-    T* y = static_cast<T*>(p.y) + row * p.ldy + c;
-    if (vec) {
-      constexpr int PV = Elem<T>::kPerVec;
-#pragma unroll
-      for (int h = 0; h < 8 / PV; ++h) stg16_nt(y + h * PV, pack16(v + h * PV, static_cast<const T*>(nullptr)));
-    } else {
-      for (int j = 0; j < 8 && c + j < p.D; ++j) Elem<T>::store(y, j, v[j]);
-    }
+    store_chunk<VEC, true>(static_cast<T*>(p.y) + row * p.ldy, c, p.D, v);
   }
 }
 
@@ -329,7 +300,9 @@ hipError_t launch_ln_width(const QuantizeArgs& p, hipStream_t stream) {
 
 template <typename T>
 hipError_t launch_type(const QuantizeArgs& p, hipStream_t stream) {
-  const bool vec = p.D % 8 == 0 && p.ldx % Elem<T>::kPerVec == 0 && reinterpret_cast<uintptr_t>(p.x) % 16 == 0;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.shift) |
+                       reinterpret_cast<uintptr_t>(p.scale);
+  const bool vec = p.D % 8 == 0 && p.ldx % Elem<T>::kPerVec == 0 && at % 16 == 0;
   if (p.shift != nullptr) return vec ? launch_ln_width<T, true>(p, stream) : launch_ln_width<T, false>(p, stream);
   return vec ? launch_plain<T, true>(p, stream) : launch_plain<T, false>(p, stream);
 }
@@ -343,11 +316,13 @@ hipError_t launch_quantize_rows_fp4(int dtype_bf16, const QuantizeArgs& p, hipSt
 hipError_t launch_dequantize_rows_fp4(int dtype_bf16, const DequantizeArgs& p, hipStream_t stream) {
   const int64_t n = (static_cast<int64_t>(p.M) * ((p.D + 7) / 8) + 255) / 256;
   const dim3 grid(static_cast<unsigned>(n < kMaxGroups ? n : kMaxGroups));
-  const int per = dtype_bf16 ? 8 : 4;
-  const int vec = p.D % 8 == 0 && p.ldy % per == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0;
-  return dtype_bf16
-             ? ECHO_LAUNCH("dequantize_rows_fp4", dequantize_fp4_k<bf16_t>, grid, dim3(256), 0, stream, p, vec)
-             : ECHO_LAUNCH("dequantize_rows_fp4", dequantize_fp4_k<float>, grid, dim3(256), 0, stream, p, vec);
+  auto go = [&](auto t) -> hipError_t {
+    typedef decltype(t) T;
+    return p.D % 8 == 0 && p.ldy % Elem<T>::kPerVec == 0 && reinterpret_cast<uintptr_t>(p.y) % 16 == 0
+               ? ECHO_LAUNCH("dequantize_rows_fp4", (dequantize_fp4_k<T, true>), grid, dim3(256), 0, stream, p)
+               : ECHO_LAUNCH("dequantize_rows_fp4", (dequantize_fp4_k<T, false>), grid, dim3(256), 0, stream, p);
+  };
+  return dtype_bf16 ? go(bf16_t{}) : go(0.0f);
 }
 
 }  // namespace echo

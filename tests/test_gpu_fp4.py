@@ -189,6 +189,17 @@ def test_quantize_layernorm(M, D, dtype):
     assert torch.equal(r2.codes.cpu().flip(0), r.codes.cpu()) and torch.equal(r2.scales.cpu().flip(0), r.scales.cpu())
 
 
+@pytest.mark.parametrize("M,D", [(3, 37), (40, 260), (5, 1025), (4, 3003), (3, 7341), (2, 10001)])
+def test_quantize_layernorm_with_vectors_at_any_element(M, D):
+    """Rows of one modulation [2, D]: of an odd D the second starts off a vector's
+    border.  The values are those of vectors of their own, bit for bit."""
+    g = _gen(D + 2)
+    x, m = _rand(g, M, D, dtype=torch.bfloat16).to(device()), (_rand(g, 2, D) * 0.1).to(device())
+    r = api.quantize_rows_fp4(x, shift=m[0], scale=m[1])
+    own = api.quantize_rows_fp4(x, shift=m[0].clone(), scale=m[1].clone())
+    assert torch.equal(r.codes, own.codes) and torch.equal(r.scales, own.scales)
+
+
 def test_quantize_empty():
     r = api.quantize_rows_fp4(torch.zeros(0, 64, device=device()))
     assert r.codes.shape == (0, 128) and r.scales.shape == (0, 16)
