@@ -59,7 +59,7 @@ def test_quantize_rejects_before_launch(lib):
                 dict(ldq=192), dict(ldq=65536 + 128), dict(lds=8), dict(lds=24), dict(lds=65552), dict(D=513, ldx=513, ldq=384),
                 dict(eps=-1.0), dict(eps=float("nan")), dict(x=None), dict(x=ODD), dict(q=None), dict(q=OFF4),
                 dict(s=None), dict(s=OFF4), dict(nx=3), dict(rows=FAKE, nx=0), dict(rows=ODD), dict(sh=FAKE),
-                dict(sc=FAKE), dict(sh=OFF4, sc=FAKE)):
+                dict(sc=FAKE), dict(sh=ODD, sc=FAKE), dict(sh=OFF4, sc=ODD)):
         assert run(**bad) == EINVAL, bad
     assert lib.echo_quantize_rows_fp4(None, FAKE, None, None, None, FAKE, FAKE, None) == EINVAL
     assert run(M=0, x=None, q=None, s=None) == OK
