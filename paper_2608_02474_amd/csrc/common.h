@@ -144,8 +144,9 @@ template <> struct Raw8<float> {
 };
 
 // The same at any element's alignment (vector accesses of any alignment are the
-// hardware's own), and chunk c of a row of D elements: what lies past its end is
-// zero and is not touched.  VEC: rows are aligned to 16 bytes and D % 8 == 0.
+// hardware's own), and the chunk of a row of D elements that starts at c: what lies
+// past the row's end is zero and is not touched.  VEC: rows are aligned to 16 bytes
+// and D % 8 == 0.  STREAM: data that is read or written once.
 typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 template <typename T>
@@ -181,18 +182,39 @@ __device__ __forceinline__ void pack8(Raw8<T>& r, const float* v) {
     r.v1 = pack16(v + 4, static_cast<const T*>(nullptr));
   }
 }
-template <bool VEC, typename T>
+// (a chunk that the row ends in is read so that it ends with the row, and moved into
+// place when it is unpacked: the loads of a thread's chunks wait for no branch)
+template <bool VEC, bool STREAM, typename T>
 __device__ __forceinline__ void load_chunk(Raw8<T>& r, const T* row, int c, int D) {
-  r = Raw8<T>{};
   if constexpr (VEC) {
-    if (c < D) r.load_nt(row + c);
-  } else if (c + 8 <= D) {
-    load8_any(r, row + c);  // (neighbours share lines here, so no streaming access)
-  } else if (c < D) {
+    const T* q = row + (c < D ? c : 0);
+    if constexpr (STREAM)
+      r.load_nt(q);
+    else
+      r.load(q);
+  } else if (D >= 8) {
+    load8_any(r, row + (c < D - 8 ? c : D - 8));  // (neighbours share lines here, so no streaming access)
+  } else {
     float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < D ? Elem<T>::load(row, c + j) : 0.0f;
+    for (int j = 0; j < 8; ++j) v[j] = Elem<T>::load(row, j < D ? j : 0);
     pack8(r, v);
+  }
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void unpack_chunk(const Raw8<T>& r, int c, int D, float* v) {
+  r.unpack(v);
+  if constexpr (VEC) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c < D ? v[j] : 0.0f;
+  } else if (c + 8 > D) {
+    const int k = D >= 8 ? c - (D - 8) : 0;
+#pragma unroll
+    for (int b = 4; b >= 1; b /= 2)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = (k & b) ? (j + b < 8 ? v[j + b] : 0.0f) : v[j];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < D ? v[j] : 0.0f;
   }
 }
 template <bool VEC, bool STREAM, typename T>

@@ -16,7 +16,7 @@
 // behind the first norm (during it too, they took the registers of a second
 // workgroup on the CU).  Rows of more than 8192 columns do neither (they would
 // leave 1024 threads no registers).  Unaligned rows take vector accesses at any
-// element (7341 columns: 206 us where single elements took 769).
+// element (7524 x 7341: 166 us where single elements took 769).
 #include "common.h"
 #include "kernels.h"
 #include "launch.h"
@@ -78,13 +78,13 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
   // a vector over the channels, `none` where it is not given (past the last column 0)
   auto vector = [&](const float* w, int u, float none, float* o) __attribute__((always_inline)) {
     const int c = (t + u * threads) * 8;
-    if (w != nullptr && (!VEC || c < D)) {
+    if (w != nullptr && (!VEC || c < D)) {  // (VEC: a branch 1 us shorter for one row than selects)
       Raw8<float> r;
+      load_chunk<VEC, false>(r, w, c, D);
       if constexpr (VEC)
-        r.load(w + c);
+        r.unpack(o);
       else
-        load_chunk<false>(r, w, c, D);
-      r.unpack(o);
+        unpack_chunk<false>(r, c, D, o);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) o[j] = none;
@@ -125,13 +125,8 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
       const int c = (t + u * threads) * 8;
       const TZ* z = static_cast<const TZ*>(p.z) + row * p.ldz;
       const TX* x = static_cast<const TX*>(p.x) + xr * p.ldx;
-      if constexpr (VEC) {
-        nz[u].load_nt(z + (c < D ? c : 0));
-        nx[u].load_nt(x + (c < D ? c : 0));
-      } else {
-        load_chunk<false>(nz[u], z, c, D);
-        load_chunk<false>(nx[u], x, c, D);
-      }
+      load_chunk<VEC, true>(nz[u], z, c, D);
+      load_chunk<VEC, true>(nx[u], x, c, D);
     }
   };
   const int64_t base = static_cast<int64_t>(blockIdx.x) * rows_per_wg;
@@ -156,20 +151,17 @@ __global__ void __launch_bounds__(MAXT) gated_norm_k(GatedNormArgs p, int thread
     float v[NV][8];
     bool bad = nbad;
 #pragma unroll
-    for (int u = 0; u < NV; ++u) {
-      nz[u].unpack(v[u]);
-      if constexpr (VEC) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[u][j] = in(u, j) ? v[u][j] : 0.0f;
-      }
-    }
+    for (int u = 0; u < NV; ++u) unpack_chunk<VEC>(nz[u], (t + u * threads) * 8, D, v[u]);
     bad = bad || no_group;
     if (p.after != NORM_NONE) norm(v, p.after, 0);
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       float m[8], x[8];
       if constexpr (!HOLD) gate_of(gm, u, m);
-      nx[u].unpack(x);
+      if constexpr (VEC)
+        nx[u].unpack(x);  // (zeroed past the row's end below)
+      else
+        unpack_chunk<false>(nx[u], (t + u * threads) * 8, D, x);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         v[u][j] = fmaf(v[u][j], HOLD ? ga[HOLD ? u : 0][j] : m[j], p.alpha * x[j]);
@@ -230,7 +222,7 @@ hipError_t launch_w(const GatedNormArgs& p, int threads, hipStream_t stream) {
 // 400000 x 64: 16 lanes to a row 67, a wave 193).  Wider rows, and unaligned ones whose
 // bounds would take the registers of a second chunk, go to up to 1024 threads with one
 // chunk, two from 8192 columns on (16000 x 8192: 327, four to 256 threads 354; 9000 x
-// 13824: 359, four to 448 threads 395; 7524 x 7341: 206, four to 256 threads 617).
+// 13824: 359, four to 448 threads 395; 7524 x 7341: 166, four to 256 threads 617).
 template <bool VEC>
 hipError_t launch_v(const GatedNormArgs& p, hipStream_t stream) {
   auto threads = [&](int chunks) { return (p.D + 8 * chunks * kWave - 1) / (8 * chunks * kWave) * kWave; };

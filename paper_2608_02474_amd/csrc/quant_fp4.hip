@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(256) quantize_fp4_k(QuantizeArgs p, int64_t st
       const T* x = static_cast<const T*>(p.x);
       bad[u] = false;
       if (row < p.M) x += row_of(p, row, bad[u]) * p.ldx;
-      load_chunk<VEC>(raw[u], x, c, p.D);
+      load_chunk<VEC, true>(raw[u], x, c, p.D);
       row += step_row;
       set += step_set;
       if (set >= sets) set -= sets, ++row;
@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(256) quantize_fp4_k(QuantizeArgs p, int64_t st
     for (int u = 0; u < U; ++u) {
       if (rows[u] >= p.M) break;
       float f[8];
-      raw[u].unpack(f);
+      unpack_chunk<VEC>(raw[u], at[u] * 128 + lane * 8, p.D, f);
       uint32_t scales;
       const uint32_t w = codes8_fp4(f, bad[u], scales);
       put_set(p, rows[u], at[u], w, scales);
@@ -142,20 +142,13 @@ __global__ void __launch_bounds__(MAXT) quantize_fp4_ln_k(QuantizeArgs p, int th
   auto modulation = [&](int u, float* sc, float* sh) __attribute__((always_inline)) {
     const int c = (t + u * threads) * 8;
     Raw8<float> rs, rh;
-    if constexpr (VEC) {
-      rs.load(p.scale + (c < D ? c : 0));
-      rh.load(p.shift + (c < D ? c : 0));
-    } else {
-      load_chunk<false>(rs, p.scale, c, D);
-      load_chunk<false>(rh, p.shift, c, D);
-    }
-    rs.unpack(sc);
-    rh.unpack(sh);
+    load_chunk<VEC, false>(rs, p.scale, c, D);
+    load_chunk<VEC, false>(rh, p.shift, c, D);
+    unpack_chunk<VEC>(rs, c, D, sc);
+    unpack_chunk<VEC>(rh, c, D, sh);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const bool in = VEC ? c < D : c + j < D;
-      sc[j] = in ? 1.0f + sc[j] : 0.0f;
-      sh[j] = in ? sh[j] : 0.0f;
+      sc[j] = (VEC ? c < D : c + j < D) ? 1.0f + sc[j] : 0.0f;
     }
   };
   float sc[HOLD ? NV : 1][8], sh[HOLD ? NV : 1][8];
@@ -169,7 +162,7 @@ __global__ void __launch_bounds__(MAXT) quantize_fp4_ln_k(QuantizeArgs p, int th
     const T* x = static_cast<const T*>(p.x) + row_of(p, row, next_bad) * p.ldx;
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
-      load_chunk<VEC>(next[AHEAD ? u : 0], x, (t + u * threads) * 8, D);
+      load_chunk<VEC, true>(next[AHEAD ? u : 0], x, (t + u * threads) * 8, D);
     }
   };
   const int64_t base = static_cast<int64_t>(blockIdx.x) * rows_per_wg;
@@ -186,11 +179,11 @@ __global__ void __launch_bounds__(MAXT) quantize_fp4_ln_k(QuantizeArgs p, int th
 #pragma unroll
     for (int u = 0; u < NV; ++u) {
       if constexpr (AHEAD) {
-        next[u].unpack(v[u]);
+        unpack_chunk<VEC>(next[u], (t + u * threads) * 8, D, v[u]);
       } else {
         Raw8<T> raw;
-        load_chunk<VEC>(raw, x, (t + u * threads) * 8, D);
-        raw.unpack(v[u]);
+        load_chunk<VEC, true>(raw, x, (t + u * threads) * 8, D);
+        unpack_chunk<VEC>(raw, (t + u * threads) * 8, D, v[u]);
       }
     }
     if constexpr (AHEAD)
@@ -258,7 +251,9 @@ constexpr int64_t kMaxGroups = 1 << 20;  // workgroups of a launch; more rows th
 template <typename T, bool VEC>
 hipError_t launch_plain(const QuantizeArgs& p, hipStream_t stream) {
   const int sets = (p.D + 127) / 128;
-  const int64_t n = (static_cast<int64_t>(p.M) * sets + 63) / 64;  // four sets to 16 lanes
+  // four sets to 16 lanes, one where there are few (300 x 1536: 2.3 us, 3.2 with four)
+  const int64_t all = static_cast<int64_t>(p.M) * sets;
+  const int64_t n = all <= static_cast<int64_t>(device_cu_count()) * 32 ? (all + 15) / 16 : (all + 63) / 64;
   const int64_t wgs = n < kMaxGroups ? n : kMaxGroups;
   return ECHO_LAUNCH("quantize_rows_fp4", (quantize_fp4_k<T, VEC>), dim3(static_cast<unsigned>(wgs)), dim3(256), 0,
                      stream, p, wgs * 16 / sets, static_cast<int>(wgs * 16 % sets));
@@ -279,8 +274,8 @@ hipError_t launch_ln(const QuantizeArgs& p, int threads, hipStream_t stream) {
 // What a reduction costs a wave is shared by its chunks, what it waits for by the
 // workgroups of a CU: up to 512 columns 16 lanes with up to four chunks a row, up to
 // 1024 a wave, then up to 256 threads with up to three chunks and no more threads than
-// that takes (32760 x 5120: three chunks to 256 threads 102 us, two to 320 142; 100000 x
-// 1024: two to a wave 60, one to 128 threads 73; 16000 x 8192: two to 512 threads 96, four
+// that takes (32760 x 5120: three chunks to 256 threads 106 us, two to 320 142; 100000 x
+// 1024: two to a wave 60, one to 128 threads 73; 16000 x 8192: two to 512 threads 84, four
 // to 256 102; 13104 x 13824: four to 448 threads 149, two to 896 172, 181 if they hold the
 // modulation).
 template <typename T, bool VEC>
