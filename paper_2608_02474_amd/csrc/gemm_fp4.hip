@@ -525,9 +525,90 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 4))
   }
 }
 
+// ---- three to 32 tokens: one launch of many small workgroups, where a tile's stages
+// and a second launch to join the depth's pieces would be most of the time.  A workgroup
+// takes R times sixteen channels, and its waves share the depth: a wave reads 256 codes
+// of every channel at a time, U such pieces in flight, and the same codes of the tokens,
+// sixteen to an instruction's columns.  The waves' sums meet in LDS and are added in the
+// waves' order.  The fragments are read as the instruction holds them, neighbouring lanes
+// in different rows, which the first-level cache serves at an eighth of its rate: that
+// bounds it (8 tokens on 1536 x 1536 codes 2.8 us where tiles and rows of 4.8 are, on
+// 5120 x 5120 7.2 and 9.7, but on 30720 x 5120 22.7 and 15.1).
+template <int TT, int R, int U, int EPI, bool CBF>
+__global__ void __launch_bounds__(1024) gemm_fp4_few(GemmFp4Args p) {
+  extern __shared__ f32x4 sums[];  // [wave][R][TT][lane]
+  const int lane = threadIdx.x % kWave, waves = blockDim.x / kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int l16 = lane & 15, lq = lane / 16, n0 = blockIdx.x * 16 * R, units = p.K / 128;
+  const uint8_t *w[R], *ws[R], *a[TT], *as[TT];  // (rows past the last one: the last one, not stored)
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t n = n0 + 16 * r + l16 < p.N ? n0 + 16 * r + l16 : p.N - 1;
+    w[r] = p.B + n * p.ldb + lq * 32;
+    ws[r] = p.sb + n * p.ldsb + lq * 2;
+  }
+#pragma unroll
+  for (int t = 0; t < TT; ++t) {
+    const int64_t m = 16 * t + l16 < p.M ? 16 * t + l16 : p.M - 1;
+    a[t] = p.A + m * p.lda + lq * 32;
+    as[t] = p.sa + m * p.ldsa + lq * 2;
+  }
+  f32x4 acc[R][TT];
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) acc[r][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int u0 = wave * U; u0 < units; u0 += waves * U) {
+    i32x4 wf[U][R][2], af[U][TT][2];
+    int wsc[U][R], asc[U][TT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = u0 + u < units ? u0 + u : u0;  // (past the depth: read again, not used)
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const u32x4_t* q = reinterpret_cast<const u32x4_t*>(w[r] + k * 128);
+        wf[u][r][0] = __builtin_bit_cast(i32x4, q[0]);
+        wf[u][r][1] = __builtin_bit_cast(i32x4, q[1]);
+        wsc[u][r] = *reinterpret_cast<const uint16_t*>(ws[r] + k * 8);
+      }
+#pragma unroll
+      for (int t = 0; t < TT; ++t) {
+        const i32x4* q = reinterpret_cast<const i32x4*>(a[t] + k * 128);
+        af[u][t][0] = q[0];
+        af[u][t][1] = q[1];
+        asc[u][t] = *reinterpret_cast<const uint16_t*>(as[t] + k * 8);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (u0 + u >= units) break;
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+          acc[r][t] = mfma_fp4<0>(wf[u][r][0], wsc[u][r], af[u][t][0], asc[u][t], acc[r][t]);
+          acc[r][t] = mfma_fp4<1>(wf[u][r][1], wsc[u][r], af[u][t][1], asc[u][t], acc[r][t]);
+        }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int t = 0; t < TT; ++t) sums[((wave * R + r) * TT + t) * kWave + lane] = acc[r][t];
+  __syncthreads();
+  for (int e = threadIdx.x; e < R * TT * kWave; e += blockDim.x) {
+    f32x4 z = sums[e];
+    for (int v = 1; v < waves; ++v) z += sums[v * R * TT * kWave + e];
+    const int l = e % kWave, rt = e / kWave, m = rt % TT * 16 + l % 16, n = n0 + rt / TT * 16 + l / 16 * 4;
+    if (m < p.M && n < p.N) out_put4<EPI, CBF>(p, m, n, z);
+  }
+}
+
 namespace {
 
-constexpr int kRowMax = 8;  // most tokens of gemm_fp4_row
+constexpr int kRowMax = 8;   // most tokens of gemm_fp4_row
+constexpr int kFewMax = 32;  // and of gemm_fp4_few
 
 enum Fp4Tile { FP4_256, FP4_128, FP4_64 };
 constexpr int kTileEdge[] = {256, 128, 64};
@@ -650,20 +731,49 @@ hipError_t launch_row(int epi, const GemmFp4Args& a, hipStream_t stream) {
   });
 }
 
+template <int TT, int R, int U>
+hipError_t launch_few(int epi, const GemmFp4Args& a, hipStream_t stream) {
+  // as many waves as the depth keeps busy, up to 16, with equal shares
+  const int pieces = (a.K / 128 + U - 1) / U, rounds = (pieces + 15) / 16, waves = (pieces + rounds - 1) / rounds;
+  const dim3 grid(static_cast<unsigned>((a.N + 16 * R - 1) / (16 * R)));
+  return with_epilogue(epi, a.c_bf16, 1, [&](auto epi_c, auto bf_c, auto) -> hipError_t {
+    return ECHO_LAUNCH("gemm_fp4_few", (gemm_fp4_few<TT, R, U, decltype(epi_c)::value, decltype(bf_c)::value>), grid,
+                       dim3(waves * kWave), static_cast<unsigned>(waves * R * TT * kWave * 16), stream, a);
+  });
+}
+
 }  // namespace
 
-// Whether a product of few tokens goes by rows: it reads the weights at the memory's
+// How a product is done.  Of few tokens by rows: that reads the weights at the memory's
 // rate, but the tokens' codes again for every two channels, through the same path
 // (1 / 2 / 4 / 8 tokens on 5120 x 5120 codes 5.0 / 5.7 / 6.5 / 9.7 us, tiles 11.3; on
-// 30720 x 5120 15.9 / 16.9 / 23.1 / 35.5, tiles 20.2).
-static bool fp4_by_rows(int M, int N, int K, const Fp4Plan& plan) {
-  return M <= 2 || (M <= kRowMax && 2.9f + (0.15f + 0.031f * M) * 1e-6f * N * K < plan.us);
+// 30720 x 5120 15.9 / 16.9 / 23.1 / 35.5, tiles 20.2); or by groups of 16 or 32
+// channels, whose time is their rounds on the device by the depth (16 tokens on 1536 x
+// 1536 / 5120 x 5120 3.0 / 7.9, tiles 4.2 / 10.5); else in tiles.
+enum Fp4Way { FP4_TILES, FP4_ROWS, FP4_FEW16, FP4_FEW32 };
+static Fp4Way fp4_way(int M, int N, int K, const Fp4Plan& plan) {
+  if (M <= 2) return FP4_ROWS;
+  Fp4Way way = FP4_TILES;
+  float us = plan.us;  // (up to a sixth too long for 9 to 32 tokens on deep rows: `margin`)
+  auto consider = [&](Fp4Way w, float t) {
+    if (t < us) us = t, way = w;
+  };
+  const float margin = M <= kRowMax ? 1.0f : 1.17f;
+  const float depth = K / 512.0f;  // 1024 codes
+  auto rounds = [&](int channels) {
+    const int ncu = device_cu_count(), wgs = (N + channels - 1) / channels;
+    return static_cast<float>((wgs + ncu - 1) / ncu);
+  };
+  if (M <= kRowMax) consider(FP4_ROWS, 2.9f + (0.15f + 0.031f * M) * 1e-6f * N * K);
+  if (M <= kFewMax) consider(FP4_FEW16, margin * (2.2f + rounds(16) * depth * (0.42f + 0.0185f * M)));
+  if (M <= kFewMax) consider(FP4_FEW32, margin * (2.4f + rounds(32) * depth * (0.82f + 0.0185f * M)));
+  return way;
 }
 
 size_t gemm_fp4_partial_bytes(int M, int N, int K, int epi) {
   if (M <= 2) return 0;
   const Fp4Plan plan = fp4_plan(M, N, K, epi);
-  return fp4_by_rows(M, N, K, plan) ? 0 : fp4_part_bytes(plan, M, N);
+  return fp4_way(M, N, K, plan) != FP4_TILES ? 0 : fp4_part_bytes(plan, M, N);
 }
 
 hipError_t launch_gemm_fp4(int epi, const GemmFp4Args& a, hipStream_t stream) {
@@ -672,8 +782,12 @@ hipError_t launch_gemm_fp4(int epi, const GemmFp4Args& a, hipStream_t stream) {
   if (a.M == 1) return launch_row<1, 2, 3>(epi, a, stream);
   if (a.M == 2) return launch_row<2, 2, 3>(epi, a, stream);
   const Fp4Plan plan = fp4_plan(a.M, a.N, a.K, epi);
-  if (fp4_by_rows(a.M, a.N, a.K, plan))
-    return a.M <= 4 ? launch_row<4, 2, 3>(epi, a, stream) : launch_row<8, 2, 3>(epi, a, stream);
+  switch (fp4_way(a.M, a.N, a.K, plan)) {
+    case FP4_ROWS: return a.M <= 4 ? launch_row<4, 2, 3>(epi, a, stream) : launch_row<8, 2, 3>(epi, a, stream);
+    case FP4_FEW16: return a.M <= 16 ? launch_few<1, 1, 2>(epi, a, stream) : launch_few<2, 1, 2>(epi, a, stream);
+    case FP4_FEW32: return a.M <= 16 ? launch_few<1, 2, 2>(epi, a, stream) : launch_few<2, 2, 2>(epi, a, stream);
+    case FP4_TILES: break;
+  }
   if (fp4_part_bytes(plan, a.M, a.N) > a.part_bytes) return hipErrorInvalidValue;
   switch (plan.tile) {
     case FP4_256: return launch_tile<256>(epi, a, plan, stream);

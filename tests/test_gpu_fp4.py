@@ -257,7 +257,9 @@ SIZES = [(1, 1, 1), (1, 16, 64), (1, 300, 5120), (2, 77, 129), (4, 33, 2049), (5
          (16, 64, 128), (17, 129, 640), (32, 48, 256), (33, 100, 100), (48, 1000, 2600), (64, 512, 1024), (65, 65, 65),
          (100, 200, 300), (128, 128, 128), (130, 70, 13824), (257, 255, 200), (300, 512, 256), (500, 1030, 384),
          (1000, 96, 4000), (1111, 2049, 130), (2100, 2304, 768), (4100, 4100, 128), (70, 300, 40000), (4200, 4400, 1100),
-         (3000, 6400, 1500), (5000, 5128, 300)]
+         (3000, 6400, 1500), (5000, 5128, 300), (3, 5, 30), (3, 1536, 1536), (8, 1001, 1535), (15, 5130, 1500),
+         (16, 2000, 5120), (7, 5131, 5000), (16, 5120, 5120), (18, 5121, 1537), (31, 2100, 515), (32, 1536, 1536),
+         (32, 9000, 256), (12, 37, 33000), (25, 8300, 4097)]
 
 
 @pytest.mark.parametrize("out_dtype", [torch.bfloat16, torch.float32])
@@ -272,7 +274,7 @@ def test_linear_sizes(M, N, K, out_dtype):
     check_linear(got.cpu(), a, w, bias, out_dtype, what=f"{M}x{N}x{K}")
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 200, 300), (6, 60, 1500), (12, 96, 520), (20, 77, 130), (60, 64, 512),
+@pytest.mark.parametrize("M,N,K", [(1, 200, 300), (6, 60, 1500), (12, 96, 520), (13, 1500, 1536), (29, 5120, 1500), (20, 77, 130), (60, 64, 512),
                                    (140, 260, 260), (700, 1000, 200), (4096, 4100, 128), (90, 256, 8000), (4200, 4400, 1100),
                                    (5000, 5128, 300), (2600, 7000, 900)])
 @pytest.mark.parametrize("epi", ["none", "gelu", "gate_bf16", "gate_f32_rows"])
