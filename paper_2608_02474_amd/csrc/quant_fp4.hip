@@ -26,13 +26,16 @@
 namespace echo {
 
 // The 4-bit codes of a lane's 8 values, packed, and the scales of the four blocks of
-// its set of 16 lanes as one word.  bad: the row is not there.
-__device__ __forceinline__ uint32_t codes8_fp4(const float* v, bool bad, uint32_t& scales) {
+// its set of 16 lanes as one word.  bad: the row is not there.  A block that lies behind
+// the D columns is zeros also where the row is NaN.
+__device__ __forceinline__ uint32_t codes8_fp4(const float* v, int set, int D, bool bad, uint32_t& scales) {
   uint32_t top = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
   top = max(top, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(top), 0xb1, 0xf, 0xf, false)));
   top = max(top, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(top), 0x4e, 0xf, 0xf, false)));
+  const int block = threadIdx.x / 4 % 4;
+  const bool live = set * 128 + block * 32 < D;
   bad = bad || top >= 0x7f800000u;
   const uint32_t e = top >> 23, byte = e > 2 ? e - 2 : 0;
   uint32_t w = 0;
@@ -49,10 +52,10 @@ __device__ __forceinline__ uint32_t codes8_fp4(const float* v, bool bad, uint32_
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4] * k, v[5] * k, s, 2);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6] * k, v[7] * k, s, 3);
   }
-  scales = (bad ? 255u : byte) << (threadIdx.x / 4 % 4 * 8);
+  scales = (!live ? 0u : bad ? 255u : byte) << (block * 8);
   scales |= dpp_ror<4>(scales);
   scales |= dpp_ror<8>(scales);
-  return bad ? 0u : w;
+  return bad || !live ? 0u : w;
 }
 
 // Set `set` of a row: lane i of its 16 has the codes w and the scales' word.
@@ -109,7 +112,7 @@ __global__ void __launch_bounds__(256) quantize_fp4_k(QuantizeArgs p, int64_t st
       float f[8];
       unpack_chunk<VEC>(raw[u], at[u] * 128 + lane * 8, p.D, f);
       uint32_t scales;
-      const uint32_t w = codes8_fp4(f, bad[u], scales);
+      const uint32_t w = codes8_fp4(f, at[u], p.D, bad[u], scales);
       put_set(p, rows[u], at[u], w, scales);
     }
   }
@@ -216,7 +219,7 @@ __global__ void __launch_bounds__(MAXT) quantize_fp4_ln_k(QuantizeArgs p, int th
       for (int j = 0; j < 8; ++j)
         v[u][j] = fmaf(v[u][j] * rstd, HOLD ? sc[HOLD ? u : 0][j] : c8[j], HOLD ? sh[HOLD ? u : 0][j] : h8[j]);
       uint32_t scales;
-      const uint32_t w = codes8_fp4(v[u], bad, scales);
+      const uint32_t w = codes8_fp4(v[u], set, D, bad, scales);
       put_set(p, row, set, w, scales);
     }
   }
