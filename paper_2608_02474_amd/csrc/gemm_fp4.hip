@@ -705,14 +705,15 @@ hipError_t launch_tile(int epi, GemmFp4Args a, const Fp4Plan& plan, hipStream_t 
   return with_epilogue(epi, a.c_bf16, a.res_bf16, [&](auto epi_c, auto bf_c, auto res_c) -> hipError_t {
     constexpr int EPI = decltype(epi_c)::value;
     constexpr bool CBF = decltype(bf_c)::value, RBF = decltype(res_c)::value;
+    constexpr const char* kName = E == 256 ? "gemm_fp4_256" : E == 128 ? "gemm_fp4_128" : "gemm_fp4_64";
     hipError_t e;
     // (the smaller tiles have several workgroups to a CU, whose ends overlap)
     if (E == 256 && stream_fits(a)) {
       const int wgs = items < device_cu_count() ? items : device_cu_count();
-      e = ECHO_LAUNCH("gemm_fp4", (gemm_fp4_tile<E, E, EPI, CBF, RBF, E == 256>), dim3(static_cast<unsigned>(wgs)),
+      e = ECHO_LAUNCH("gemm_fp4_256_stream", (gemm_fp4_tile<E, E, EPI, CBF, RBF, E == 256>), dim3(static_cast<unsigned>(wgs)),
                       dim3(256), 0, stream, a);
     } else {
-      e = ECHO_LAUNCH("gemm_fp4", (gemm_fp4_tile<E, E, EPI, CBF, RBF, false>), dim3(static_cast<unsigned>(items)),
+      e = ECHO_LAUNCH(kName, (gemm_fp4_tile<E, E, EPI, CBF, RBF, false>), dim3(static_cast<unsigned>(items)),
                       dim3(256), 0, stream, a);
     }
     if (e != hipSuccess || tail == 0) return e;
