@@ -701,7 +701,8 @@ int echo_cross_attention(const echo_cross_attention_cfg* cfg, const void* q, con
  * q [B][L][H][dh], k [B][L][Hk][dh] (Hk = 0: none, k and k_out are not looked
  * at), q_out and k_out with their strides, in elements, as in
  * echo_cross_attention but of any multiple; dh values are contiguous.  An output
- * may be its input itself (same pointer and strides) and else overlaps no input.
+ * may be its input itself (same pointer and strides) and else overlaps no input; it
+ * holds no row twice (no stride of 0 along more than one element, row or head).
  * freq: device fp64 [dims / 2].  All pointers by their element type.
  * Requires 2 <= dims <= dh <= 512, dims even, H >= 1, H + Hk <= 65536, B * L <
  * 2^24, magnitude finite.  B, L >= 0 (0: no-op).

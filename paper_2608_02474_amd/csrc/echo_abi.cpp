@@ -347,6 +347,10 @@ bool rotary_supported(const echo_rotary_cfg* c) {
 bool same_strides(const echo_strides& a, const echo_strides& b) {
   return a.batch == b.batch && a.row == b.row && a.head == b.head;
 }
+// an output's rows: in the place of a repeated input row they would be turned once each
+bool rows_apart(const echo_strides& s, int32_t B, int32_t L, int32_t H) {
+  return (B == 1 || s.batch > 0) && (L == 1 || s.row > 0) && (H == 1 || s.head > 0);
+}
 
 // ---- norms on both sides of a sub-layer
 bool norm_ok(int n) { return n == ECHO_NORM_NONE || n == ECHO_NORM_RMS || n == ECHO_NORM_LAYER; }
@@ -961,6 +965,7 @@ int echo_rotary(const echo_rotary_cfg* cfg, const void* q, const void* k, const 
   if (!elem_aligned(q, es) || !elem_aligned(q_out, es) || !elem_aligned(freq, 8) ||
       (positions != nullptr && !elem_aligned(positions, 4)) ||
       (keys && (!elem_aligned(k, es) || !elem_aligned(k_out, es))) ||
+      !rows_apart(cfg->q_out, cfg->B, cfg->L, cfg->H) || (keys && !rows_apart(cfg->k_out, cfg->B, cfg->L, cfg->Hk)) ||
       (q == q_out && !same_strides(cfg->q, cfg->q_out)) ||
       (keys && k == k_out && !same_strides(cfg->k, cfg->k_out)))
     return ECHO_EINVAL;
