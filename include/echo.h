@@ -753,7 +753,8 @@ int echo_rotary(const echo_rotary_cfg* cfg, const void* q, const void* k, const 
  * Writes dims / 2 values to freq and one to magnitude (host pointers).  A grid
  * takes PLAIN and LINEAR.  Returns an echo_status: ECHO_EINVAL for dims odd or
  * outside [2, 512], base <= 1, factor < 1, original_length < 1, low <= 0 or high
- * <= low where they are used, values that are not finite, or null pointers.
+ * <= low where they are used, values that are not finite (the base of ECHO_ROTARY_BASE
+ * among them), or null pointers.
  */
 typedef enum {
   ECHO_ROTARY_PLAIN = 0,

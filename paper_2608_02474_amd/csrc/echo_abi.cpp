@@ -1002,6 +1002,7 @@ int echo_rotary_frequencies(const echo_rotary_freq_cfg* cfg, double* freq, float
                 !std::isfinite(cfg->high) || !(cfg->high > cfg->low)))
     return ECHO_EINVAL;
   const double base = s == ECHO_ROTARY_BASE ? cfg->base * std::pow(cfg->factor, cfg->dims / (cfg->dims - 2.0)) : cfg->base;
+  if (!std::isfinite(base)) return ECHO_EINVAL;
   const auto clamp = [](double v, double lo, double hi) { return v < lo ? lo : v > hi ? hi : v; };
   const auto pair_of = [&](double turns) {
     return n * std::log(cfg->original_length / (kTwoPi * turns)) / std::log(base);

@@ -1,10 +1,10 @@
 """Refusals of the rotary positions at the C entries, on the CPU: outputs that hold a row
-more than once."""
+more than once, and frequencies whose base is past fp64."""
 import ctypes
 
 import pytest
 
-from paper_2608_02474_amd import _lib
+from paper_2608_02474_amd import _lib, api
 
 FAKE, FAKE2 = ctypes.c_void_p(0x10000), ctypes.c_void_p(0x20000)
 F3, F4 = ctypes.c_void_p(0x30000), ctypes.c_void_p(0x40000)
@@ -29,3 +29,12 @@ def test_outputs_hold_no_row_twice(at):
     assert run(q=zero, qo=zero, out=FAKE) == _lib.ECHO_EINVAL
     assert run(k=zero, ko=zero, k_out=FAKE2) == _lib.ECHO_EINVAL
     assert run(B=0, qo=zero) == _lib.ECHO_OK                       # nothing to write
+
+
+def test_bases_past_fp64_are_refused():
+    """base factor^(dims / (dims - 2)) overflows: every frequency but the first would be 0."""
+    kw = dict(scaling="base", base=1e300, factor=1e6)
+    with pytest.raises(RuntimeError, match="echo_rotary_frequencies"):
+        api.rotary_frequencies(4, **kw)
+    freq, _, _ = api.rotary_frequencies(64, **{**kw, "base": 1e4})
+    assert all(f > 0 for f in freq)
