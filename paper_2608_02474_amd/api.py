@@ -482,7 +482,7 @@ def block_partial(params: dict, x: torch.Tensor, idx: torch.Tensor, n_sel: int, 
         if batch_invariant:
             raise ValueError("batch_invariant does not go with weights in 8 bits or 4")
         return _block_partial_rows(params, x, idx, n_sel, H, ln_eps, y_sel, workspace, rotary)
-    if rotary is not None or "after1" in params or "after2" in params:
+    if rotary is not None or params.get("after1") is not None or params.get("after2") is not None:
         raise ValueError("rotary and norms after the sub-layers go with weights in 8 or 4 bits")
     lib = _lib_handle()
     _dev(x, "x")
