@@ -26,16 +26,14 @@
 namespace echo {
 
 // The 4-bit codes of a lane's 8 values, packed, and the scales of the four blocks of
-// its set of 16 lanes as one word.  bad: the row is not there.  A block that lies behind
-// the D columns is zeros also where the row is NaN.
-__device__ __forceinline__ uint32_t codes8_fp4(const float* v, int set, int D, bool bad, uint32_t& scales) {
+// its set of 16 lanes as one word.  bad: the row is not there.  live: the lane's block has
+// columns; one behind the last column is zeros also where the row is NaN.
+__device__ __forceinline__ uint32_t codes8_fp4(const float* v, bool bad, bool live, uint32_t& scales) {
   uint32_t top = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
   top = max(top, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(top), 0xb1, 0xf, 0xf, false)));
   top = max(top, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(top), 0x4e, 0xf, 0xf, false)));
-  const int block = threadIdx.x / 4 % 4;
-  const bool live = set * 128 + block * 32 < D;
   bad = bad || top >= 0x7f800000u;
   const uint32_t e = top >> 23, byte = e > 2 ? e - 2 : 0;
   uint32_t w = 0;
@@ -52,7 +50,7 @@ __device__ __forceinline__ uint32_t codes8_fp4(const float* v, int set, int D, b
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4] * k, v[5] * k, s, 2);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6] * k, v[7] * k, s, 3);
   }
-  scales = (!live ? 0u : bad ? 255u : byte) << (block * 8);
+  scales = (!live ? 0u : bad ? 255u : byte) << (threadIdx.x / 4 % 4 * 8);
   scales |= dpp_ror<4>(scales);
   scales |= dpp_ror<8>(scales);
   return bad || !live ? 0u : w;
@@ -69,6 +67,11 @@ __device__ __forceinline__ void put_set(const QuantizeArgs& p, int64_t row, int 
     if (sets % 2 == 1) *reinterpret_cast<uint32_t*>(codes + 64 + 4 * i) = 0;
     if (i > 0 && i <= 3 - (sets - 1) % 4) *reinterpret_cast<uint32_t*>(sc + 4 * i) = 0;
   }
+}
+
+// whether the lane's block of a set has columns
+__device__ __forceinline__ bool live_block(const QuantizeArgs& p, int set) {
+  return set * 128 + static_cast<int>(threadIdx.x / 4 % 4) * 32 < p.D;
 }
 
 __device__ __forceinline__ int64_t row_of(const QuantizeArgs& p, int64_t row, bool& bad) {
@@ -101,6 +104,8 @@ __global__ void __launch_bounds__(256) quantize_fp4_k(QuantizeArgs p, int64_t st
       const T* x = static_cast<const T*>(p.x);
       bad[u] = false;
       if (row < p.M) x += row_of(p, row, bad[u]) * p.ldx;
+      // (blocks behind the last column hold zeros here, so a row that is not there is all that makes them NaN)
+      if (p.rows != nullptr) bad[u] = bad[u] && live_block(p, set);
       load_chunk<VEC, true>(raw[u], x, c, p.D);
       row += step_row;
       set += step_set;
@@ -112,7 +117,7 @@ __global__ void __launch_bounds__(256) quantize_fp4_k(QuantizeArgs p, int64_t st
       float f[8];
       unpack_chunk<VEC>(raw[u], at[u] * 128 + lane * 8, p.D, f);
       uint32_t scales;
-      const uint32_t w = codes8_fp4(f, at[u], p.D, bad[u], scales);
+      const uint32_t w = codes8_fp4(f, bad[u], true, scales);
       put_set(p, rows[u], at[u], w, scales);
     }
   }
@@ -219,7 +224,7 @@ __global__ void __launch_bounds__(MAXT) quantize_fp4_ln_k(QuantizeArgs p, int th
       for (int j = 0; j < 8; ++j)
         v[u][j] = fmaf(v[u][j] * rstd, HOLD ? sc[HOLD ? u : 0][j] : c8[j], HOLD ? sh[HOLD ? u : 0][j] : h8[j]);
       uint32_t scales;
-      const uint32_t w = codes8_fp4(v[u], set, D, bad, scales);
+      const uint32_t w = codes8_fp4(v[u], bad, live_block(p, set), scales);
       put_set(p, row, set, w, scales);
     }
   }
