@@ -204,7 +204,9 @@ namespace {
 template <int MAXT, int NV, bool VEC, bool HOLD, bool NARROW = false>
 hipError_t launch_w(const GatedNormArgs& p, int threads, hipStream_t stream) {
   const int block = threads <= kWave ? 256 : threads, rpb = block / threads;
-  // consecutive rows of a workgroup share one read of the vectors
+  // consecutive rows of a workgroup share one read of the vectors; of few rows each has a
+  // workgroup of its own, which reads them all (1950 x 1536, five vectors: 10.6 us, 60 MB of
+  // vectors from the L2s beside 36 MB of rows)
   // (a whole number of workgroups to a CU: 9000 x 13824 takes 431 us with 7/3 of them)
   const int64_t want = static_cast<int64_t>(device_cu_count()) * (2048 / block);
   int64_t per = (p.M + want - 1) / want;

@@ -155,7 +155,8 @@ __global__ void __launch_bounds__(256, (BM + BN <= 256 ? 2 : 1)) gemm_fp4_tile(G
 
   const int rd_a = (wm * WM + l16) * 128, rd_b = (BM + wn * WN + l16) * 128;
   // the halves of a k-step are its even and its odd blocks, so that a lane's two
-  // scales are neighbours
+  // scales are neighbours; in this order lanes of lq 0 and 1 (2 and 3) share banks, four
+  // cycles more for each read of 16 bytes, which the order of gemm_int8.hip does not have
   const int rd_sa = (wm * WM + l16) * 16 + 2 * lq, rd_sb = (BM + wn * WN + l16) * 16 + 2 * lq;
   const int ch0 = ((2 * lq) ^ (l16 >> 1)) * 16, ch1 = ((2 * lq + 1) ^ (l16 >> 1)) * 16;
   i32x4 fa[2][TI], fb[2][TJ];
@@ -710,8 +711,8 @@ hipError_t launch_tile(int epi, GemmFp4Args a, const Fp4Plan& plan, hipStream_t 
     // (the smaller tiles have several workgroups to a CU, whose ends overlap)
     if (E == 256 && stream_fits(a)) {
       const int wgs = items < device_cu_count() ? items : device_cu_count();
-      e = ECHO_LAUNCH("gemm_fp4_256_stream", (gemm_fp4_tile<E, E, EPI, CBF, RBF, E == 256>), dim3(static_cast<unsigned>(wgs)),
-                      dim3(256), 0, stream, a);
+      e = ECHO_LAUNCH("gemm_fp4_256_stream", (gemm_fp4_tile<E, E, EPI, CBF, RBF, E == 256>),
+                      dim3(static_cast<unsigned>(wgs)), dim3(256), 0, stream, a);
     } else {
       e = ECHO_LAUNCH(kName, (gemm_fp4_tile<E, E, EPI, CBF, RBF, false>), dim3(static_cast<unsigned>(items)),
                       dim3(256), 0, stream, a);

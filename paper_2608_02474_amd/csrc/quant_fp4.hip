@@ -285,7 +285,8 @@ hipError_t launch_ln(const QuantizeArgs& p, int threads, hipStream_t stream) {
 // that takes (32760 x 5120: three chunks to 256 threads 106 us, two to 320 142; 100000 x
 // 1024: two to a wave 60, one to 128 threads 73; 16000 x 8192: two to 512 threads 84, four
 // to 256 102; 13104 x 13824: four to 448 threads 149, two to 896 172, 181 if they hold the
-// modulation).
+// modulation).  Rows of more than 16384 columns are more than 1024 threads hold: 71 to 85
+// registers spill (5120 x 32768: 341 us, 1.25 TB/s; 10240 x 16384 without: 134, 3.2).
 template <typename T, bool VEC>
 hipError_t launch_ln_width(const QuantizeArgs& p, hipStream_t stream) {
   auto threads = [&](int chunks) { return (p.D + 8 * chunks * kWave - 1) / (8 * chunks * kWave) * kWave; };
